@@ -278,7 +278,8 @@ def prepare(case, seed):
     st = {"case": c, "x": _logits(c, seed), "u": _uniform(seed, 2, (rows,)).clamp_max(1.0 - 2.0 ** -24),
           "t": _uniform(seed, 3, (rows,), 0.6, 1.2), "top_k": None, "top_p": None, "min_p": None,
           "tokens": empty((rows,), torch.int32), "kept": empty((rows,), torch.int32), "logprob": empty((rows,), torch.float32),
-          "filtered": empty((rows, c["vocab"]), torch.float32) if c["out"] else None}
+          "filtered": empty((rows, c["vocab"]), torch.float32) if c["out"] else None,
+          "work": empty((rows, 32768), torch.float32)}      # what the parts of a long row leave to each other
     if "k" in on:
         st["top_k"] = torch.randint(20, 200, (rows,), generator=_gen(seed, 4), device="cuda", dtype=torch.int32)
     if "p" in on:
@@ -421,7 +422,7 @@ def _own(st):
                               c["head_dim"] ** -0.5, st["out"], st["work"])
         return {"out": st["out"], "data": st["data"], "scales": st["scales"]}
     sv.spec_filter_sample(st["x"], st["u"], st["t"], st["tokens"], st["top_k"], st["top_p"], st["min_p"], st["logprob"],
-                          st["kept"], st["filtered"])
+                          st["kept"], st["filtered"], st["work"])
     out = {"tokens": st["tokens"], "kept": st["kept"], "logprob": st["logprob"]}
     if st["filtered"] is not None:
         out["filtered"] = st["filtered"]
