@@ -1,5 +1,5 @@
-"""ctypes binding of libspecverify.so: the same entry points as include/spec_verify.h,
-include/spec_decode.h and include/spec_kernels.h, taking torch tensors where the C side takes device pointers.  Argument
+"""ctypes binding of libspecverify.so: the same entry points as include/spec_verify.h, include/spec_decode.h,
+include/spec_q8.h and include/spec_kernels.h, taking torch tensors where the C side takes device pointers.  Argument
 marshalling only -- no arithmetic of the method happens here, and there is no fallback: if the
 HIP library is missing or fails to load, every call raises."""
 from __future__ import annotations
@@ -79,6 +79,21 @@ class spec_lookahead_cfg(C.Structure):
 class spec_decode_view(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("tokens", "n_tokens", "n_accepted", "draft_tokens", "draft_logits",
                                           "target_logits", "prev_token", "last_token", "counters")]
+
+
+class spec_kv8_cache(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scales", C.c_void_p), ("table", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_pages", "n_kv_heads", "head_dim", "batch", "blocks_per_seq")]
+
+
+class spec_filter_args(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("ld", C.c_int64),
+                ("uniforms", C.c_void_p), ("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p)]
+
+
+class spec_filter_out(C.Structure):
+    _fields_ = [("tokens", C.c_void_p), ("logprob", C.c_void_p), ("n_kept", C.c_void_p), ("logits_out", C.c_void_p)]
 
 
 PLAN_MAX_PASSES, PLAN_PROJECTIONS = 32, 5
@@ -174,6 +189,22 @@ def lib():
         L.spec_lookahead_update_per_seq.argtypes = [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
         L.spec_lookahead_accept.argtypes = [C.c_void_p, C.c_int32]
         L.spec_lookahead_accept.restype = C.c_double
+        i32, i64, ptr, f32 = C.c_int32, C.c_int64, C.c_void_p, C.c_float
+        L.spec_q8_quantize.argtypes = [ptr, i32, i64, i32, i32, ptr, ptr, ptr]
+        L.spec_q8_add_rmsnorm.argtypes = [ptr, i32, ptr, i32, ptr, f32, i32, i32, ptr, ptr, ptr, ptr]
+        L.spec_q8_swiglu.argtypes = [ptr, i32, i32, i32, ptr, ptr, ptr]
+        L.spec_q8_packed_weight_bytes.restype = C.c_size_t
+        L.spec_q8_packed_weight_bytes.argtypes = [i32, i32]
+        L.spec_q8_pack_weight.argtypes = [ptr, ptr, i32, i32, ptr]
+        L.spec_q8_gemm.argtypes = [ptr, ptr, ptr, ptr, ptr, i32, i32, i32, i32, ptr]
+        L.spec_kv8_append.argtypes = [C.POINTER(spec_kv8_cache), ptr, i32, ptr, ptr, i32, i32, ptr, i32, ptr, ptr]
+        L.spec_kv8_workspace_bytes.restype = C.c_size_t
+        L.spec_kv8_workspace_bytes.argtypes = [i32, i32, i32]
+        L.spec_kv8_attention.argtypes = [C.POINTER(spec_kv8_cache), ptr, i64, i32, ptr, ptr, i32, i32, i32, f32, ptr, ptr,
+                                         C.c_size_t, ptr]
+        L.spec_filter_workspace_bytes.restype = C.c_size_t
+        L.spec_filter_workspace_bytes.argtypes = [i32, i32]
+        L.spec_filter_sample.argtypes = [C.POINTER(spec_filter_args), C.POINTER(spec_filter_out), ptr, C.c_size_t, ptr]
         _lib = L
     return _lib
 
@@ -413,6 +444,170 @@ def spec_decode_get_view(d: Decoder) -> spec_decode_view:
     v = spec_decode_view()
     _check(lib().spec_decode_get_view(d.ptr, C.byref(v)))
     return v
+
+
+# ---- 8-bit operators and filtered draws (include/spec_q8.h) ---------------------------------------
+
+_F8 = torch.float8_e4m3fn
+_DTYPES = {torch.float32: SPEC_DTYPE_FP32, torch.bfloat16: SPEC_DTYPE_BF16}
+
+
+def _dtype(t: torch.Tensor) -> int:
+    if t.dtype not in _DTYPES:
+        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _rows_ptr(t: torch.Tensor, cols: int) -> int:
+    """Device pointer of a [rows][cols] tensor whose rows are contiguous and any distance apart."""
+    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols or (t.stride(1) != 1 and cols > 1):
+        raise ValueError(f"expected a device tensor of rows of {cols} contiguous elements")
+    return t.data_ptr()
+
+
+def _expect(t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _q8_out(rows: int, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor], device):
+    kp = (cols + 127) // 128 * 128
+    if q is None:
+        q = torch.empty((rows, kp), dtype=_F8, device=device)
+    if scales is None:
+        scales = torch.empty((kp // 128, rows), dtype=torch.float32, device=device)
+    return _expect(q, (rows, kp)), _expect(scales, (kp // 128, rows))
+
+
+def spec_q8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """Rows of x [rows][cols] (any row stride) -> (q e4m3 [rows][Kp], scales fp32 [Kp/128][rows])."""
+    rows, cols = x.shape
+    q, scales = _q8_out(rows, cols, q, scales, x.device)
+    ld = x.stride(0) if rows > 1 else cols
+    _check(lib().spec_q8_quantize(_rows_ptr(x, cols), _dtype(x), ld, rows, cols, _ptr(q, _F8),
+                                  _ptr(scales, torch.float32), _stream(stream)))
+    return q, scales
+
+
+def spec_q8_add_rmsnorm(x: torch.Tensor, delta: Optional[torch.Tensor], gain: torch.Tensor, eps: float,
+                        x_out: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                        scales: Optional[torch.Tensor] = None, stream=None):
+    """x + delta -> x_out (may be x; None: not kept); its RMSNorm times gain -> (q, scales)."""
+    rows, cols = x.shape
+    q, scales = _q8_out(rows, cols, q, scales, x.device)
+    _check(lib().spec_q8_add_rmsnorm(_ptr(x), _dtype(x), _ptr(_expect(delta, x.shape)), 0 if delta is None else _dtype(delta),
+                                     _ptr(_expect(gain, (cols,)), torch.float32), float(eps), rows, cols,
+                                     _ptr(_expect(x_out, x.shape), x.dtype), _ptr(q, _F8), _ptr(scales, torch.float32),
+                                     _stream(stream)))
+    return q, scales
+
+
+def spec_q8_swiglu(gate_up: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """silu(gate) * up of [rows][gate columns | up columns] -> (q, scales)."""
+    rows, cols = gate_up.shape
+    if cols % 2:
+        raise ValueError("gate_up needs as many up columns as gate columns")
+    q, scales = _q8_out(rows, cols // 2, q, scales, gate_up.device)
+    _check(lib().spec_q8_swiglu(_ptr(gate_up), _dtype(gate_up), rows, cols // 2, _ptr(q, _F8), _ptr(scales, torch.float32),
+                                _stream(stream)))
+    return q, scales
+
+
+def spec_q8_packed_weight_bytes(n_out: int, n_in: int) -> int:
+    return int(lib().spec_q8_packed_weight_bytes(n_out, n_in))
+
+
+def spec_q8_pack_weight(src: torch.Tensor, stream=None) -> torch.Tensor:
+    """Row-major e4m3 [n_out][n_in] -> new device buffer in the tile order of spec_q8_gemm."""
+    n_out, n_in = src.shape
+    dst = torch.empty(spec_q8_packed_weight_bytes(n_out, n_in), dtype=_F8, device=src.device)
+    _check(lib().spec_q8_pack_weight(_ptr(src, _F8), _ptr(dst), n_out, n_in, _stream(stream)))
+    return dst
+
+
+def spec_q8_gemm(q: torch.Tensor, scales: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor, y: torch.Tensor, stream=None):
+    """y [M][N] (float32 or bfloat16) = rows (q [M][Kp], scales [Kp/128][M]) times the packed matrix, w_scales
+    [ceil(N/128)][Kp/128]."""
+    M, kp = q.shape
+    N = y.shape[1]
+    _expect(y, (M, N)), _expect(scales, (kp // 128, M)), _expect(w_scales, ((N + 127) // 128, kp // 128))
+    if w_packed.numel() != (N + 15) // 16 * 16 * kp or kp % 128:
+        raise ValueError(f"expected a packed matrix of {N} x {kp}")
+    _check(lib().spec_q8_gemm(_ptr(q, _F8), _ptr(scales, torch.float32), _ptr(w_packed, _F8), _ptr(w_scales, torch.float32), _ptr(y),
+                              _dtype(y), M, N, kp, _stream(stream)))
+    return y
+
+
+class Kv8Cache:
+    """One layer's 8-bit cache: data e4m3 [pages][kv heads][2][32 * head_dim], scales fp32 [pages][kv heads][2],
+    table int32 [batch][blocks].  Holds the tensors it points into."""
+
+    def __init__(self, data: torch.Tensor, scales: torch.Tensor, table: torch.Tensor, head_dim: int):
+        pages, heads = data.shape[0], data.shape[1]
+        _expect(data, (pages, heads, 2, 32 * head_dim)), _expect(scales, (pages, heads, 2))
+        self.data, self.scales, self.table = data, scales, table
+        self.c = spec_kv8_cache(_ptr(data, _F8), _ptr(scales, torch.float32), _ptr(table, torch.int32), pages, heads, head_dim,
+                                table.shape[0], table.shape[1])
+
+
+def spec_kv8_append(cache: Kv8Cache, qkv: torch.Tensor, row0: torch.Tensor, kv_len: torch.Tensor, n_q_heads: int, max_window: int,
+                    cos_sin: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, stream=None):
+    """The keys and values of qkv bf16 [rows][(q + 2 kv heads) * head_dim] -> the cache; rotated queries -> q_out."""
+    c = cache.c
+    rows = qkv.shape[0]
+    _expect(qkv, (rows, (n_q_heads + 2 * c.n_kv_heads) * c.head_dim)), _expect(row0, (c.batch + 1,)), _expect(kv_len, (c.batch,))
+    _expect(q_out, (rows, n_q_heads * c.head_dim))
+    max_pos = 0
+    if cos_sin is not None:
+        max_pos = cos_sin.shape[0]
+        _expect(cos_sin, (max_pos, c.head_dim // 2, 2))
+    _check(lib().spec_kv8_append(C.byref(c), _ptr(qkv, torch.bfloat16), n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
+                                 rows, max_window, _ptr(cos_sin, torch.float32), max_pos, _ptr(q_out, torch.bfloat16), _stream(stream)))
+
+
+def spec_kv8_workspace_bytes(rows: int, n_q_heads: int, head_dim: int) -> int:
+    return int(lib().spec_kv8_workspace_bytes(rows, n_q_heads, head_dim))
+
+
+def spec_kv8_attention(cache: Kv8Cache, q: torch.Tensor, row0: torch.Tensor, kv_len: torch.Tensor, n_q_heads: int, max_window: int,
+                       max_len: int, scale: float, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
+    """out bf16 [rows][n_q_heads * head_dim]; q: bf16 rows of as many elements, any multiple of 8 apart."""
+    c = cache.c
+    rows, cols = out.shape
+    _expect(out, (rows, n_q_heads * c.head_dim)), _expect(q, out.shape), _expect(row0, (c.batch + 1,)), _expect(kv_len, (c.batch,))
+    if q.dtype != torch.bfloat16:
+        raise ValueError(f"expected dtype {torch.bfloat16}, got {q.dtype}")
+    ld = q.stride(0) if rows > 1 else cols
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().spec_kv8_attention(C.byref(c), _rows_ptr(q, cols), ld, n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
+                                    rows, max_window, max_len, scale, _ptr(out, torch.bfloat16), _ptr(workspace), nbytes,
+                                    _stream(stream)))
+    return out
+
+
+def spec_filter_workspace_bytes(rows: int, vocab: int) -> int:
+    return int(lib().spec_filter_workspace_bytes(rows, vocab))
+
+
+def spec_filter_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature: Optional[torch.Tensor], tokens: torch.Tensor,
+                       top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+                       logprob: Optional[torch.Tensor] = None, n_kept: Optional[torch.Tensor] = None,
+                       logits_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
+    """One draw per row of logits [rows][vocab] (float32 or bfloat16, any row stride); per-row parameters are device
+    tensors, None switches a filter off.  logits_out fp32: the logits, -inf where not kept."""
+    rows, vocab = logits.shape
+    for t in (uniforms, temperature, tokens, top_k, top_p, min_p, logprob, n_kept):
+        _expect(t, (rows,))
+    _expect(logits_out, (rows, vocab))
+    ld = logits.stride(0) if rows > 1 else vocab
+    f = torch.float32
+    args = spec_filter_args(_rows_ptr(logits, vocab), _dtype(logits), rows, vocab, ld, _ptr(uniforms, f), _ptr(temperature, f),
+                            _ptr(top_k, torch.int32), _ptr(top_p, f), _ptr(min_p, f))
+    out = spec_filter_out(_ptr(tokens, torch.int32), _ptr(logprob, f), _ptr(n_kept, torch.int32), _ptr(logits_out, f))
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().spec_filter_sample(C.byref(args), C.byref(out), _ptr(workspace), nbytes, _stream(stream)))
+    return tokens
 
 
 class Lookahead:

@@ -10,7 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecverify.so")
 SOURCES = ["attention.hip", "attention_reuse.hip", "spec_verify.hip", "forward.hip", "sampler.hip", "gemm.hip",
-           "elementwise.hip", "probe.hip", "decode.hip", "lookahead.hip"]
+           "elementwise.hip", "probe.hip", "decode.hip", "lookahead.hip", "q8_rows.hip", "q8_gemm.hip", "kv8.hip",
+           "filter_sample.hip"]
 # packed-fp32 instructions are disabled for all device code.  The first kernel arguments (up to 14 dwords, whole structs
 # excepted) come in scalar registers with the wavefront instead of by a load that every wavefront waits for before its
 # first address: a step is a chain of small launches (1B shape, batch 1, 120 of them: 812 -> 787 us).  Kernels list
@@ -22,7 +23,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-mllvm", "-amdg
 # 32 of them out and back around every block's products (the rare rescaling is vector arithmetic).
 # The GEMM kernels keep the default: several of their variants measured slower with this option.
 SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-                "attention_reuse.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+                "attention_reuse.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+                "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 OBJ_DIR = os.path.join(HERE, "_build")
 
 

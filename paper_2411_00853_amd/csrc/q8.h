@@ -1,0 +1,62 @@
+// What the operators on 8-bit numbers (spec_q8.h) share on the device.
+#pragma once
+
+#include "common.h"
+#include "../../include/spec_q8.h"
+
+namespace specv {
+
+typedef __bf16 q8_bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 q8_bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 q8_halfx8 __attribute__((ext_vector_type(8)));
+typedef _Float16 q8_halfx2 __attribute__((ext_vector_type(2)));
+typedef float q8_floatx2 __attribute__((ext_vector_type(2)));
+typedef float q8_floatx4 __attribute__((ext_vector_type(4)));
+typedef int q8_intx4 __attribute__((ext_vector_type(4)));
+typedef int q8_intx8 __attribute__((ext_vector_type(8)));
+typedef unsigned q8_uintx2 __attribute__((ext_vector_type(2)));
+
+constexpr float Q8_MAX = 448.f;         // largest e4m3 number
+constexpr float Q8_TINY = 0x1p-126f;    // smallest scale
+
+inline int q8_blocks(int cols) { return (cols + SPEC_Q8_BLOCK - 1) / SPEC_Q8_BLOCK; }
+inline bool q8_dtype(int t) { return t == SPEC_DTYPE_FP32 || t == SPEC_DTYPE_BF16; }
+
+// Four fp32 numbers to four e4m3 bytes, to nearest even (|v| <= 448 up to rounding, or NaN)
+__device__ __forceinline__ unsigned q8_pack4(float a, float b, float c, float d)
+{
+    int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+}
+
+__device__ __forceinline__ float q8_unpack(unsigned byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
+
+// Eight consecutive elements from any element-aligned address
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Q8Eight {
+    T v[8];
+};
+
+__device__ __forceinline__ void q8_load8(const float* p, float* v)
+{
+    const Q8Eight<float> x = *reinterpret_cast<const Q8Eight<float>*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = x.v[i];
+}
+
+__device__ __forceinline__ float q8_widen(uint16_t b) { return __uint_as_float((unsigned)b << 16); }
+__device__ __forceinline__ float q8_widen(float f) { return f; }
+
+__device__ __forceinline__ void q8_load8(const uint16_t* p, float* v)
+{
+    const Q8Eight<uint16_t> x = *reinterpret_cast<const Q8Eight<uint16_t>*>(p);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = q8_widen(x.v[i]);
+}
+
+__device__ __forceinline__ uint16_t q8_round_bf16(float f)
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)f);
+}
+
+}  // namespace specv

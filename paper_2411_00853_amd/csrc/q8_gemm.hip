@@ -1,0 +1,226 @@
+// Y = X * W^T on 8-bit numbers, a scale for each block of 128: y[m][n] = sum_kb sx[kb][m] * sw[n/128][kb] * d, with d the
+// product of the two blocks of 128 columns, which is what one 16x16x128 matrix instruction adds up.  The instruction starts
+// from zero at every block, and the block's scales multiply its result on the way into the fp32 sum.
+//
+// The fp8 instruction does not add up in fp32: what it drops lies below 2^-11 of a block's largest product (measured on random tiles;
+// 1.4e-5 of the result on normally distributed rows, 3e-5 with outlier channels, whatever K).  Next to the rounding of a bf16 result
+// (1.7e-3) that is nothing, so those take it; fp32 results take the bf16 instruction at half the rate, into which e4m3 numbers go exactly.
+//
+// W is the instruction's first operand: a lane then holds four neighbouring columns of one row of Y, so that it needs one
+// scale of X, and the scale of W is the same for all lanes.
+#include "q8.h"
+
+namespace specv {
+namespace {
+
+__device__ __forceinline__ q8_floatx4 mfma_fp8(const q8_intx8& a, const q8_intx8& b)
+{
+    const q8_floatx4 zero = {0.f, 0.f, 0.f, 0.f};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, zero, 0, 0, 0, 0, 0, 0);
+}
+
+// The same product with every sum in fp32: e4m3 numbers are bf16 numbers
+struct Wide {
+    q8_bf16x8 v[4];
+};
+
+__device__ __forceinline__ Wide widen(const q8_intx8& a)
+{
+    Wide r;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const q8_bf16x2 x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)a[2 * k], 1.f, false);
+        const q8_bf16x2 y = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)a[2 * k], 1.f, true);
+        const q8_bf16x2 z = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)a[2 * k + 1], 1.f, false);
+        const q8_bf16x2 w = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((unsigned)a[2 * k + 1], 1.f, true);
+        r.v[k] = (q8_bf16x8){x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
+    }
+    return r;
+}
+
+__device__ __forceinline__ q8_floatx4 mfma_wide(const Wide& a, const Wide& b)
+{
+    q8_floatx4 d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v[k], b.v[k], d, 0, 0, 0);
+    return d;
+}
+
+// What a kernel keeps of a loaded operand, and the product of two blocks, by the type of the result
+template <typename T>
+struct Block;
+template <>
+struct Block<uint16_t> {
+    typedef q8_intx8 Op;
+    static __device__ __forceinline__ Op op(const q8_intx8& v) { return v; }
+    static __device__ __forceinline__ q8_floatx4 dot(const Op& a, const Op& b) { return mfma_fp8(a, b); }
+};
+template <>
+struct Block<float> {
+    typedef Wide Op;
+    static __device__ __forceinline__ Op op(const q8_intx8& v) { return widen(v); }
+    static __device__ __forceinline__ q8_floatx4 dot(const Op& a, const Op& b) { return mfma_wide(a, b); }
+};
+
+// The operand of one lane: sixteen bytes of either half of the block of 128
+__device__ __forceinline__ q8_intx8 operand(const uint8_t* lo, const uint8_t* hi)
+{
+    const q8_intx4 a = *reinterpret_cast<const q8_intx4*>(lo), b = *reinterpret_cast<const q8_intx4*>(hi);
+    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+__device__ __forceinline__ void store4(float* y, const q8_floatx4& v, int n, int N, bool whole)
+{
+    if (whole && n + 4 <= N) {
+        *reinterpret_cast<q8_floatx4*>(y + n) = v;
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < N) y[n + i] = v[i];
+}
+
+__device__ __forceinline__ void store4(uint16_t* y, const q8_floatx4& v, int n, int N, bool whole)
+{
+    if (whole && n + 4 <= N) {
+        uint16_t b[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = q8_round_bf16(v[i]);
+        *reinterpret_cast<uint2*>(y + n) = make_uint2(b[0] | (unsigned)b[1] << 16, b[2] | (unsigned)b[3] << 16);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (n + i < N) y[n + i] = q8_round_bf16(v[i]);
+}
+
+constexpr int TILE = 16 * SPEC_Q8_BLOCK;   // bytes of a 16 x 128 tile of W
+
+// A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out the blocks of K and add their sums up in LDS.
+template <int RT, int NT, typename T>
+__global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
+                                                     const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles)
+{
+    __shared__ q8_floatx4 part[8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int j0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * RT);
+    const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
+    q8_floatx4 acc[RT][NT];
+#pragma unroll
+    for (int a = 0; a < RT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) acc[a][b] = (q8_floatx4){0.f, 0.f, 0.f, 0.f};
+    int row[RT];
+#pragma unroll
+    for (int a = 0; a < RT; ++a) row[a] = min(m0 + 16 * a + r16, M - 1);
+    for (int kb = wave; kb < n_blocks; kb += waves) {
+        typename Block<T>::Op wf[NT], xf[RT];
+        float s[RT];
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            const uint8_t* p = w + ((size_t)kb * n_tiles + min(j0 + b, n_tiles - 1)) * TILE + lane * 16;
+            wf[b] = Block<T>::op(operand(p, p + 1024));
+        }
+#pragma unroll
+        for (int a = 0; a < RT; ++a) {
+            const uint8_t* p = x + row[a] * kp + (size_t)kb * SPEC_Q8_BLOCK + 16 * g;
+            xf[a] = Block<T>::op(operand(p, p + 64));
+            s[a] = sx[(size_t)kb * M + row[a]];
+        }
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            const float ws = sw[(size_t)(min(j0 + b, n_tiles - 1) >> 3) * n_blocks + kb];
+#pragma unroll
+            for (int a = 0; a < RT; ++a) {
+                const q8_floatx4 d = Block<T>::dot(wf[b], xf[a]);
+                const float f = s[a] * ws;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[i], f, acc[a][b][i]);
+            }
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < RT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) {
+            if (a + b) __syncthreads();
+            part[wave][lane] = acc[a][b];
+            __syncthreads();
+            if (wave == (a * NT + b) % waves) {   // the wavefronts take turns
+                q8_floatx4 v = part[0][lane];
+                for (int k = 1; k < waves; ++k) v += part[k][lane];
+                const int m = m0 + 16 * a + r16;
+                if (m < M) store4(y + (size_t)m * N, v, (j0 + b) * 16 + 4 * g, N, (N & 3) == 0);
+            }
+        }
+}
+
+template <int RT, int NT, typename T>
+void launch_skinny(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
+{
+    const int n_tiles = (N + 15) / 16;
+    hipLaunchKernelGGL((skinny_kernel<RT, NT, T>), dim3((n_tiles + NT - 1) / NT, (M + 16 * RT - 1) / (16 * RT)), dim3(512), 0, s,
+                       (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks, n_tiles);
+}
+
+template <typename T>
+void launch_gemm(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
+{
+    if (M <= 16) launch_skinny<1, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else launch_skinny<4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+}
+
+// One thread copies sixteen bytes of the packed order
+__global__ void __launch_bounds__(256) pack_kernel(const uint8_t* __restrict__ src, uint8_t* __restrict__ dst, int n_out, int n_in, int n_tiles,
+                                                   size_t total)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= total) return;
+    const int n = i & 15, g = (i >> 4) & 3, h = (i >> 6) & 1;
+    const size_t tile = i >> 7;
+    const int j = (int)(tile % n_tiles), kb = (int)(tile / n_tiles);
+    const int row = 16 * j + n, col = kb * SPEC_Q8_BLOCK + 64 * h + 16 * g;
+    uint8_t b[16];
+    for (int e = 0; e < 16; ++e) b[e] = row < n_out && col + e < n_in ? src[(size_t)row * n_in + col + e] : 0;
+    *reinterpret_cast<q8_intx4*>(dst + i * 16) = *reinterpret_cast<const q8_intx4*>(b);
+}
+
+}  // namespace
+}  // namespace specv
+
+using namespace specv;
+
+extern "C" size_t spec_q8_packed_weight_bytes(int32_t n_out, int32_t n_in)
+{
+    if (n_out <= 0 || n_in <= 0) return 0;
+    return (size_t)((n_out + 15) / 16) * (size_t)q8_blocks(n_in) * TILE;
+}
+
+extern "C" int spec_q8_pack_weight(const void* src, void* dst_packed, int32_t n_out, int32_t n_in, void* stream)
+{
+    if (!src || !dst_packed) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_pack_weight: null pointer");
+    if (n_out <= 0 || n_in <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_pack_weight: %d x %d", n_out, n_in);
+    if ((uintptr_t)dst_packed & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_pack_weight: dst_packed is not 16-byte aligned");
+    const size_t total = spec_q8_packed_weight_bytes(n_out, n_in) / 16;
+    if (total > ((size_t)1 << 38)) return fail(SPEC_ERR_SHAPE, "spec_q8_pack_weight: %d x %d is too large", n_out, n_in);
+    hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, (hipStream_t)stream, (const uint8_t*)src,
+                       (uint8_t*)dst_packed, n_out, n_in, (n_out + 15) / 16, total);
+    SPECV_LAUNCH_CHECK("pack_kernel");
+    return SPEC_OK;
+}
+
+extern "C" int spec_q8_gemm(const void* q, const float* scales, const void* w_packed, const float* w_scales, void* y, int32_t y_dtype,
+                            int32_t M, int32_t N, int32_t K, void* stream)
+{
+    if (M < 0 || N <= 0 || K <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: M = %d, N = %d, K = %d", M, N, K);
+    if (!q8_dtype(y_dtype)) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: unknown type %d", y_dtype);
+    if (!M) return SPEC_OK;
+    if (!q || !scales || !w_packed || !w_scales || !y) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: null pointer");
+    if (((uintptr_t)q | (uintptr_t)w_packed | (uintptr_t)y) & 15)
+        return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: q, w_packed and y have to be 16-byte aligned");
+    if (M > 65535 * 16) return fail(SPEC_ERR_SHAPE, "spec_q8_gemm: %d rows, at most %d", M, 65535 * 16);
+    if (y_dtype == SPEC_DTYPE_BF16) launch_gemm<uint16_t>(q, w_packed, scales, w_scales, y, M, N, q8_blocks(K), (hipStream_t)stream);
+    else launch_gemm<float>(q, w_packed, scales, w_scales, y, M, N, q8_blocks(K), (hipStream_t)stream);
+    SPECV_LAUNCH_CHECK("spec_q8_gemm");
+    return SPEC_OK;
+}

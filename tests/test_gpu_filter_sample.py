@@ -1,0 +1,181 @@
+"""Filtered draws against the definition in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import q8_ref as ref
+from paper_2411_00853_amd import binding as sv
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def draw(x, u, t=None, k=None, p=None, mp=None, out=True, workspace=True):
+    rows, vocab = x.shape
+    i32 = lambda: torch.full((rows,), -9, dtype=torch.int32, device="cuda")  # noqa: E731
+    tokens, kept, lp = i32(), i32(), torch.full((rows,), 9.0, device="cuda")
+    lo = torch.full((rows, vocab), 5.0, device="cuda") if out else None
+    ws = None
+    if workspace and (nb := sv.spec_filter_workspace_bytes(rows, vocab)):
+        ws = torch.full((nb // 4,), -1, dtype=torch.int32, device="cuda")      # whatever it holds
+    sv.spec_filter_sample(x, u, t, tokens, k, p, mp, lp, kept, lo, ws)
+    return tokens, kept, lp, lo
+
+
+def check(x, u, t=None, k=None, p=None, mp=None, out=True, workspace=True):
+    tokens, kept, lp, lo = draw(x, u, t, k, p, mp, out, workspace)
+    val = lambda v, r, none: none if v is None else v[r].item()  # noqa: E731
+    for r in range(x.shape[0]):
+        ref.check_draw(x[r], u[r].item(), val(t, r, 1.0), val(k, r, 0), val(p, r, 1.0), val(mp, r, 0.0), int(tokens[r]), int(kept[r]),
+                       float(lp[r]), lo[r] if out else None)
+    return tokens, kept, lp, lo
+
+
+def inputs(seed, rows, vocab, dtype="fp32", std=2.5):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn((rows, vocab), generator=g, device="cuda") * std).to(DTYPES[dtype])
+    return x, torch.rand(rows, generator=g, device="cuda").clamp_max(1 - 2.0 ** -24), g
+
+
+def params(g, rows, on):
+    f = lambda lo, hi: torch.rand(rows, generator=g, device="cuda") * (hi - lo) + lo  # noqa: E731
+    return (f(0.5, 1.4), torch.randint(1, 300, (rows,), generator=g, device="cuda", dtype=torch.int32) if "k" in on else None,
+            f(0.3, 0.99) if "p" in on else None, f(0.001, 0.2) if "m" in on else None)
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("on", ["", "k", "p", "m", "kp", "km", "pm", "kpm"])
+@pytest.mark.parametrize("vocab", [1000, 32003, 128256])
+def test_filters(vocab, on, dtype, workspace):
+    x, u, g = inputs(len(on) + vocab, 6, vocab, dtype)
+    t, k, p, mp = params(g, 6, on)
+    check(x, u, t, k, p, mp, True, workspace)
+    check(x, u, t, k, p, mp, False, workspace)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3, 63, 64, 65, 127, 1023, 1024, 1025, 4097, 16385, 65537, 262144])
+def test_vocabularies(vocab):
+    x, u, g = inputs(vocab, 3, vocab)
+    for on in ("", "kpm"):
+        check(x, u, *params(g, 3, on))
+
+
+def test_many_rows_at_any_distance():
+    x, u, g = inputs(3, 150, 2005)
+    view = x[:, 3:1903]
+    check(view, u, *params(g, 150, "kpm"))
+    check(view, u, None)
+
+
+@pytest.mark.parametrize("vocab", [5000, 70000])
+def test_equal_logits(vocab):
+    """All equal, a few values, and rows of bf16 steps: the lowest ids go first."""
+    u = torch.tensor([0.0, 0.3, 0.999], device="cuda")
+    k = torch.tensor([1, 777, 4999], dtype=torch.int32, device="cuda")
+    x = torch.zeros((3, vocab), device="cuda")
+    tokens, kept, lp, lo = check(x, u, None, k)
+    assert kept.tolist() == k.tolist() and tokens.tolist() == [0, int(0.3 * 777), int(0.999 * 4999)]
+    assert all(bool((lo[r, : int(k[r])] == 0).all()) for r in range(3))
+    p = torch.tensor([0.1, 0.5, 0.99], device="cuda")
+    check(x, u, None, None, p)
+    check(x, u, None, k, p)
+    x = torch.randint(0, 3, (3, vocab), device="cuda").float()
+    for args in ((None, k), (None, None, p), (None, k, p), (None,)):
+        check(x, u, *args)
+    x = (torch.randn((3, vocab), device="cuda") * 0.05).to(torch.bfloat16)
+    for args in ((None, k), (None, None, p), (None, k, p)):
+        check(x, u, *args)
+    x = torch.full((3, vocab), -3.0e38, device="cuda")
+    check(x, u, None, k)
+
+
+def test_flat_and_peaked_rows():
+    x, u, g = inputs(9, 4, 50000, std=0.01)
+    t, k, p, mp = params(g, 4, "kpm")
+    check(x, u, t, None, p)
+    check(x, u, t, k + 20000, p)
+    x[:, 77] = 90.0
+    tokens, kept, _, _ = check(x, u, None, None, p)
+    assert tokens.tolist() == [77] * 4 and kept.tolist() == [1] * 4
+
+
+def test_excluded_and_extreme_logits():
+    x, u, g = inputs(10, 5, 3001)
+    x[0, torch.arange(3001) != 17] = -math.inf
+    x[1, ::2] = -math.inf
+    x[2, 5:] = torch.finfo(torch.float32).min
+    x[3] = torch.finfo(torch.float32).min
+    x[4, 1::3] = -0.0
+    x[4, ::3] = 0.0
+    for on in ("", "k", "kpm"):
+        tokens, kept, _, _ = check(x, u, *params(g, 5, on))
+        assert int(tokens[0]) == 17 and int(kept[0]) == 1 and int(tokens[1]) % 2 == 1 and int(tokens[2]) < 5
+
+
+def test_rows_without_a_distribution():
+    x, u, g = inputs(11, 4, 2000)
+    x[0, 5], x[1, 1999], x[2] = math.nan, math.inf, -math.inf
+    for on in ("", "kpm"):
+        tokens, kept, lp, lo = draw(x, u, *params(g, 4, on))
+        assert tokens[:3].tolist() == [-1] * 3 and kept[:3].tolist() == [0] * 3 and bool(lp[:3].isnan().all())
+        assert torch.all(lo[:3] == -math.inf) and int(tokens[3]) >= 0
+
+
+def test_parameters_that_switch_off_or_keep_one():
+    x, u, g = inputs(12, 4, 3000)
+    z = lambda *v: torch.tensor(v, device="cuda")  # noqa: E731
+    check(x, u, None, torch.tensor([0, -5, 3000, 1 << 30], dtype=torch.int32, device="cuda"), z(1.0, 2.0, 1.5, math.inf), z(0.0, -1.0, 0.0, -0.5))
+    best = x.argmax(1).int()
+    for args in ((z(0.0, 0.0, -1.0, 0.0),), (None, torch.ones(4, dtype=torch.int32, device="cuda")), (None, None, z(0.0, 0.0, 1e-9, 1e-30)),
+                 (None, None, None, z(1.0, 1.0, 1.0, 5.0))):
+        tokens, kept, lp, _ = draw(x, u, *args)
+        assert torch.equal(tokens, best) and kept.tolist() == [1] * 4 and torch.all(lp == 0)
+    tied = x.clone()
+    tied[:, 900] = tied[:, 333] = 50.0
+    assert draw(tied, u, z(0.0, 0.0, 0.0, 0.0))[0].tolist() == [333] * 4
+    check(x, z(0.0, 1 - 2.0 ** -24, 0.5, 2.0 ** -24), z(1e-3, 0.05, 50.0, 1e6))
+
+
+def test_the_same_call_gives_the_same_bits_and_a_graph_too():
+    x, u, g = inputs(13, 8, 128256)
+    t, k, p, mp = params(g, 8, "kpm")
+    for args in ((t, k, p, mp), (t, None, p, None), (t, None, None, None)):
+        first = draw(x, u, *args)
+        for _ in range(3):
+            again = draw(x, u, *args)
+            assert all(torch.equal(a, b) for a, b in zip(first, again))
+    tokens, kept = (torch.empty(8, dtype=torch.int32, device="cuda") for _ in range(2))
+    ws = torch.empty(max(1, sv.spec_filter_workspace_bytes(8, 128256) // 4), device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sv.spec_filter_sample(x, u, t, tokens, None, p, mp, None, kept, None, ws)
+    for r in range(4):
+        x.add_(0.1 * torch.randn(x.shape, generator=g, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = draw(x, u, t, None, p, mp)
+        assert torch.equal(tokens, want[0]) and torch.equal(kept, want[1])
+
+
+def test_a_filtered_row_is_what_the_verify_step_takes():
+    """Target rows filtered here, proposals drawn from rows filtered here: whatever the step emits is a kept token."""
+    B, K, V = 4, 3, 5000
+    x, u, g = inputs(14, B * (K + 1), V)
+    _, _, _, target = draw(x, u, None, torch.full((B * (K + 1),), 50, dtype=torch.int32, device="cuda"))
+    y, v, _ = inputs(15, B * K, V)
+    toks, _, _, q = draw(0.5 * x.view(B, K + 1, V)[:, :K].reshape(B * K, V) + 0.5 * y, v, None, torch.full((B * K,), 50, dtype=torch.int32, device="cuda"))
+    na = torch.empty(B, dtype=torch.int32, device="cuda")
+    ot = torch.empty((B, K + 1), dtype=torch.int32, device="cuda")
+    h = sv.spec_verify_init(sv.sampler_cfg(V, B, K), None, None, None)
+    sv.spec_verify_step(h, [K] * B, torch.rand((B, K + 1), generator=g, device="cuda"), 1.0, na, ot, draft_tokens=toks.view(B, K).contiguous(),
+                        draft_logits=q.view(B, K, V), target_logits_in=target)
+    torch.cuda.synchronize()
+    for b in range(B):
+        a = int(na[b])
+        assert 0 <= a <= K
+        for i in range(a + 1):
+            assert float(target.view(B, K + 1, V)[b, i, int(ot[b, i])]) > -math.inf
+    h.close()
