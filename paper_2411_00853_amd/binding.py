@@ -453,9 +453,10 @@ _DTYPES = {torch.float32: SPEC_DTYPE_FP32, torch.bfloat16: SPEC_DTYPE_BF16}
 
 
 def _dtype(t: torch.Tensor) -> int:
-    if t.dtype not in _DTYPES:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    return _DTYPES[t.dtype]
+    return code
 
 
 def _rows_ptr(t: torch.Tensor, cols: int) -> int:
@@ -466,9 +467,16 @@ def _rows_ptr(t: torch.Tensor, cols: int) -> int:
 
 
 def _expect(t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
-    if t is not None and tuple(t.shape) != tuple(shape):
+    if t is not None and t.shape != shape:
         raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
     return t
+
+
+def _raw_stream(stream) -> Optional[int]:
+    """What _stream gives, without a Stream object for the current stream: these calls take a few microseconds in all."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+    return stream.cuda_stream or None
 
 
 def _q8_out(rows: int, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor], device):
@@ -486,7 +494,7 @@ def spec_q8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scales: 
     q, scales = _q8_out(rows, cols, q, scales, x.device)
     ld = x.stride(0) if rows > 1 else cols
     _check(lib().spec_q8_quantize(_rows_ptr(x, cols), _dtype(x), ld, rows, cols, _ptr(q, _F8),
-                                  _ptr(scales, torch.float32), _stream(stream)))
+                                  _ptr(scales, torch.float32), _raw_stream(stream)))
     return q, scales
 
 
@@ -499,7 +507,7 @@ def spec_q8_add_rmsnorm(x: torch.Tensor, delta: Optional[torch.Tensor], gain: to
     _check(lib().spec_q8_add_rmsnorm(_ptr(x), _dtype(x), _ptr(_expect(delta, x.shape)), 0 if delta is None else _dtype(delta),
                                      _ptr(_expect(gain, (cols,)), torch.float32), float(eps), rows, cols,
                                      _ptr(_expect(x_out, x.shape), x.dtype), _ptr(q, _F8), _ptr(scales, torch.float32),
-                                     _stream(stream)))
+                                     _raw_stream(stream)))
     return q, scales
 
 
@@ -510,7 +518,7 @@ def spec_q8_swiglu(gate_up: torch.Tensor, q: Optional[torch.Tensor] = None, scal
         raise ValueError("gate_up needs as many up columns as gate columns")
     q, scales = _q8_out(rows, cols // 2, q, scales, gate_up.device)
     _check(lib().spec_q8_swiglu(_ptr(gate_up), _dtype(gate_up), rows, cols // 2, _ptr(q, _F8), _ptr(scales, torch.float32),
-                                _stream(stream)))
+                                _raw_stream(stream)))
     return q, scales
 
 
@@ -522,7 +530,7 @@ def spec_q8_pack_weight(src: torch.Tensor, stream=None) -> torch.Tensor:
     """Row-major e4m3 [n_out][n_in] -> new device buffer in the tile order of spec_q8_gemm."""
     n_out, n_in = src.shape
     dst = torch.empty(spec_q8_packed_weight_bytes(n_out, n_in), dtype=_F8, device=src.device)
-    _check(lib().spec_q8_pack_weight(_ptr(src, _F8), _ptr(dst), n_out, n_in, _stream(stream)))
+    _check(lib().spec_q8_pack_weight(_ptr(src, _F8), _ptr(dst), n_out, n_in, _raw_stream(stream)))
     return dst
 
 
@@ -535,7 +543,7 @@ def spec_q8_gemm(q: torch.Tensor, scales: torch.Tensor, w_packed: torch.Tensor, 
     if w_packed.numel() != (N + 15) // 16 * 16 * kp or kp % 128:
         raise ValueError(f"expected a packed matrix of {N} x {kp}")
     _check(lib().spec_q8_gemm(_ptr(q, _F8), _ptr(scales, torch.float32), _ptr(w_packed, _F8), _ptr(w_scales, torch.float32), _ptr(y),
-                              _dtype(y), M, N, kp, _stream(stream)))
+                              _dtype(y), M, N, kp, _raw_stream(stream)))
     return y
 
 
@@ -563,7 +571,7 @@ def spec_kv8_append(cache: Kv8Cache, qkv: torch.Tensor, row0: torch.Tensor, kv_l
         max_pos = cos_sin.shape[0]
         _expect(cos_sin, (max_pos, c.head_dim // 2, 2))
     _check(lib().spec_kv8_append(C.byref(c), _ptr(qkv, torch.bfloat16), n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
-                                 rows, max_window, _ptr(cos_sin, torch.float32), max_pos, _ptr(q_out, torch.bfloat16), _stream(stream)))
+                                 rows, max_window, _ptr(cos_sin, torch.float32), max_pos, _ptr(q_out, torch.bfloat16), _raw_stream(stream)))
 
 
 def spec_kv8_workspace_bytes(rows: int, n_q_heads: int, head_dim: int) -> int:
@@ -582,7 +590,7 @@ def spec_kv8_attention(cache: Kv8Cache, q: torch.Tensor, row0: torch.Tensor, kv_
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().spec_kv8_attention(C.byref(c), _rows_ptr(q, cols), ld, n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
                                     rows, max_window, max_len, scale, _ptr(out, torch.bfloat16), _ptr(workspace), nbytes,
-                                    _stream(stream)))
+                                    _raw_stream(stream)))
     return out
 
 
@@ -606,7 +614,7 @@ def spec_filter_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature
                             _ptr(top_k, torch.int32), _ptr(top_p, f), _ptr(min_p, f))
     out = spec_filter_out(_ptr(tokens, torch.int32), _ptr(logprob, f), _ptr(n_kept, torch.int32), _ptr(logits_out, f))
     nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().spec_filter_sample(C.byref(args), C.byref(out), _ptr(workspace), nbytes, _stream(stream)))
+    _check(lib().spec_filter_sample(C.byref(args), C.byref(out), _ptr(workspace), nbytes, _raw_stream(stream)))
     return tokens
 
 

@@ -10,143 +10,489 @@ namespace {
 typedef unsigned long long u64;
 
 constexpr int TPB = 1024, WAVES = TPB / 64;
-constexpr float MASS_ONE = 0x1p44f;
+constexpr int BINS = 4096;      // of falling logits, over the 31 nats in which a token has mass
+constexpr int LIST = 2048;      // tokens that may matter, where that few are known to
+constexpr int SMALL = 1024;     // tokens of the bin that a cut falls into
+constexpr float NATS = 31.f;    // exp(-31) * 2^44 < 1
+constexpr float HALF_ONE = 0x1p22f;
+constexpr u64 MASS_ONE = 1ull << 44;
 
+// ---- a wavefront's sums by DPP ------------------------------------------------------------------------------------------
+enum { DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e, DPP_SHR1 = 0x111, DPP_SHR2 = 0x112, DPP_SHR4 = 0x114, DPP_SHR8 = 0x118, DPP_MIRROR = 0x140,
+       DPP_HALF_MIRROR = 0x141, DPP_BCAST15 = 0x142, DPP_BCAST31 = 0x143 };
+template <int CTRL, int ROWS>
+__device__ __forceinline__ unsigned dpp(unsigned v)   // lanes without a source get 0
+{
+    return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 dpp(u64 v)
+{
+    return (u64)dpp<CTRL, ROWS>((unsigned)(v >> 32)) << 32 | dpp<CTRL, ROWS>((unsigned)v);
+}
+template <typename T>
+__device__ __forceinline__ T wave_scan(T v)   // inclusive
+{
+    v += dpp<DPP_SHR1, 0xf>(v);
+    v += dpp<DPP_SHR2, 0xf>(v);
+    v += dpp<DPP_SHR4, 0xf>(v);
+    v += dpp<DPP_SHR8, 0xf>(v);
+    v += dpp<DPP_BCAST15, 0xa>(v);
+    v += dpp<DPP_BCAST31, 0xc>(v);
+    return v;
+}
+__device__ __forceinline__ unsigned last_lane(unsigned v) { return (unsigned)__builtin_amdgcn_readlane((int)v, 63); }
+__device__ __forceinline__ u64 last_lane(u64 v) { return (u64)last_lane((unsigned)(v >> 32)) << 32 | last_lane((unsigned)v); }
+template <typename T>
+__device__ __forceinline__ T wave_sum(T v)   // the same for all lanes
+{
+    return last_lane(wave_scan(v));
+}
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+    v = max(v, dpp<DPP_XOR1, 0xf>(v));
+    v = max(v, dpp<DPP_XOR2, 0xf>(v));
+    v = max(v, dpp<DPP_HALF_MIRROR, 0xf>(v));
+    v = max(v, dpp<DPP_MIRROR, 0xf>(v));
+    v = max(v, dpp<DPP_BCAST15, 0xa>(v));
+    v = max(v, dpp<DPP_BCAST31, 0xc>(v));
+    return last_lane(v);
+}
+
+// ---- what a workgroup knows of its row ----------------------------------------------------------------------------------
 // Ascending with the logit; -0 and 0 are one value
 __device__ __forceinline__ unsigned key_of(float x)
 {
     const unsigned u = __float_as_uint(x + 0.f);
     return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
+__device__ __forceinline__ float logit_of(unsigned key) { return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu)); }
+
+struct Cut {        // tokens of a larger key are in, those of this key up to id
+    unsigned key;
+    int id;
+    __device__ __forceinline__ bool has(float l, int i) const
+    {
+        const unsigned k = key_of(l);
+        return k > key || (k == key && i <= id);
+    }
+};
 
 struct Sums {
-    u64 a, b;
+    u64 n, mass;
 };
 
-__device__ __forceinline__ Sums block_sums(u64 a, u64 b, Sums* lds)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        a += __shfl_xor(a, d);
-        b += __shfl_xor(b, d);
-    }
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = {a, b};
-    __syncthreads();
-    Sums s = lds[0];
-    for (int w = 1; w < WAVES; ++w) {
-        s.a += lds[w].a;
-        s.b += lds[w].b;
-    }
-    return s;
-}
-
-struct Cut {
-    unsigned key;   // tokens above it are in, those at it up to id
-    int id;
+struct Lds {
+    u64 hist[BINS];
+    float lx[LIST];
+    int lid[LIST];
+    float sx[SMALL];
+    int sid[SMALL];
+    u64 sv[SMALL];
+    Sums wave[WAVES];
+    unsigned tops[WAVES];
+    int n_list, n_small, bin;
+    unsigned least_key;
+    u64 above;
+    Cut cut;
 };
 
-// A row of logits, read again by every pass
+// Masses of a row.  (l - top) / t is the rounded quotient: r is the rounded 1 / t, and one step of correction behind the product
+// with it gives what a division does, at a third of the instructions.
+struct Masses {
+    float top, t, r, per_nat;   // per_nat: bins of one unit of logit
+    __device__ __forceinline__ u64 operator()(float l) const
+    {
+        const float d = l - top, q = d * r;
+        if (!(q >= -NATS - 1.f)) return 0;   // also -inf
+        const float e = expf(fmaf(fmaf(-q, t, d), r, q)) * HALF_ONE;
+        return (u64)(unsigned)e << 22 | (unsigned)(__builtin_amdgcn_fractf(e) * HALF_ONE);
+    }
+    __device__ __forceinline__ int bin(float l) const { return (int)fminf((top - l) * per_nat, (float)(BINS - 1)); }
+};
+
+// ---- where tokens come from: registers, memory or the list in LDS ----------------------------------------------------------
 template <typename T>
+struct Vec;   // elements of a lane's load
+template <>
+struct Vec<float> {
+    static constexpr int N = 4;
+};
+template <>
+struct Vec<uint16_t> {
+    static constexpr int N = 8;
+};
+template <typename T>
+struct __attribute__((packed, aligned(sizeof(T)))) Some {
+    T v[Vec<T>::N];
+};
+
+// A wavefront's load covers CHUNK consecutive ids; chunk c is wavefront c % WAVES's.  NV loads of a thread stay in registers, with NV = 0
+// every pass reads the row again.
+template <typename T, int NV>
 struct Row {
+    static constexpr int N = Vec<T>::N, CHUNK = 64 * N;
     const T* x;
     int vocab;
-    float top, t;
-    bool greedy;
-    u64 least;   // smallest mass kept (min-p), at least 1
+    float v[NV ? NV : 1][N];
 
-    __device__ __forceinline__ float logit(int i) const { return q8_widen(x[i]); }
-    __device__ __forceinline__ u64 mass(float l) const
+    __device__ __forceinline__ void fetch(int k, float* to) const
     {
-        if (greedy) return l == top ? (u64)MASS_ONE : 0;
-        return l > -INFINITY ? (u64)(expf((l - top) / t) * MASS_ONE) : 0;
-    }
-    __device__ __forceinline__ static bool in(const Cut& c, unsigned key, int i) { return key > c.key || (key == c.key && i <= c.id); }
-    // number and mass of the tokens within `c`, of key `from` or more, at least `w_min` heavy, with an id of at most `last`
-    __device__ Sums sums(const Cut& c, unsigned from, u64 w_min, int last, Sums* lds) const
-    {
-        u64 n = 0, m = 0;
-        for (int i = threadIdx.x; i <= last; i += TPB) {
-            const float l = logit(i);
-            const unsigned k = key_of(l);
-            if (k < from || !in(c, k, i)) continue;
-            const u64 w = mass(l);
-            if (w < w_min) continue;
-            ++n;
-            m += w;
+        const int i = (k * TPB + (int)threadIdx.x) * N;
+        if (i + N <= vocab) {
+            const Some<T> s = *reinterpret_cast<const Some<T>*>(x + i);
+#pragma unroll
+            for (int e = 0; e < N; ++e) to[e] = q8_widen(s.v[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) to[e] = i + e < vocab ? q8_widen(x[i + e]) : -INFINITY;
         }
-        return block_sums(n, m, lds);
+    }
+    __device__ __forceinline__ void load()
+    {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) fetch(k, v[k]);
+    }
+    // f(chunk, id of the first, N logits): whole wavefronts
+    template <typename F>
+    __device__ __forceinline__ void each_vec(F f) const
+    {
+        const int wave = threadIdx.x >> 6;
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                f(k * WAVES + wave, (k * TPB + (int)threadIdx.x) * N, v[k]);
+                __builtin_amdgcn_sched_barrier(0);   // one load's masses at a time: side by side they do not fit the registers
+            }
+        } else {
+            constexpr int AHEAD = 16 / N;
+            const int n = (vocab + TPB * N - 1) / (TPB * N);
+            for (int k = 0; k < n; k += AHEAD) {
+                float l[AHEAD][N];
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) fetch(k + j, l[j]);
+#pragma unroll
+                for (int j = 0; j < AHEAD; ++j) f((k + j) * WAVES + wave, ((k + j) * TPB + (int)threadIdx.x) * N, l[j]);
+            }
+        }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const   // f(logit, id); ids beyond the vocabulary come with -inf
+    {
+        each_vec([&](int, int i, const float* l) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) f(l[e], i + e);
+        });
     }
 };
 
-// The shortest prefix of the order that holds `need` tokens (by_mass: that mass), within cut `c`: its last token.
-// The caller knows that c holds as much.
-template <typename T>
-__device__ Cut shortest(const Row<T>& r, Cut c, u64 need, bool by_mass, Sums* lds)
+struct List {
+    const Lds* s;
+    int n;
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        for (int i = threadIdx.x; i < n; i += TPB) f(s->lx[i], s->lid[i]);
+    }
+};
+
+// ---- steps of the whole workgroup -------------------------------------------------------------------------------------------
+__device__ __forceinline__ Sums block_sums(u64 n, u64 mass, Lds& s)
 {
+    n = wave_sum(n);
+    mass = wave_sum(mass);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = {n, mass};
+    __syncthreads();
+    Sums r = s.wave[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) {
+        r.n += s.wave[w].n;
+        r.mass += s.wave[w].mass;
+    }
+    return r;
+}
+
+// The entry of hist[0 .. n) (n a multiple of TPB) in which the running sum reaches `need`, and the sum before it, to s.bin and s.above
+__device__ __forceinline__ void crossing(Lds& s, int n, u64 need)
+{
+    const int per = n / TPB, i0 = threadIdx.x * per, wave = threadIdx.x >> 6;
+    u64 mine = 0;
+    for (int i = 0; i < per; ++i) mine += s.hist[i0 + i];
+    const u64 upto = wave_scan(mine);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) s.wave[wave].n = upto;
+    __syncthreads();
+    u64 before = upto - mine;
+    for (int w = 0; w < wave; ++w) before += s.wave[w].n;
+    if (before < need && before + mine >= need) {
+        int i = i0;
+        for (; before + s.hist[i] < need; ++i) before += s.hist[i];
+        s.bin = i;
+        s.above = before;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void clear(Lds& s, int n)
+{
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += TPB) s.hist[i] = 0;
+    if (threadIdx.x == 0) s.n_small = 0;
+    __syncthreads();
+}
+
+// The shortest prefix that holds `need` (tokens, or mass), by bisection: for a bin of more tokens than SMALL, as many equal logits make
+template <typename S>
+__device__ Cut bisect(const S& src, const Masses& m, const Cut c, u64 need, bool by_mass, int vocab, Lds& s)
+{
+    auto value = [&](float l) {
+        const u64 w = m(l);
+        return by_mass ? w : (u64)(w > 0);
+    };
+    auto from = [&](unsigned key) {
+        u64 v = 0;
+        src.each([&](float l, int i) {
+            if (key_of(l) >= key && c.has(l, i)) v += value(l);
+        });
+        return block_sums(v, 0, s).n;
+    };
     unsigned lo = c.key, hi = 0xffffffffu;   // lo holds enough; hi + 1 does not
     while (lo < hi) {
         const unsigned mid = lo + (hi - lo) / 2 + 1;
-        const Sums s = r.sums(c, mid, 1, r.vocab - 1, lds);
-        if ((by_mass ? s.b : s.a) >= need) lo = mid;
+        if (from(mid) >= need) lo = mid;
         else hi = mid - 1;
     }
-    const unsigned key = lo;
-    u64 above = 0;
-    if (key != 0xffffffffu) {
-        const Sums s = r.sums(c, key + 1, 1, r.vocab - 1, lds);
-        above = by_mass ? s.b : s.a;
-    }
-    int first = 0, last = key == c.key ? c.id : r.vocab - 1;   // the id of the last of the equal ones that is needed
+    const u64 above = lo == 0xffffffffu ? 0 : from(lo + 1);
+    int first = 0, last = lo == c.key ? c.id : vocab - 1;   // the id of the last of the equal ones that is needed
     while (first < last) {
         const int mid = first + (last - first) / 2;
-        u64 n = 0, m = 0;
-        for (int i = threadIdx.x; i <= mid; i += TPB) {
-            const float l = r.logit(i);
-            if (key_of(l) != key) continue;
-            const u64 w = r.mass(l);
-            n += w > 0;
-            m += w;
-        }
-        const Sums s = block_sums(n, m, lds);
-        if (above + (by_mass ? s.b : s.a) >= need) last = mid;
+        u64 v = 0;
+        src.each([&](float l, int i) {
+            if (i <= mid && key_of(l) == lo) v += value(l);
+        });
+        if (above + block_sums(v, 0, s).n >= need) last = mid;
         else first = mid + 1;
     }
-    return {key, last};
+    return {lo, last};
 }
 
+// The same for a source that holds all tokens of logit `lowest` and more, where the prefix lies: a histogram of falling logits, and the
+// tokens of the bin that it ends in, each against each.  c holds as much as needed and becomes the cut; false: the bin is too full.
+template <typename S>
+__device__ bool shortest(const S& src, const Masses& m, Cut& c, u64 need, bool by_mass, float lowest, Lds& s)
+{
+    clear(s, BINS);
+    src.each([&](float l, int i) {
+        if (l < lowest || !c.has(l, i)) return;
+        const u64 w = m(l);
+        if (w) atomicAdd(&s.hist[m.bin(l)], by_mass ? w : 1);
+    });
+    __syncthreads();
+    crossing(s, BINS, need);
+    const int bin = s.bin;
+    const u64 above = s.above;
+    src.each([&](float l, int i) {
+        if (l < lowest || m.bin(l) != bin || !c.has(l, i)) return;
+        const u64 w = m(l);
+        if (!w) return;
+        const int at = atomicAdd(&s.n_small, 1);
+        if (at >= SMALL) return;
+        s.sx[at] = l;
+        s.sid[at] = i;
+        s.sv[at] = by_mass ? w : 1;
+    });
+    __syncthreads();
+    const int n = s.n_small;
+    if (n > SMALL) return false;
+    if ((int)threadIdx.x < n) {
+        const Cut me = {key_of(s.sx[threadIdx.x]), s.sid[threadIdx.x]};
+        const u64 v = s.sv[threadIdx.x];
+        u64 upto = above;
+        for (int j = 0; j < n; ++j)
+            if (me.has(s.sx[j], s.sid[j])) upto += s.sv[j];
+        if (upto >= need && upto - v < need) s.cut = me;
+    }
+    __syncthreads();
+    c = s.cut;
+    return true;
+}
+
+struct Params {
+    int k;
+    float p;
+    u64 least;   // smallest mass kept
+};
+
+struct Results {
+    int32_t* token;
+    float* logprob;
+    int32_t* n_kept;
+    float* out;
+};
+
+template <typename S>
+__device__ __forceinline__ Sums within(const S& src, const Masses& m, const Cut& c, Lds& s)
+{
+    u64 n = 0, mass = 0;
+    src.each([&](float l, int i) {
+        if (!c.has(l, i)) return;
+        const u64 w = m(l);
+        n += w > 0;
+        mass += w;
+    });
+    return block_sums(n, mass, s);
+}
+
+__device__ __forceinline__ u64 share(float p, u64 mass) { return max((u64)ceil((double)fmaxf(p, 0.f) * (double)mass), (u64)1); }
+
+// Top-k (if it cuts) and top-p within a source
+template <typename S>
+__device__ bool cuts(const S& src, const Masses& m, const Params& a, Cut& c, int vocab, Lds& s)
+{
+    if (a.k <= 0 && !(a.p < 1.f)) return true;
+    Sums all = within(src, m, c, s);
+    if (a.k > 0 && (u64)a.k < all.n) {
+        if (!shortest(src, m, c, (u64)a.k, false, -INFINITY, s)) return false;
+        if (a.p < 1.f) all = within(src, m, c, s);
+    }
+    if (a.p < 1.f) {
+        // what lies `reach` and more below the top weighs less than the share that is cut off, in all
+        const float reach = logf((float)vocab * (float)MASS_ONE / ((1.f - fmaxf(a.p, 0.f)) * (float)all.mass)) + 0.05f;
+        return shortest(src, m, c, share(a.p, all.mass), true, m.top - fmaxf(reach, 0.05f) * m.t, s);
+    }
+    return true;
+}
+
+// The draw among the tokens of a cut, and the results.  `list` holds all of them, or is NULL.
+template <typename T, int NV>
+__device__ __forceinline__ void finish(const Row<T, NV>& r, const List* list, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
+                                       Lds& s)
+{
+    constexpr int N = Row<T, NV>::N, CHUNK = Row<T, NV>::CHUNK;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    clear(s, 1024);   // the kept masses by chunk of ids
+    u64 n = 0;
+    if (list) {
+        list->each([&](float l, int i) {
+            if (!c.has(l, i)) return;
+            const u64 w = m(l);
+            if (w < a.least) return;
+            ++n;
+            atomicAdd(&s.hist[i / CHUNK], w);
+        });
+    } else {
+        r.each_vec([&](int chunk, int i0, const float* l) {
+            unsigned hi = 0, lo = 0;   // of 512 masses at most: no carry out of either half
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const u64 w = m(l[e]);
+                if (w < a.least || !c.has(l[e], i0 + e)) continue;
+                ++n;
+                hi += (unsigned)(w >> 22);
+                lo += (unsigned)w & 0x3fffffu;
+            }
+            hi = wave_sum(hi);
+            lo = wave_sum(lo);
+            if (lane == 0 && chunk < 1024) s.hist[chunk] = ((u64)hi << 22) + lo;
+        });
+    }
+    __syncthreads();
+    const Sums kept = block_sums(n, s.hist[threadIdx.x], s);
+    const u64 target = min((u64)((double)u * (double)kept.mass), kept.mass - 1);
+    crossing(s, 1024, target + 1);
+    if (wave == 0) {
+        u64 w[N], sum = 0;
+        const int i0 = s.bin * CHUNK + lane * N;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = i0 + e < r.vocab ? q8_widen(r.x[i0 + e]) : -INFINITY;
+            w[e] = m(l);
+            if (w[e] < a.least || !c.has(l, i0 + e)) w[e] = 0;
+            sum += w[e];
+        }
+        const u64 before = s.above + wave_scan(sum) - sum;
+        if (before <= target && before + sum > target) {
+            int at = 0;   // the first whose running sum exceeds the target
+            u64 drawn = 0, upto = before;
+            bool done = false;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                upto += w[e];
+                if (!done && upto > target) {
+                    at = e;
+                    drawn = w[e];
+                    done = true;
+                }
+            }
+            *o.token = i0 + at;
+            if (o.logprob) *o.logprob = (float)log((double)drawn / (double)kept.mass);
+            if (o.n_kept) *o.n_kept = (int)kept.n;
+        }
+    }
+    if (o.out)
+        r.each([&](float l, int i) {
+            if (i < r.vocab) o.out[i] = c.has(l, i) && m(l) >= a.least ? l : -INFINITY;
+        });
+}
+
+// A row with more equal logits than a bin's list takes
 template <typename T>
+__device__ __forceinline__ void slow_row(const T* x, int vocab, const Masses& m, const Params& a, float u, const Results& o, Lds& s)
+{
+    const Row<T, 0> r = {x, vocab, {}};
+    Cut c = {0, vocab - 1};
+    Sums all = within(r, m, c, s);
+    if (a.k > 0 && (u64)a.k < all.n) {
+        c = bisect(r, m, c, (u64)a.k, false, vocab, s);
+        all = within(r, m, c, s);
+    }
+    if (a.p < 1.f) c = bisect(r, m, c, share(a.p, all.mass), true, vocab, s);
+    finish<T, 0>(r, nullptr, m, a, c, u, o, s);
+}
+
+template <typename T, int NV>
 __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ uniforms,
                                                      const float* __restrict__ temperature, const int32_t* __restrict__ top_k,
                                                      const float* __restrict__ top_p, const float* __restrict__ min_p,
                                                      int32_t* __restrict__ tokens, float* __restrict__ logprob, int32_t* __restrict__ n_kept,
                                                      float* __restrict__ out)
 {
-    __shared__ Sums lds[WAVES];
-    const int row = blockIdx.x;
-    Row<T> r;
+    __shared__ Lds s;
+    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Row<T, NV> r;
     r.x = logits + (size_t)row * ld;
     r.vocab = vocab;
-    // the largest logit, and whether the row holds a NaN or a +inf
-    unsigned top = 0;
-    u64 bad = 0;
-    for (int i = threadIdx.x; i < vocab; i += TPB) {
-        const float l = r.logit(i);
-        if (!(l < INFINITY)) bad = 1;
-        else top = max(top, key_of(l));
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+    r.load();
+    const float t0 = temperature ? temperature[row] : 1.f, u = uniforms[row];
+    Params a;
+    a.k = t0 > 0.f ? top_k ? top_k[row] : 0 : 1;
+    a.p = top_p ? top_p[row] : 1.f;
+    const float mp = min_p ? min_p[row] : 0.f;
+    a.least = mp > 0.f ? max((u64)ceil(fmin((double)mp, 1.0) * (double)MASS_ONE), (u64)1) : 1;
+
+    // the largest logit, each thread's own, and whether the row holds a NaN or a +inf
+    float mine = -INFINITY;
+    bool bad = false;
+    r.each([&](float l, int) {
+        bad |= !(l < INFINITY);
+        mine = fmaxf(mine, l);
+    });
     {
-        __shared__ unsigned tops[WAVES];
-        if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
-        bad = block_sums(bad, 0, lds).a;
-        for (int w = 0; w < WAVES; ++w) top = max(top, tops[w]);
+        const unsigned w = wave_max(__any(bad) ? 0xffffffffu : key_of(mine));
+        if (lane == 0) s.tops[wave] = w;
     }
-    r.top = __uint_as_float(top ^ ((top >> 31) ? 0x80000000u : 0xffffffffu));
-    r.t = temperature ? temperature[row] : 1.f;
-    r.greedy = !(r.t > 0.f);
-    if (bad || !(r.top > -INFINITY)) {
+    if (threadIdx.x == 0) {
+        s.n_list = 0;
+        s.least_key = 0xffffffffu;
+    }
+    __syncthreads();
+    unsigned top = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = max(top, s.tops[w]);
+    Masses m;
+    m.top = logit_of(top);
+    if (top == 0xffffffffu || !(m.top > -INFINITY)) {
         if (threadIdx.x == 0) {
             tokens[row] = -1;
             if (logprob) logprob[row] = __uint_as_float(0x7fc00000u);
@@ -156,37 +502,79 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
             for (int i = threadIdx.x; i < vocab; i += TPB) out[(size_t)row * vocab + i] = -INFINITY;
         return;
     }
+    m.t = t0 > 0.f ? fminf(t0, 0x1.fffffep127f) : 1.f;
+    m.r = 1.f / m.t;
+    m.per_nat = (float)BINS / (NATS * m.t);
+
     Cut c = {0, vocab - 1};
-    const Sums all = r.sums(c, 0, 1, vocab - 1, lds);
-    u64 z = all.b;
-    const int k = r.greedy ? 1 : top_k ? top_k[row] : 0;
-    if (k > 0 && (u64)k < all.a) {
-        c = shortest(r, c, (u64)k, false, lds);
-        z = r.sums(c, 0, 1, vocab - 1, lds).b;
+    if (a.k == 1) {   // the first token alone
+        int first = 0x7fffffff;
+        r.each([&](float l, int i) {
+            if (l == m.top) first = min(first, i);
+        });
+        const unsigned w = wave_max(0x7fffffffu - (unsigned)first);
+        __syncthreads();
+        if (lane == 0) s.tops[wave] = w;
+        __syncthreads();
+        unsigned best = 0;
+        for (int i = 0; i < WAVES; ++i) best = max(best, s.tops[i]);
+        c = {top, (int)(0x7fffffffu - best)};
     }
-    const float p = top_p ? top_p[row] : 1.f;
-    if (p < 1.f) c = shortest(r, c, max((u64)ceil((double)p * (double)z), (u64)1), true, lds);
-    const float mp = min_p ? min_p[row] : 0.f;
-    r.least = mp > 0.f ? max((u64)ceil(fmin((double)mp, 1.0) * (double)MASS_ONE), (u64)1) : 1;
-    const Sums kept = r.sums(c, 0, r.least, vocab - 1, lds);
-    u64 target = (u64)((double)uniforms[row] * (double)kept.b);
-    target = min(target, kept.b - 1);
-    int first = 0, last = vocab - 1;
-    while (first < last) {
-        const int mid = first + (last - first) / 2;
-        if (r.sums(c, 0, r.least, mid, lds).b > target) last = mid;
-        else first = mid + 1;
-    }
-    if (threadIdx.x == 0) {
-        tokens[row] = first;
-        if (logprob) logprob[row] = (float)log((double)r.mass(r.logit(first)) / (double)kept.b);
-        if (n_kept) n_kept[row] = (int)kept.a;
-    }
-    if (out)
-        for (int i = threadIdx.x; i < vocab; i += TPB) {
-            const float l = r.logit(i);
-            out[(size_t)row * vocab + i] = Row<T>::in(c, key_of(l), i) && r.mass(l) >= r.least ? l : -INFINITY;
+    const Results o = {tokens + row, logprob ? logprob + row : nullptr, n_kept ? n_kept + row : nullptr, out ? out + (size_t)row * vocab : nullptr};
+    if (a.k == 1) {
+        if (threadIdx.x == 0) {
+            *o.token = c.id;
+            if (o.logprob) *o.logprob = 0.f;
+            if (o.n_kept) *o.n_kept = 1;
         }
+        if (o.out)
+            r.each([&](float l, int i) {
+                if (i < vocab) o.out[i] = i == c.id ? l : -INFINITY;
+            });
+        return;
+    }
+    bool listed = false;
+    if (a.k > 1 && a.k <= TPB) {
+        // The k-th largest of the threads' largest logits is at most the k-th largest of all: what is as large makes the list.
+        clear(s, BINS);
+        const bool some = m(mine) > 0;
+        if (some) atomicAdd(&s.hist[m.bin(mine)], 1ull);
+        if (threadIdx.x == 0) s.bin = BINS - 1;
+        __syncthreads();
+        crossing(s, BINS, (u64)a.k);
+        if (some && m.bin(mine) <= s.bin) atomicMin(&s.least_key, key_of(mine));
+        const bool few = __syncthreads_count(some) < a.k;   // then everything with mass may be among the first k
+        const float least = few ? -INFINITY : logit_of(s.least_key);
+        r.each([&](float l, int i) {
+            if (l < least || !(l > -INFINITY)) return;
+            const int at = atomicAdd(&s.n_list, 1);
+            if (at < LIST) {
+                s.lx[at] = l;
+                s.lid[at] = i;
+            }
+        });
+        __syncthreads();
+        listed = s.n_list <= LIST;
+        if (!few) c.key = s.least_key;   // no token outside the list is in
+    }
+    const List list = {&s, s.n_list};
+    if (listed ? cuts(list, m, a, c, vocab, s) : cuts(r, m, a, c, vocab, s)) finish(r, listed ? &list : nullptr, m, a, c, u, o, s);
+    else slow_row<T>(r.x, vocab, m, a, u, o, s);
+}
+
+template <typename T>
+void launch_filter(const spec_filter_args* a, const spec_filter_out* o, hipStream_t s)
+{
+    constexpr int PER = TPB * Vec<T>::N;
+    auto go = [&](auto nv) {
+        constexpr int NV = decltype(nv)::value;
+        hipLaunchKernelGGL((filter_kernel<T, NV>), dim3(a->rows), dim3(TPB), 0, s, (const T*)a->logits, a->ld, a->vocab, a->uniforms, a->temperature,
+                           a->top_k, a->top_p, a->min_p, o->tokens, o->logprob, o->n_kept, o->logits_out);
+    };
+    // rows of up to 32768 logits stay in registers
+    if (a->vocab <= 8192) go(std::integral_constant<int, 8192 / PER>());
+    else if (a->vocab <= 32768) go(std::integral_constant<int, 32768 / PER>());
+    else go(std::integral_constant<int, 0>());
 }
 
 }  // namespace
@@ -212,14 +600,8 @@ extern "C" int spec_filter_sample(const spec_filter_args* a, const spec_filter_o
     if (!a->rows) return SPEC_OK;
     if (!a->logits || !a->uniforms || !o->tokens) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: null pointer");
     if ((uintptr_t)workspace & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: the workspace is not 16-byte aligned");
-    const dim3 grid(a->rows);
-    hipStream_t s = (hipStream_t)stream;
-    if (a->dtype == SPEC_DTYPE_BF16)
-        hipLaunchKernelGGL((filter_kernel<uint16_t>), grid, dim3(TPB), 0, s, (const uint16_t*)a->logits, a->ld, a->vocab, a->uniforms, a->temperature,
-                           a->top_k, a->top_p, a->min_p, o->tokens, o->logprob, o->n_kept, o->logits_out);
-    else
-        hipLaunchKernelGGL((filter_kernel<float>), grid, dim3(TPB), 0, s, (const float*)a->logits, a->ld, a->vocab, a->uniforms, a->temperature,
-                           a->top_k, a->top_p, a->min_p, o->tokens, o->logprob, o->n_kept, o->logits_out);
+    if (a->dtype == SPEC_DTYPE_BF16) launch_filter<uint16_t>(a, o, (hipStream_t)stream);
+    else launch_filter<float>(a, o, (hipStream_t)stream);
     SPECV_LAUNCH_CHECK("filter_kernel");
     return SPEC_OK;
 }
