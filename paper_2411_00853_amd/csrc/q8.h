@@ -59,4 +59,31 @@ __device__ __forceinline__ uint16_t q8_round_bf16(float f)
     return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
+// 16 bytes (4 with DWORD) per lane straight into LDS, to lds + 16 (4) * lane.  The compiler does not know of the request: wait_fetches.
+// (m0 is none of the registers that the compiler hands out, about which it warns; it may set m0 for an instruction of its own.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void q8_fetch_lds(const void* base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+__device__ __forceinline__ void q8_fetch_lds_dword(const void* base, uint32_t offset, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(base) : "memory", "m0");
+}
+#pragma clang diagnostic pop
+template <int N>
+__device__ __forceinline__ void q8_wait_fetches()   // at most N requests of this wavefront still under way
+{
+    static_assert(N < 64, "the counter has six bits");
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void q8_wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void q8_barrier()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 }  // namespace specv

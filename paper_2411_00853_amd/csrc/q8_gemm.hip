@@ -52,7 +52,13 @@ struct Block;
 template <>
 struct Block<uint16_t> {
     typedef q8_intx8 Op;
-    static __device__ __forceinline__ Op op(const q8_intx8& v) { return v; }
+    // The empty statement is where all eight registers are known to be read.  Without it this compiler takes those of an operand that is
+    // carried around a loop for free after the first (seen in the generated code: a product's own result, and addresses, written over them).
+    static __device__ __forceinline__ Op op(q8_intx8 v)
+    {
+        asm("" : "+v"(v));
+        return v;
+    }
     static __device__ __forceinline__ q8_floatx4 dot(const Op& a, const Op& b) { return mfma_fp8(a, b); }
 };
 template <>
@@ -63,10 +69,10 @@ struct Block<float> {
 };
 
 // The operand of one lane: sixteen bytes of either half of the block of 128
+__device__ __forceinline__ q8_intx8 join(const q8_intx4& a, const q8_intx4& b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
 __device__ __forceinline__ q8_intx8 operand(const uint8_t* lo, const uint8_t* hi)
 {
-    const q8_intx4 a = *reinterpret_cast<const q8_intx4*>(lo), b = *reinterpret_cast<const q8_intx4*>(hi);
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    return join(*reinterpret_cast<const q8_intx4*>(lo), *reinterpret_cast<const q8_intx4*>(hi));
 }
 
 __device__ __forceinline__ void store4(float* y, const q8_floatx4& v, int n, int N, bool whole)
@@ -96,13 +102,16 @@ __device__ __forceinline__ void store4(uint16_t* y, const q8_floatx4& v, int n, 
 
 constexpr int TILE = 16 * SPEC_Q8_BLOCK;   // bytes of a 16 x 128 tile of W
 
-// A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out the blocks of K and add their sums up in LDS.
+// ---- few rows: the stream of W ------------------------------------------------------------------------------------------
+//
+// A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out the blocks of K and add their sums up in LDS.  Both
+// operands go straight into registers, the next block's while this one's products run.
 template <int RT, int NT, typename T>
 __global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
                                                      const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles)
 {
     __shared__ q8_floatx4 part[8][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, r16 = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, r16 = lane & 15, g = lane >> 4;
     const int j0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * RT);
     const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
     q8_floatx4 acc[RT][NT];
@@ -110,33 +119,69 @@ __global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__
     for (int a = 0; a < RT; ++a)
 #pragma unroll
         for (int b = 0; b < NT; ++b) acc[a][b] = (q8_floatx4){0.f, 0.f, 0.f, 0.f};
-    int row[RT];
+    const uint8_t* xr[RT];
+    const float* sr[RT];
 #pragma unroll
-    for (int a = 0; a < RT; ++a) row[a] = min(m0 + 16 * a + r16, M - 1);
-    for (int kb = wave; kb < n_blocks; kb += waves) {
-        typename Block<T>::Op wf[NT], xf[RT];
-        float s[RT];
+    for (int a = 0; a < RT; ++a) {
+        const int row = min(m0 + 16 * a + r16, M - 1);
+        xr[a] = x + row * kp + 16 * g;
+        sr[a] = sx + row;
+    }
+    struct Loaded {
+        q8_intx8 w[NT], x[RT];
+        float s[RT], ws[NT];
+    };
+    auto load = [&](Loaded& l, int kb) {
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
-            const uint8_t* p = w + ((size_t)kb * n_tiles + min(j0 + b, n_tiles - 1)) * TILE + lane * 16;
-            wf[b] = Block<T>::op(operand(p, p + 1024));
+            const int j = min(j0 + b, n_tiles - 1);
+            const uint8_t* p = w + ((size_t)kb * n_tiles + j) * TILE + lane * 16;
+            l.w[b] = join(__builtin_nontemporal_load(reinterpret_cast<const q8_intx4*>(p)),
+                          __builtin_nontemporal_load(reinterpret_cast<const q8_intx4*>(p + 1024)));
+            l.ws[b] = sw[(size_t)(j >> 3) * n_blocks + kb];
         }
 #pragma unroll
         for (int a = 0; a < RT; ++a) {
-            const uint8_t* p = x + row[a] * kp + (size_t)kb * SPEC_Q8_BLOCK + 16 * g;
-            xf[a] = Block<T>::op(operand(p, p + 64));
-            s[a] = sx[(size_t)kb * M + row[a]];
+            const uint8_t* p = xr[a] + (size_t)kb * SPEC_Q8_BLOCK;
+            l.x[a] = operand(p, p + 64);
+            l.s[a] = sr[a][(size_t)kb * M];
         }
+    };
+    auto multiply = [&](const Loaded& l) {
+        typename Block<T>::Op xf[RT];
+#pragma unroll
+        for (int a = 0; a < RT; ++a) xf[a] = Block<T>::op(l.x[a]);
 #pragma unroll
         for (int b = 0; b < NT; ++b) {
-            const float ws = sw[(size_t)(min(j0 + b, n_tiles - 1) >> 3) * n_blocks + kb];
+            const typename Block<T>::Op wf = Block<T>::op(l.w[b]);
 #pragma unroll
             for (int a = 0; a < RT; ++a) {
-                const q8_floatx4 d = Block<T>::dot(wf[b], xf[a]);
-                const float f = s[a] * ws;
+                const q8_floatx4 d = Block<T>::dot(wf, xf[a]);
+                const float f = l.s[a] * l.ws[b];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[i], f, acc[a][b][i]);
             }
+        }
+    };
+    Loaded even, odd;
+    int kb = wave;
+    if (kb < n_blocks) {
+        load(even, kb);
+        for (;;) {
+            if (kb + waves >= n_blocks) {
+                multiply(even);
+                break;
+            }
+            load(odd, kb + waves);
+            multiply(even);
+            kb += waves;
+            if (kb + waves >= n_blocks) {
+                multiply(odd);
+                break;
+            }
+            load(even, kb + waves);
+            multiply(odd);
+            kb += waves;
         }
     }
 #pragma unroll
@@ -155,6 +200,109 @@ __global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__
         }
 }
 
+// ---- many rows: the matrix cores ----------------------------------------------------------------------------------------
+//
+// A workgroup of eight wavefronts, WR x WC, takes 16 WR RT rows by 16 WC CT columns.  A stage holds one block of K of both operands
+// as 2 KiB tiles in operand order, so that every LDS read is 1 KiB on end, with the rows' scales behind them.  Stages are fetched
+// S - 1 ahead, straight into LDS.
+template <int WR, int WC, int RT, int CT, int S, typename T>
+__global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
+                                                       const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles,
+                                                       int row_blocks, int col_blocks)
+{
+    static_assert(WR * WC == 8 && CT * 16 <= 128 && 128 % (CT * 16) == 0, "a wavefront's columns share the scale of W");
+    constexpr int BR = WR * RT, BC = WC * CT, KIB = 2 * (BR + BC), U = KIB / 8, STAGE = KIB * 1024 + BR * 64 + 256;
+    static_assert(KIB % 8 == 0 && BR % 4 == 0 && BR <= 28 && S * STAGE <= 160 * 1024, "tile shape");
+    constexpr int PER = U + 1;   // requests of a wavefront for a stage
+    __shared__ __attribute__((aligned(16))) char lds[S * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
+    const int wr = wave / WC, wc = wave % WC;
+    // The row blocks of a column block follow each other on one XCD: its L2 has W once
+    const int total = row_blocks * col_blocks, xcd = blockIdx.x & 7, each = total >> 3, more = total & 7;
+    const int id = xcd * each + min(xcd, more) + (blockIdx.x >> 3);
+    const int m0 = (id % row_blocks) * BR * 16, j0 = (id / row_blocks) * BC;
+    const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+
+    // Request u of this wavefront is the KiB 8 u + wave of a stage: half of a tile, W's first.  Rows and columns beyond the end
+    // are the last ones again (never stored).
+    uint32_t offset[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int kib = 8 * u + wave, tile = kib >> 1, half = kib & 1;
+        if (tile < BC) offset[u] = (uint32_t)min(j0 + tile, n_tiles - 1) * TILE + half * 1024 + lane * 16;
+        else offset[u] = (uint32_t)(min(m0 + 16 * (tile - BC) + r16, M - 1) - min(m0, M - 1)) * (uint32_t)kp + 64 * half + 16 * g;
+    }
+    const uint8_t* xb = x + (size_t)m0 * kp;
+    const uint8_t* wb = w;
+    // 64 scales a wavefront: the rows', and by those left over the columns' blocks' (j0 is a multiple of eight tiles or within one)
+    const bool rows_scales = wave * 4 < BR;
+    const float* sb = rows_scales ? sx : sw;
+    const size_t s_step = rows_scales ? (size_t)M : 1;
+    const uint32_t s_off = rows_scales ? (uint32_t)min(m0 + wave * 64 + lane, M - 1) * 4u : (uint32_t)(min((j0 >> 3) + lane, (n_tiles - 1) >> 3) * n_blocks) * 4u;
+    const uint32_t s_to = lds0 + KIB * 1024 + (rows_scales ? wave * 256 : BR * 64);
+    auto request = [&](int slot) {
+        const uint32_t to = lds0 + slot * STAGE + wave * 1024;
+#pragma unroll
+        for (int u = 0; u < U; ++u) q8_fetch_lds((8 * u + 7) / 2 < BC || (8 * u + wave) / 2 < BC ? wb : xb, offset[u], to + u * 8192);
+        q8_fetch_lds_dword(sb, s_off, s_to + slot * STAGE);
+        wb += (size_t)n_tiles * TILE;
+        xb += SPEC_Q8_BLOCK;
+        sb += s_step;
+    };
+
+    const int w_scale = ((j0 + wc * CT) >> 3) - (j0 >> 3);
+    q8_floatx4 acc[RT][CT];
+#pragma unroll
+    for (int a = 0; a < RT; ++a)
+#pragma unroll
+        for (int b = 0; b < CT; ++b) acc[a][b] = (q8_floatx4){0.f, 0.f, 0.f, 0.f};
+
+    int asked = 0;
+    for (; asked < min(n_blocks, S - 1); ++asked) request(asked);
+    for (int kb = 0; kb < n_blocks; ++kb) {
+        q8_wait_lds();   // what is read of stage kb - 1 is in registers
+        if (asked - 1 - kb >= S - 2) q8_wait_fetches<(S - 2) * PER>();
+        else q8_wait_fetches<0>();
+        q8_barrier();   // stage kb is whole, and every wavefront is done with stage kb - 1
+        if (asked < n_blocks) {
+            request(asked % S);
+            ++asked;
+        }
+        const char* st = lds + (kb % S) * STAGE;
+        const char* wl = st + wc * CT * TILE + lane * 16;
+        const char* xl = st + (BC + wr * RT) * TILE + lane * 16;
+        const float* sl = reinterpret_cast<const float*>(st + KIB * 1024) + wr * RT * 16 + r16;
+        const float ws = *reinterpret_cast<const float*>(st + KIB * 1024 + BR * 64 + 4 * w_scale);
+        typename Block<T>::Op wf[CT];
+#pragma unroll
+        for (int b = 0; b < CT; ++b) {
+            const char* p = wl + b * TILE;
+            wf[b] = Block<T>::op(operand((const uint8_t*)p, (const uint8_t*)p + 1024));
+        }
+#pragma unroll
+        for (int a = 0; a < RT; ++a) {
+            const char* p = xl + a * TILE;
+            const typename Block<T>::Op xf = Block<T>::op(operand((const uint8_t*)p, (const uint8_t*)p + 1024));
+            const float f = sl[16 * a] * ws;
+            q8_floatx4 d[CT];
+#pragma unroll
+            for (int b = 0; b < CT; ++b) d[b] = Block<T>::dot(wf[b], xf);
+#pragma unroll
+            for (int b = 0; b < CT; ++b)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[b][i], f, acc[a][b][i]);
+        }
+    }
+#pragma unroll
+    for (int a = 0; a < RT; ++a) {
+        const int m = m0 + (wr * RT + a) * 16 + r16;
+        if (m >= M) continue;
+#pragma unroll
+        for (int b = 0; b < CT; ++b) store4(y + (size_t)m * N, acc[a][b], (j0 + wc * CT + b) * 16 + 4 * g, N, (N & 3) == 0);
+    }
+}
+
 template <int RT, int NT, typename T>
 void launch_skinny(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
 {
@@ -163,11 +311,39 @@ void launch_skinny(const void* x, const void* w, const float* sx, const float* s
                        (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks, n_tiles);
 }
 
+template <int WR, int WC, int RT, int CT, int S, typename T>
+void launch_tiled(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
+{
+    constexpr int BR = WR * RT, BC = WC * CT;
+    const int n_tiles = (N + 15) / 16, row_blocks = (M + 16 * BR - 1) / (16 * BR), col_blocks = (n_tiles + BC - 1) / BC;
+    auto kernel = tiled_kernel<WR, WC, RT, CT, S, T>;
+    hipLaunchKernelGGL(kernel, dim3(row_blocks * col_blocks), dim3(512), 0, s, (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks,
+                       n_tiles, row_blocks, col_blocks);
+}
+
+template <int RT, typename T>
+void launch_few(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
+{
+    const int n_tiles = (N + 15) / 16;
+    constexpr int MOST = sizeof(T) == 2 || RT < 3 ? 4 : 2;   // with more an fp32 result's operands do not fit the registers
+    if (n_tiles >= 1024) launch_skinny<RT, MOST, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else if (n_tiles >= 512) launch_skinny<RT, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else launch_skinny<RT, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+}
+
 template <typename T>
 void launch_gemm(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
 {
-    if (M <= 16) launch_skinny<1, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    else launch_skinny<4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if (M <= 16) return launch_few<1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if (M <= 32) return launch_few<2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if (M <= 48) return launch_few<3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    const int64_t big = (int64_t)((M + 255) / 256) * ((N + 255) / 256), mid = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
+    // (the fetches' offsets have 32 bits)
+    const bool near = N < (1 << 24) && n_blocks < (1 << 15) && mid < (1 << 30);
+    if constexpr (sizeof(T) == 2)
+        if (near && big >= 200) return launch_tiled<2, 4, 8, 4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if (near && mid >= 128) return launch_tiled<2, 4, 4, 2, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    launch_skinny<4, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
 }
 
 // One thread copies sixteen bytes of the packed order
