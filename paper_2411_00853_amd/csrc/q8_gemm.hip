@@ -106,12 +106,13 @@ constexpr int TILE = 16 * SPEC_Q8_BLOCK;   // bytes of a 16 x 128 tile of W
 //
 // A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out the blocks of K and add their sums up in LDS.  Both
 // operands go straight into registers, the next block's while this one's products run.
-template <int RT, int NT, typename T>
-__global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
+template <int RT, int NT, int WAVES, typename T>
+__global__ void __launch_bounds__(64 * WAVES) skinny_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
                                                      const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles)
 {
-    __shared__ q8_floatx4 part[8][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, r16 = lane & 15, g = lane >> 4;
+    constexpr int waves = WAVES;
+    __shared__ q8_floatx4 part[WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int j0 = blockIdx.x * NT, m0 = blockIdx.y * (16 * RT);
     const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
     q8_floatx4 acc[RT][NT];
@@ -202,17 +203,20 @@ __global__ void __launch_bounds__(512) skinny_kernel(const uint8_t* __restrict__
 
 // ---- many rows: the matrix cores ----------------------------------------------------------------------------------------
 //
-// A workgroup of eight wavefronts, WR x WC, takes 16 WR RT rows by 16 WC CT columns.  A stage holds one block of K of both operands
-// as 2 KiB tiles in operand order, so that every LDS read is 1 KiB on end, with the rows' scales behind them.  Stages are fetched
-// S - 1 ahead, straight into LDS.
+// WR x WC wavefronts take 16 WR RT rows by 16 WC CT columns.  A stage holds one block of K of both operands as 2 KiB tiles, with the
+// scales behind them.  Stages are fetched S - 1 ahead, straight into LDS.
+//
+// W's tiles are in operand order.  A tile of X is 16 rows of 128 bytes, the 16-byte pieces of row n in the order piece ^ (n & 7): eight
+// lanes then fetch a whole line of memory (four rows' pieces of 64 bytes a request come at a third of the rate: 9.6 TB/s from the
+// L2s where whole lines come at 28), and the eight lanes of an LDS cycle still read eight different groups of banks.
 template <int WR, int WC, int RT, int CT, int S, typename T>
-__global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
+__global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
                                                        const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles,
                                                        int row_blocks, int col_blocks)
 {
-    static_assert(WR * WC == 8 && CT * 16 <= 128 && 128 % (CT * 16) == 0, "a wavefront's columns share the scale of W");
-    constexpr int BR = WR * RT, BC = WC * CT, KIB = 2 * (BR + BC), U = KIB / 8, STAGE = KIB * 1024 + BR * 64 + 256;
-    static_assert(KIB % 8 == 0 && BR % 4 == 0 && BR <= 28 && S * STAGE <= 160 * 1024, "tile shape");
+    static_assert(CT * 16 <= 128 && 128 % (CT * 16) == 0, "a wavefront's columns share the scale of W");
+    constexpr int W = WR * WC, BR = WR * RT, BC = WC * CT, KIB = 2 * (BR + BC), U = (KIB + W - 1) / W, STAGE = KIB * 1024 + (BR + 3) / 4 * 256 + 256;
+    static_assert((BR + 3) / 4 < W && S * STAGE <= 160 * 1024, "tile shape");
     constexpr int PER = U + 1;   // requests of a wavefront for a stage
     __shared__ __attribute__((aligned(16))) char lds[S * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
@@ -224,14 +228,14 @@ __global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict
     const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
 
-    // Request u of this wavefront is the KiB 8 u + wave of a stage: half of a tile, W's first.  Rows and columns beyond the end
+    // Request u of this wavefront is the KiB W u + wave of a stage: half of a tile, W's first.  Rows and columns beyond the end
     // are the last ones again (never stored).
     uint32_t offset[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int kib = 8 * u + wave, tile = kib >> 1, half = kib & 1;
+        const int kib = min(W * u + wave, KIB - 1), tile = kib >> 1, half = kib & 1;   // (a wavefront without one repeats the last)
         if (tile < BC) offset[u] = (uint32_t)min(j0 + tile, n_tiles - 1) * TILE + half * 1024 + lane * 16;
-        else offset[u] = (uint32_t)(min(m0 + 16 * (tile - BC) + r16, M - 1) - min(m0, M - 1)) * (uint32_t)kp + 64 * half + 16 * g;
+        else offset[u] = (uint32_t)(min(m0 + 16 * (tile - BC) + 8 * half + (lane >> 3), M - 1) - m0) * (uint32_t)kp + (((lane & 7) ^ (lane >> 3)) * 16);
     }
     const uint8_t* xb = x + (size_t)m0 * kp;
     const uint8_t* wb = w;
@@ -240,15 +244,21 @@ __global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict
     const float* sb = rows_scales ? sx : sw;
     const size_t s_step = rows_scales ? (size_t)M : 1;
     const uint32_t s_off = rows_scales ? (uint32_t)min(m0 + wave * 64 + lane, M - 1) * 4u : (uint32_t)(min((j0 >> 3) + lane, (n_tiles - 1) >> 3) * n_blocks) * 4u;
-    const uint32_t s_to = lds0 + KIB * 1024 + (rows_scales ? wave * 256 : BR * 64);
-    auto request = [&](int slot) {
-        const uint32_t to = lds0 + slot * STAGE + wave * 1024;
-#pragma unroll
-        for (int u = 0; u < U; ++u) q8_fetch_lds((8 * u + 7) / 2 < BC || (8 * u + wave) / 2 < BC ? wb : xb, offset[u], to + u * 8192);
-        q8_fetch_lds_dword(sb, s_off, s_to + slot * STAGE);
+    const uint32_t s_to = lds0 + KIB * 1024 + (rows_scales ? wave * 256 : (BR + 3) / 4 * 256);
+    uint32_t slot_to = 0;
+    auto request = [&](int u) {
+        if (u < U) {
+            const int kib = min(W * u + wave, KIB - 1);
+            q8_fetch_lds((W * u + W - 1) / 2 < BC || kib / 2 < BC ? wb : xb, offset[u], lds0 + slot_to + kib * 1024);
+        } else {
+            q8_fetch_lds_dword(sb, s_off, s_to + slot_to);
+        }
+    };
+    auto advance = [&]() {
         wb += (size_t)n_tiles * TILE;
         xb += SPEC_Q8_BLOCK;
         sb += s_step;
+        slot_to = slot_to == (S - 1) * STAGE ? 0 : slot_to + STAGE;
     };
 
     const int w_scale = ((j0 + wc * CT) >> 3) - (j0 >> 3);
@@ -259,40 +269,63 @@ __global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict
         for (int b = 0; b < CT; ++b) acc[a][b] = (q8_floatx4){0.f, 0.f, 0.f, 0.f};
 
     int asked = 0;
-    for (; asked < min(n_blocks, S - 1); ++asked) request(asked);
+    for (; asked < min(n_blocks, S - 1); ++asked) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) request(u);
+        advance();
+    }
+    uint32_t from = 0;
+    const char* const wl0 = lds + wc * CT * TILE + lane * 16;
+    const char* const xl0 = lds + (BC + wr * RT) * TILE + r16 * 128 + ((g ^ (r16 & 7)) * 16);
+    const char* const xh0 = lds + (BC + wr * RT) * TILE + r16 * 128 + (((g ^ (r16 & 7)) * 16) ^ 64);
     for (int kb = 0; kb < n_blocks; ++kb) {
         q8_wait_lds();   // what is read of stage kb - 1 is in registers
         if (asked - 1 - kb >= S - 2) q8_wait_fetches<(S - 2) * PER>();
         else q8_wait_fetches<0>();
         q8_barrier();   // stage kb is whole, and every wavefront is done with stage kb - 1
-        if (asked < n_blocks) {
-            request(asked % S);
+        const char *wl = wl0 + from, *xl = xl0 + from, *xh = xh0 + from;
+        const float* sl = reinterpret_cast<const float*>(lds + from + KIB * 1024) + wr * RT * 16 + r16;
+        auto read_x = [&](int a) { return Block<T>::op(operand((const uint8_t*)xl + a * TILE, (const uint8_t*)xh + a * TILE)); };
+        // X tiles read ahead, and requests between the products rather than in front of the LDS reads, which they hold up: not with the
+        // largest accumulators, where either costs more registers than there are
+        constexpr bool ROOM = RT * CT < 32;
+        constexpr int AHEAD = ROOM ? 1 : 0;
+        const bool more = asked < n_blocks;
+        if (!ROOM && more) {
+#pragma unroll
+            for (int u = 0; u < PER; ++u) request(u);
+            advance();
             ++asked;
         }
-        const char* st = lds + (kb % S) * STAGE;
-        const char* wl = st + wc * CT * TILE + lane * 16;
-        const char* xl = st + (BC + wr * RT) * TILE + lane * 16;
-        const float* sl = reinterpret_cast<const float*>(st + KIB * 1024) + wr * RT * 16 + r16;
-        const float ws = *reinterpret_cast<const float*>(st + KIB * 1024 + BR * 64 + 4 * w_scale);
-        typename Block<T>::Op wf[CT];
+        typename Block<T>::Op wf[CT], xf[1 + AHEAD];
+        if (AHEAD) xf[0] = read_x(0);
 #pragma unroll
         for (int b = 0; b < CT; ++b) {
             const char* p = wl + b * TILE;
             wf[b] = Block<T>::op(operand((const uint8_t*)p, (const uint8_t*)p + 1024));
         }
+        const float ws = *reinterpret_cast<const float*>(lds + from + KIB * 1024 + (BR + 3) / 4 * 256 + 4 * w_scale);
 #pragma unroll
         for (int a = 0; a < RT; ++a) {
-            const char* p = xl + a * TILE;
-            const typename Block<T>::Op xf = Block<T>::op(operand((const uint8_t*)p, (const uint8_t*)p + 1024));
+            if (a + AHEAD < RT) xf[(a + AHEAD) & AHEAD] = read_x(a + AHEAD);
             const float f = sl[16 * a] * ws;
             q8_floatx4 d[CT];
 #pragma unroll
-            for (int b = 0; b < CT; ++b) d[b] = Block<T>::dot(wf[b], xf);
+            for (int b = 0; b < CT; ++b) d[b] = Block<T>::dot(wf[b], xf[a & AHEAD]);
+            if (ROOM && more) {
+#pragma unroll
+                for (int u = a; u < PER; u += RT) request(u);
+            }
 #pragma unroll
             for (int b = 0; b < CT; ++b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[b][i], f, acc[a][b][i]);
         }
+        if (ROOM && more) {
+            advance();
+            ++asked;
+        }
+        from = from == (S - 1) * STAGE ? 0 : from + STAGE;
     }
 #pragma unroll
     for (int a = 0; a < RT; ++a) {
@@ -303,11 +336,11 @@ __global__ void __launch_bounds__(512, 2) tiled_kernel(const uint8_t* __restrict
     }
 }
 
-template <int RT, int NT, typename T>
+template <int RT, int NT, int WAVES, typename T>
 void launch_skinny(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
 {
     const int n_tiles = (N + 15) / 16;
-    hipLaunchKernelGGL((skinny_kernel<RT, NT, T>), dim3((n_tiles + NT - 1) / NT, (M + 16 * RT - 1) / (16 * RT)), dim3(512), 0, s,
+    hipLaunchKernelGGL((skinny_kernel<RT, NT, WAVES, T>), dim3((n_tiles + NT - 1) / NT, (M + 16 * RT - 1) / (16 * RT)), dim3(64 * WAVES), 0, s,
                        (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks, n_tiles);
 }
 
@@ -317,33 +350,68 @@ void launch_tiled(const void* x, const void* w, const float* sx, const float* sw
     constexpr int BR = WR * RT, BC = WC * CT;
     const int n_tiles = (N + 15) / 16, row_blocks = (M + 16 * BR - 1) / (16 * BR), col_blocks = (n_tiles + BC - 1) / BC;
     auto kernel = tiled_kernel<WR, WC, RT, CT, S, T>;
-    hipLaunchKernelGGL(kernel, dim3(row_blocks * col_blocks), dim3(512), 0, s, (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks,
+    hipLaunchKernelGGL(kernel, dim3(row_blocks * col_blocks), dim3(64 * WR * WC), 0, s, (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks,
                        n_tiles, row_blocks, col_blocks);
 }
 
+// Up to 64 rows.  Wide matrices: a workgroup takes WC column tiles, as many workgroups as fit the 256 compute units in one go, and X
+// passes through LDS once for all of them.  Others: a column tile or two a workgroup, whose wavefronts share out K -- 32 rows of 4096
+// x 4096 take 7.1 us that way and 12.2 the other, of 22016 x 4096 23.7 and 20.7; 48 rows of 22016 x 4096 31.0 and 21.0.
 template <int RT, typename T>
-void launch_few(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
+void launch_few(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, bool near, hipStream_t s)
 {
     const int n_tiles = (N + 15) / 16;
-    constexpr int MOST = sizeof(T) == 2 || RT < 3 ? 4 : 2;   // with more an fp32 result's operands do not fit the registers
-    if (n_tiles >= 1024) launch_skinny<RT, MOST, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    else if (n_tiles >= 512) launch_skinny<RT, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    else launch_skinny<RT, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if constexpr (RT == 1) {
+        // (one row of 22016 x 4096: 15.5 us with two tiles and eight wavefronts, 17.0 with one; 8 rows of 12288 x 4096: 9.8 with one
+        // tile and four wavefronts, 11.7 with eight; 2048 x 8192: 5.9 with sixteen, 6.4 with eight)
+        if (n_tiles >= 1024) launch_skinny<1, 2, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles >= 512) launch_skinny<1, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_blocks < 48) launch_skinny<1, 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else launch_skinny<1, 1, 16, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    } else {
+        if (n_tiles > 1536 && near) launch_tiled<1, 8, RT, 1, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 1024 && near) launch_tiled<1, 6, RT, 1, 5, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 512 && near) launch_tiled<1, 4, RT, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 256 && RT < 4) launch_skinny<RT, RT < 4 ? 2 : 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 256 && near) launch_tiled<2, 4, 2, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else launch_skinny<RT, 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    }
 }
+
+// A tile shape's time for one block of K, in us with a workgroup on every compute unit (bf16 results, K = 4096)
+struct TileShape {
+    int rows, cols;
+    float us;
+};
+constexpr TileShape SHAPES[] = {{64, 64, 0.35f}, {64, 128, 0.45f}, {128, 128, 0.7f}, {256, 128, 1.1f}, {256, 256, 2.1f}};
 
 template <typename T>
 void launch_gemm(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
 {
-    if (M <= 16) return launch_few<1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    if (M <= 32) return launch_few<2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    if (M <= 48) return launch_few<3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    const int64_t big = (int64_t)((M + 255) / 256) * ((N + 255) / 256), mid = (int64_t)((M + 127) / 128) * ((N + 127) / 128);
-    // (the fetches' offsets have 32 bits)
-    const bool near = N < (1 << 24) && n_blocks < (1 << 15) && mid < (1 << 30);
-    if constexpr (sizeof(T) == 2)
-        if (near && big >= 200) return launch_tiled<2, 4, 8, 4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    if (near && mid >= 128) return launch_tiled<2, 4, 4, 2, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    launch_skinny<4, 1, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    const bool near = N < (1 << 24) && n_blocks < (1 << 15);   // the fetches' offsets have 32 bits
+    if (M <= 16) return launch_few<1, T>(x, w, sx, sw, y, M, N, n_blocks, near, s);
+    if (M <= 32) return launch_few<2, T>(x, w, sx, sw, y, M, N, n_blocks, near, s);
+    if (M <= 48) return launch_few<3, T>(x, w, sx, sw, y, M, N, n_blocks, near, s);
+    // (up to 64 workgroups of the smallest tile: 100 rows of 1024 x 8192 take 18.6 us with K shared out, 23.4 with tiles)
+    if (M <= 64 || !near || (int64_t)((M + 63) / 64) * ((N + 63) / 64) <= 64) return launch_few<4, T>(x, w, sx, sw, y, M, N, n_blocks, near, s);
+    // the shape of the fewest rounds of 256 workgroups, each at its price (an fp32 result's operands fit the smaller ones only)
+    int best = 0;
+    float least = 0.f;
+    for (int i = 0; i < (sizeof(T) == 2 ? 5 : 3); ++i) {
+        const int64_t wgs = (int64_t)((M + SHAPES[i].rows - 1) / SHAPES[i].rows) * ((N + SHAPES[i].cols - 1) / SHAPES[i].cols);
+        const float us = (float)((wgs + 255) / 256) * SHAPES[i].us;
+        if (i == 0 || us < least) {
+            least = us;
+            best = i;
+        }
+    }
+    if constexpr (sizeof(T) == 2) {
+        if (best == 4) return launch_tiled<2, 4, 8, 4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        if (best == 3) return launch_tiled<4, 2, 4, 4, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    }
+    if (best == 2) launch_tiled<2, 4, 4, 2, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else if (best == 1) launch_tiled<2, 4, 2, 2, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else launch_tiled<2, 4, 2, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
 }
 
 // One thread copies sixteen bytes of the packed order

@@ -48,6 +48,16 @@ def test_many_rows(M, N, K, dtype):
     check(M, N, K, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N,K", [(1, 20000, 1200), (9, 9000, 700), (3, 500, 8192), (16, 4100, 5000),      # a column tile or two a workgroup
+                                   (20, 3000, 1500), (30, 6001, 1100), (20, 9000, 900), (32, 20000, 700), (25, 30000, 600),
+                                   (40, 3000, 1500), (48, 6001, 1100), (33, 9000, 900), (40, 20000, 700), (45, 30000, 600),
+                                   (50, 3000, 1500), (64, 6001, 1100), (57, 9000, 900), (64, 20000, 700), (60, 30000, 600),
+                                   (70, 2000, 2500), (600, 2500, 1300), (900, 4000, 1290), (2048, 8192, 900)])
+def test_every_launch_shape(M, N, K, dtype):
+    check(M, N, K, dtype)
+
+
 def test_every_row_count_up_to_a_few_tiles():
     for M in range(1, 140, 3):
         check(M, 272, 384, "fp32", M)
