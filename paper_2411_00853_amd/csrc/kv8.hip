@@ -46,112 +46,133 @@ __device__ __forceinline__ float pow2_scale(float amax)
 
 constexpr int APPEND_TPB = 256;
 
-// A workgroup takes one page of one sequence and kv head: its new positions are rotated into LDS, their magnitude and the page's older
-// positions decide the scale, and the bytes are written by their one owner.  It also rotates the queries of its heads and rows.
+// Eight dimensions and the eight they are rotated with
+struct Octets {
+    float lo[8], hi[8];
+};
+
+__device__ __forceinline__ Octets load_octets(const uint16_t* p, int half)
+{
+    Octets o;
+    q8_load8(p, o.lo);
+    q8_load8(p + half, o.hi);
+    return o;
+}
+
+__device__ __forceinline__ void rotate(Octets& o, const float2* cs)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float2 c = cs[i];
+        const float x = o.lo[i] * c.x - o.hi[i] * c.y;
+        o.hi[i] = o.hi[i] * c.x + o.lo[i] * c.y;
+        o.lo[i] = x;
+    }
+}
+
+// Two kinds of workgroups for a sequence and kv head.  The first `pages` take one page each: a thread has sixteen dimensions of a new
+// position's key and value in registers, their magnitudes and the page's older positions decide the scale, and the bytes are written by
+// their one owner.  The rest rotate the queries of the head, sixteen dimensions a thread.
 template <int HD>
 __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __restrict__ qkv, const int32_t* __restrict__ row0,
-                                                            const int32_t* __restrict__ kv_len, Pages c, const float2* __restrict__ cos_sin,
-                                                            int max_pos, int rows, int group, uint16_t* __restrict__ q_out)
+                                                            const int32_t* __restrict__ kv_len, const float2* __restrict__ cos_sin, int pages,
+                                                            int max_pos, int rows, int group, uint16_t* __restrict__ q_out, Pages c)
 {
-    __shared__ float fresh[2][PAGE][HD];
-    __shared__ unsigned top[2];
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, hk = c.n_kv_heads, hq = hk * group;
+    constexpr int OCTETS = HD / 16, AT_ONCE = APPEND_TPB / OCTETS;   // positions of a workgroup: 32 or 64
+    static_assert(AT_ONCE >= PAGE, "a page's positions at once");
+    __shared__ unsigned top[2][APPEND_TPB / 64];
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, hk = c.n_kv_heads, hq = hk * group, oct = tid % OCTETS, d = oct * 8;
     int r0, w;
     if (!window_of(row0, b, rows, &r0, &w)) return;
     const int n = kv_len[b], ld = (hq + 2 * hk) * HD;
-    if (n < 0 || n >= c.blocks * PAGE) {   // no place for any row (the first workgroup of a head says so)
-        if (q_out && blockIdx.x == 0)
-            for (int i = tid; i < w * group * HD; i += APPEND_TPB)
-                q_out[(size_t)(r0 + i / (group * HD)) * hq * HD + h * group * HD + i % (group * HD)] = 0;
+    const int limit = min(c.blocks * PAGE, cos_sin ? max_pos : 0x7fffffff);   // positions there is a place for
+    if ((int)blockIdx.x >= pages) {
+        const int i = ((int)blockIdx.x - pages) * AT_ONCE + tid / OCTETS, j = i / group, head = h * group + i % group;
+        if (j >= w) return;
+        Octets o = load_octets(qkv + (size_t)(r0 + j) * ld + head * HD + d, HD / 2);
+        const long pos = (long)n + j;
+        const bool in = n >= 0 && pos < limit;
+        if (cos_sin) rotate(o, cos_sin + (in ? pos : 0) * (HD / 2) + d);
+        uint16_t lo[8], hi[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            lo[e] = in ? q8_round_bf16(o.lo[e]) : 0;
+            hi[e] = in ? q8_round_bf16(o.hi[e]) : 0;
+        }
+        uint16_t* dst = q_out + ((size_t)(r0 + j) * hq + head) * HD + d;
+        *reinterpret_cast<q8_intx4*>(dst) = *reinterpret_cast<const q8_intx4*>(lo);
+        *reinterpret_cast<q8_intx4*>(dst + HD / 2) = *reinterpret_cast<const q8_intx4*>(hi);
         return;
     }
-    const int blk = n / PAGE + blockIdx.x, lo = max(blk * PAGE, n), hi = (int)min((long)blk * PAGE + PAGE, (long)n + w);
+    if (n < 0 || n >= limit) return;
+    const int blk = n / PAGE + blockIdx.x;
+    const int lo = max(blk * PAGE, n), hi = (int)min((long)min((long)blk * PAGE + PAGE, (long)n + w), (long)limit);
     if (lo >= hi) return;
-    const int page = blk < c.blocks ? c.table[(size_t)b * c.blocks + blk] : -1;
-    const int seen = min(hi, cos_sin ? max_pos : hi);   // positions the rotation table has
-    if (q_out) {   // a thread a pair of dimensions of a query
-        for (int i = tid; i < (hi - lo) * group * (HD / 2); i += APPEND_TPB) {
-            const int d = i % (HD / 2), k = i / (HD / 2), head = h * group + k % group, pos = lo + k / group, row = r0 + pos - n;
-            const uint16_t* src = qkv + (size_t)row * ld + head * HD + d;
-            float a = q8_widen(src[0]), o = q8_widen(src[HD / 2]);
-            if (cos_sin) {
-                const float2 cs = pos < seen ? cos_sin[(size_t)pos * (HD / 2) + d] : make_float2(0.f, 0.f);
-                const float x = a * cs.x - o * cs.y;
-                o = o * cs.x + a * cs.y;
-                a = x;
-            }
-            const bool in = pos < seen && blk < c.blocks;
-            uint16_t* dst = q_out + ((size_t)row * hq + head) * HD + d;
-            dst[0] = in ? q8_round_bf16(a) : 0;
-            dst[HD / 2] = in ? q8_round_bf16(o) : 0;
-        }
-    }
-    if (page < 0 || page >= c.n_pages || lo >= seen) return;
-    if (tid < 2) top[tid] = 0;
-    __syncthreads();
-    unsigned mk = 0, mv = 0;
-    auto grown = [](unsigned m, float f) {   // the largest finite magnitude
-        const unsigned u = __float_as_uint(f) & 0x7fffffffu;
-        return u < 0x7f800000u ? max(m, u) : m;
-    };
-    for (int i = tid; i < (seen - lo) * (HD / 2); i += APPEND_TPB) {
-        const int d = i % (HD / 2), pos = lo + i / (HD / 2), t = pos - blk * PAGE;
-        const uint16_t* src = qkv + (size_t)(r0 + pos - n) * ld + (hq + h) * HD + d;
-        float a = q8_widen(src[0]), o = q8_widen(src[HD / 2]);
-        if (cos_sin) {
-            const float2 cs = cos_sin[(size_t)pos * (HD / 2) + d];
-            const float x = a * cs.x - o * cs.y;
-            o = o * cs.x + a * cs.y;
-            a = x;
-        }
-        const float v0 = q8_widen(src[hk * HD]), v1 = q8_widen(src[hk * HD + HD / 2]);
-        fresh[0][t][d] = a;
-        fresh[0][t][d + HD / 2] = o;
-        fresh[1][t][d] = v0;
-        fresh[1][t][d + HD / 2] = v1;
-        mk = grown(grown(mk, a), o);
-        mv = grown(grown(mv, v0), v1);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        mk = max(mk, (unsigned)__shfl_xor((int)mk, d));
-        mv = max(mv, (unsigned)__shfl_xor((int)mv, d));
-    }
-    if ((tid & 63) == 0) {
-        atomicMax(&top[0], mk);
-        atomicMax(&top[1], mv);
-    }
-    __syncthreads();
-    const int older = max(n - blk * PAGE, 0), first = lo - blk * PAGE, last = seen - blk * PAGE;
+    const int page = c.table[(size_t)b * c.blocks + blk];
+    if (page < 0 || page >= c.n_pages) return;
     float* sc = c.scales + ((size_t)page * hk + h) * 2;
     uint8_t* bytes = c.data + ((size_t)page * hk + h) * (2 * PAGE * HD);
-    float was[2], s[2];
+    const float was[2] = {sc[0], sc[1]};
+    const int pos = lo + tid / OCTETS, t = pos - blk * PAGE, older = max(n - blk * PAGE, 0);
+    const bool mine = pos < hi;
+    Octets x[2];
+    unsigned most[2] = {0, 0};
+    if (mine) {
+        const uint16_t* src = qkv + (size_t)(r0 + pos - n) * ld + (hq + h) * HD + d;
+        x[0] = load_octets(src, HD / 2);
+        x[1] = load_octets(src + hk * HD, HD / 2);
+        if (cos_sin) rotate(x[0], cos_sin + (size_t)pos * (HD / 2) + d);
+        auto grown = [](unsigned m, float f) {   // the largest finite magnitude
+            const unsigned u = __float_as_uint(f) & 0x7fffffffu;
+            return u < 0x7f800000u ? max(m, u) : m;
+        };
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-        const float need = pow2_scale(__uint_as_float(top[kv]));
-        was[kv] = sc[kv];
-        s[kv] = older ? fmaxf(was[kv], need) : need;
+        for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most[kv] = grown(grown(most[kv], x[kv].lo[e]), x[kv].hi[e]);
     }
-    __syncthreads();   // every thread has read the old scales
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
+        most[kv] = q8_wave_max(most[kv]);
+        if ((tid & 63) == 0) top[kv][tid >> 6] = most[kv];
+    }
+    __syncthreads();   // also: every thread has the old scales
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+        unsigned m = 0;
+#pragma unroll
+        for (int k = 0; k < APPEND_TPB / 64; ++k) m = max(m, top[kv][k]);
+        const float need = pow2_scale(__uint_as_float(m)), s = older ? fmaxf(was[kv], need) : need, r = 1.f / s;
         uint8_t* p = bytes + kv * PAGE * HD;
-        const float r = 1.f / s[kv];
-        for (int i = tid; i < (last - first) * HD; i += APPEND_TPB) {
-            const int t = first + i / HD, d = i % HD;
-            const float f = fresh[kv][t][d] * r;
-            // beyond 448 lie only an infinity and what is not a number
-            const unsigned v = fabsf(f) <= 2.f * Q8_MAX ? q8_pack4(f, 0.f, 0.f, 0.f) : 0x7fu;
-            p[kv ? value_byte(t, d) : key_byte<HD>(t, d)] = (uint8_t)v;
+        if (mine) {
+            auto byte = [&](float f) {   // beyond 448 lie only an infinity and what is not a number
+                f *= r;
+                return fabsf(f) <= 2.f * Q8_MAX ? f : __uint_as_float(0x7fc00000u);
+            };
+            const Octets& v = x[kv];
+            const unsigned a0 = q8_pack4(byte(v.lo[0]), byte(v.lo[1]), byte(v.lo[2]), byte(v.lo[3]));
+            const unsigned a1 = q8_pack4(byte(v.lo[4]), byte(v.lo[5]), byte(v.lo[6]), byte(v.lo[7]));
+            const unsigned b0 = q8_pack4(byte(v.hi[0]), byte(v.hi[1]), byte(v.hi[2]), byte(v.hi[3]));
+            const unsigned b1 = q8_pack4(byte(v.hi[4]), byte(v.hi[5]), byte(v.hi[6]), byte(v.hi[7]));
+            if (kv == 0) {
+                *reinterpret_cast<uint2*>(p + key_byte<HD>(t, d)) = make_uint2(a0, a1);
+                *reinterpret_cast<uint2*>(p + key_byte<HD>(t, d + HD / 2)) = make_uint2(b0, b1);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    p[value_byte(t, d + e)] = (uint8_t)((e < 4 ? a0 : a1) >> (8 * (e & 3)));
+                    p[value_byte(t, d + HD / 2 + e)] = (uint8_t)((e < 4 ? b0 : b1) >> (8 * (e & 3)));
+                }
+            }
         }
-        if (older && s[kv] > was[kv]) {
+        if (older && s > was[kv]) {
             const float f = was[kv] * r;
             for (int i = tid; i < older * HD; i += APPEND_TPB) {
-                const int t = i / HD, d = i % HD, at = kv ? value_byte(t, d) : key_byte<HD>(t, d);
+                const int at = kv ? value_byte(i / HD, i % HD) : key_byte<HD>(i / HD, i % HD);
                 p[at] = (uint8_t)q8_pack4(q8_unpack(p[at]) * f, 0.f, 0.f, 0.f);
             }
         }
-        if (tid == 0) sc[kv] = s[kv];
+        if (tid == 0) sc[kv] = s;
     }
 }
 
@@ -176,7 +197,7 @@ struct AttnArgs {
     int64_t ld_q;
     const int32_t* row0;
     const int32_t* kv_len;
-    int rows, group, parts, tiles;
+    int rows, group, parts, part_pages, tiles;   // part_pages: of each part but a sequence's last, which takes what is left
     float scale;          // of the scores, times log2(e)
     uint16_t* out;
     float* part_o;        // [rows][heads][parts][HD]
@@ -197,14 +218,8 @@ __device__ __forceinline__ q8_halfx8 values8(unsigned a, unsigned b)
     return (q8_halfx8){x[0], x[1], y[0], y[1], z[0], z[1], w[0], w[1]};
 }
 
-__device__ __forceinline__ bool has_nan(unsigned x) { return (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0; }
-
-// The four positions base .. base + 3 of a word, those beyond `last` zero
-__device__ __forceinline__ unsigned upto(unsigned x, int base, int last)
-{
-    const int keep = last - base + 1;   // bytes
-    return keep >= 4 ? x : keep <= 0 ? 0u : x & ((1u << (8 * keep)) - 1u);
-}
+// 0xff in the bytes that are no numbers
+__device__ __forceinline__ unsigned nan_bytes(unsigned x) { return ((((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xffu; }
 
 template <int HD, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
@@ -213,7 +228,8 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     __shared__ q8_floatx4 merged[NW][DT][64];
     __shared__ float2 ml[NW][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
-    const int b = blockIdx.z, h = blockIdx.y / a.tiles, q0 = (blockIdx.y % a.tiles) * (16 * RT), hk = a.c.n_kv_heads;
+    // (heads fastest: consecutive workgroups go to different XCDs, and a part that many sequences lack would leave one of them idle)
+    const int b = blockIdx.z, hk = a.c.n_kv_heads, h = blockIdx.x % hk, q0 = (blockIdx.x / hk) * (16 * RT), part = blockIdx.y;
     int r0, w;
     if (!window_of(a.row0, b, a.rows, &r0, &w)) return;
     const int n_q = w * a.group;
@@ -221,7 +237,14 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     const int cap = a.c.blocks * PAGE, given = a.kv_len[b], n = min(given, cap);
     const int j_lo = q0 / a.group, j_hi = min(n_q - 1, q0 + 16 * RT - 1) / a.group;
     const int len = given < 0 ? 0 : (int)min((long)n + j_hi + 1, (long)cap), n_blk = (len + PAGE - 1) / PAGE;
-    const int per = (n_blk + a.parts - 1) / a.parts, c0 = min(n_blk, (int)blockIdx.x * per), c1 = min(n_blk, c0 + per);
+    if (part > 0 && part * a.part_pages >= n_blk) {   // nothing to do: says so
+        for (int i = threadIdx.x; i < min(16 * RT, n_q - q0); i += 64 * NW) {
+            const int qi = q0 + i;
+            a.part_ml[((size_t)(r0 + qi / a.group) * hk * a.group + h * a.group + qi % a.group) * a.parts + part] = make_float2(REF_NONE, 0.f);
+        }
+        return;
+    }
+    const int c0 = part * a.part_pages, c1 = part == a.parts - 1 ? n_blk : min(n_blk, c0 + a.part_pages);
 
     q8_bf16x8 qf[RT][KC][2];
     int lim[RT];
@@ -248,22 +271,27 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
         for (int d = 0; d < DT; ++d) o[t][d] = zero;
     }
     const int32_t* pages = a.c.table + (size_t)b * a.c.blocks;
-
-    for (int blk = c0 + wave; blk < c1; blk += NW) {
-        const int page = pages[blk];
-        if (page < 0 || page >= a.c.n_pages) continue;
-        const size_t at = (size_t)page * hk + h;
-        const uint8_t* kp = a.c.data + at * (2 * PAGE * HD) + lane * 16;
-        q8_intx4 kr[2][KC], vr[DT / 2];
+    struct Page {
+        q8_intx4 k[2][KC], v[DT / 2];
+    };
+    auto fetch_k = [&](Page& pg, int page) {
+        const uint8_t* kp = a.c.data + ((size_t)page * hk + h) * (2 * PAGE * HD) + lane * 16;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int k = 0; k < KC; ++k) kr[s][k] = *reinterpret_cast<const q8_intx4*>(kp + (s * KC + k) * 1024);
+            for (int k = 0; k < KC; ++k) pg.k[s][k] = __builtin_nontemporal_load(reinterpret_cast<const q8_intx4*>(kp + (s * KC + k) * 1024));
+    };
+    auto fetch_v = [&](Page& pg, int page) {
+        const uint8_t* vp = a.c.data + ((size_t)page * hk + h) * (2 * PAGE * HD) + PAGE * HD + lane * 16;
 #pragma unroll
-        for (int d = 0; d < DT / 2; ++d) vr[d] = *reinterpret_cast<const q8_intx4*>(kp + PAGE * HD + d * 1024);
-        const float ks = a.c.scales[at * 2] * a.scale, vs = a.c.scales[at * 2 + 1];
-        const float lv = fmaxf(__log2f(vs), LOG2_VS_LEAST), inv = exp2f(-lv);
-
+        for (int d = 0; d < DT / 2; ++d) pg.v[d] = __builtin_nontemporal_load(reinterpret_cast<const q8_intx4*>(vp + d * 1024));
+    };
+    // Scores of page blk against all rows, weights, and the weighted values; the registers of its keys and values take page `next`
+    // as soon as they are free.  (These loads are never branched around, or every wait would be for all of them: behind the last page it
+    // is read again.)
+    auto take = [&](Page& pg, int blk, bool there, float ks, float lv, float inv, int next) {
+        const auto& kr = pg.k;
+        auto& vr = pg.v;
         q8_floatx4 sc[RT][2];
 #pragma unroll
         for (int t = 0; t < RT; ++t) sc[t][0] = sc[t][1] = zero;
@@ -277,9 +305,11 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
                     sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[t][k][0], sc[t][s], 0, 0, 0);
                     sc[t][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[t][k][1], sc[t][s], 0, 0, 0);
                 }
+                __builtin_amdgcn_sched_barrier(0);   // all of a page widened at once would not fit the registers
             }
+        fetch_k(pg, next);
         const int first = blk * PAGE;
-        const bool masked = first + PAGE - 1 > n + j_lo;
+        const bool masked = !there || first + PAGE - 1 > n + j_lo;
         q8_halfx8 p[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
@@ -289,7 +319,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v = fmaf(sc[t][s][i], ks, lv);
-                    if (masked) v = first + 16 * s + 4 * g + i <= lim[t] ? v : -INFINITY;
+                    if (masked) v = there && first + 16 * s + 4 * g + i <= lim[t] ? v : -INFINITY;
                     x[4 * s + i] = v;
                     m = fmaxf(m, v);
                 }
@@ -311,39 +341,61 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
             }
             sum[t] = fmaf(add, inv, sum[t]);
         }
-        bool odd = false;   // a masked place holds what is not a number: zero times it would not be zero
         if (masked) {
             unsigned f = 0;
 #pragma unroll
             for (int d = 0; d < DT / 2; ++d)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f |= has_nan((unsigned)vr[d][e]);
-            odd = __any(f != 0);
-        }
-        if (!odd) {
+                for (int e = 0; e < 4; ++e) f |= nan_bytes((unsigned)vr[d][e]);
+            // Zero times what is not a number is not zero: where a page with a masked place holds one, ones in its place count against
+            // ones for the places a row sees, the rows that see it lose that dimension, and zeros go through the product below.
+            if (__any(f != 0)) {
+                q8_halfx8 seen[RT];
 #pragma unroll
-            for (int d = 0; d < DT; ++d) {
-                const q8_halfx8 v = values8((unsigned)vr[d >> 1][(d & 1) * 2], (unsigned)vr[d >> 1][(d & 1) * 2 + 1]);
+                for (int t = 0; t < RT; ++t)
 #pragma unroll
-                for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], o[t][d], 0, 0, 0);
-            }
-        } else {
-            // one pass for each last visible position: its rows alone take the result, of values cut off behind it
-            for (int last = first; last < first + PAGE; ++last) {
+                    for (int e = 0; e < 8; ++e) seen[t][e] = there && first + 16 * (e >> 2) + 4 * g + (e & 3) <= lim[t] ? (_Float16)1.f : (_Float16)0.f;
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    const bool mine = min(lim[t], first + PAGE - 1) == last;
-                    if (!__any(mine)) continue;
+                for (int d = 0; d < DT; ++d) {
+                    const unsigned nl = nan_bytes((unsigned)vr[d >> 1][(d & 1) * 2]), nh = nan_bytes((unsigned)vr[d >> 1][(d & 1) * 2 + 1]);
+                    const q8_halfx8 ones = values8(nl & 0x38383838u, nh & 0x38383838u);   // 0x38: 1
+                    vr[d >> 1][(d & 1) * 2] &= (int)~nl;
+                    vr[d >> 1][(d & 1) * 2 + 1] &= (int)~nh;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const unsigned lo = upto((unsigned)vr[d >> 1][(d & 1) * 2], first + 4 * g, last);
-                        const unsigned hi = upto((unsigned)vr[d >> 1][(d & 1) * 2 + 1], first + 16 + 4 * g, last);
-                        const q8_floatx4 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(values8(lo, hi), p[t], zero, 0, 0, 0);
-                        if (mine) o[t][d] += r;
+                    for (int t = 0; t < RT; ++t) {
+                        const q8_floatx4 r = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, seen[t], zero, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[t][d][i] = r[i] > 0.f ? __uint_as_float(0x7fc00000u) : o[t][d][i];
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+            const q8_halfx8 v = values8((unsigned)vr[d >> 1][(d & 1) * 2], (unsigned)vr[d >> 1][(d & 1) * 2 + 1]);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) o[t][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[t], o[t][d], 0, 0, 0);
+            if (d & 1) __builtin_amdgcn_sched_barrier(0);
+        }
+        fetch_v(pg, next);
+    };
+    // This wavefront's next 64 pages, one a lane: their numbers and scales.  A page that is not there is read as page 0 and left out.
+    for (int first_blk = c0 + wave; first_blk < c1; first_blk += 64 * NW) {
+        const int blk = first_blk + lane * NW, n_mine = min(64, (c1 - first_blk + NW - 1) / NW);
+        int page = blk < c1 ? pages[blk] : -1;
+        const bool there = page >= 0 && page < a.c.n_pages;
+        page = there ? page : 0;
+        const float2 s2 = *reinterpret_cast<const float2*>(a.c.scales + ((size_t)page * hk + h) * 2);
+        const float ks = s2.x * a.scale, lv = there ? fmaxf(__log2f(s2.y), LOG2_VS_LEAST) : 0.f, inv = exp2f(-lv);
+        const int last = n_mine - 1;
+        auto number = [&](int i) { return __builtin_amdgcn_readlane(page, min(i, last)); };
+        auto of = [&](float f, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)); };
+        Page pg;
+        fetch_k(pg, number(0));
+        fetch_v(pg, number(0));
+        for (int i = 0; i <= last; ++i)
+            take(pg, first_blk + i * NW, __builtin_amdgcn_readlane((int)there, i), of(ks, i), of(lv, i), of(inv, i), number(i + 1));
     }
 
     // The wavefronts' results, 16 query rows at a time
@@ -378,7 +430,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
                 const unsigned y = q8_round_bf16(v[2] * f) | (unsigned)q8_round_bf16(v[3] * f) << 16;
                 *reinterpret_cast<uint2*>(dst) = make_uint2(x, y);
             } else {
-                const size_t pt = at * a.parts + blockIdx.x;
+                const size_t pt = at * a.parts + part;
                 *reinterpret_cast<q8_floatx4*>(a.part_o + pt * HD + dim) = v;
                 if (dim == 0) a.part_ml[pt] = make_float2(m, den);
             }
@@ -386,30 +438,45 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     }
 }
 
-// A wavefront joins the parts of one (row, head)
-template <int HD>
-__global__ void __launch_bounds__(64) join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, uint16_t* __restrict__ out, int parts,
-                                                  const int32_t* __restrict__ row0, int batch, int hq)
-{
-    const size_t at = blockIdx.x;
-    if ((int)(at / hq) >= row0[batch]) return;   // a row of no sequence
-    const float2* x = part_ml + at * parts;
-    float m = REF_NONE, den = 0.f, v[HD / 64];
-#pragma unroll
-    for (int i = 0; i < HD / 64; ++i) v[i] = 0.f;
-    for (int k = 0; k < parts; ++k) m = fmaxf(m, x[k].x);
-    for (int k = 0; k < parts; ++k) {
-        const float f = exp2f(x[k].x - m);
-        den = fmaf(x[k].y, f, den);
-#pragma unroll
-        for (int i = 0; i < HD / 64; ++i) v[i] = fmaf(part_o[(at * parts + k) * HD + i * 64 + threadIdx.x], f, v[i]);
-    }
-    const float f = den == 0.f ? 0.f : 1.f / den;
-#pragma unroll
-    for (int i = 0; i < HD / 64; ++i) out[at * HD + i * 64 + threadIdx.x] = q8_round_bf16(v[i] * f);
-}
-
 constexpr int MAX_PARTS = 64;
+
+// `per` (a power of two) groups of HD/4 threads join the parts of one (row, head): a thread has four dimensions of every per-th part.
+template <int HD>
+__global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, int parts, int per,
+                                                   size_t items, const int32_t* __restrict__ row0, int batch, int hq, uint16_t* __restrict__ out)
+{
+    constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
+    __shared__ float2 ml[GROUPS][MAX_PARTS];
+    __shared__ q8_floatx4 sums[GROUPS][LANES];
+    const int tid = threadIdx.x, grp = tid / LANES, dim = (tid % LANES) * 4, item = grp / per, sub = grp % per;
+    const size_t at = (size_t)blockIdx.x * (GROUPS / per) + item;
+    const bool on = at < items && (int)(at / hq) < row0[batch];   // else a row of no sequence
+    if (on)
+        for (int k = tid - item * per * LANES; k < parts; k += per * LANES) ml[item][k] = part_ml[at * parts + k];
+    __syncthreads();
+    q8_floatx4 o = {0.f, 0.f, 0.f, 0.f};
+    float den = 0.f;
+    if (on) {
+        float m = REF_NONE;
+        for (int k = 0; k < parts; ++k) m = fmaxf(m, ml[item][k].x);
+        for (int k = 0; k < parts; ++k) den = fmaf(ml[item][k].y, exp2f(ml[item][k].x - m), den);
+#pragma unroll 4
+        for (int k = sub; k < parts; k += per) {
+            const float2 x = ml[item][k];
+            const float f = exp2f(x.x - m);
+            const q8_floatx4 v = *reinterpret_cast<const q8_floatx4*>(part_o + (at * parts + k) * HD + dim);
+            o += x.y == 0.f ? (q8_floatx4){0.f, 0.f, 0.f, 0.f} : v * f;   // a part without a position has written nothing else
+        }
+    }
+    sums[grp][tid % LANES] = o;
+    __syncthreads();
+    if (!on || sub) return;
+    for (int i = 1; i < per; ++i) o += sums[grp + i][tid % LANES];
+    const float f = den == 0.f ? 0.f : 1.f / den;
+    const unsigned x = q8_round_bf16(o[0] * f) | (unsigned)q8_round_bf16(o[1] * f) << 16;
+    const unsigned y = q8_round_bf16(o[2] * f) | (unsigned)q8_round_bf16(o[3] * f) << 16;
+    *reinterpret_cast<uint2*>(out + at * HD + dim) = make_uint2(x, y);
+}
 
 int compute_units()
 {
@@ -424,25 +491,35 @@ int compute_units()
     return n;
 }
 
-template <int HD, int RT>
+template <int HD, int RT, int NW>
 void launch_attn(AttnArgs a, int batch, int max_window, int max_len, size_t ws_floats, void* ws, hipStream_t s)
 {
-    constexpr int NW = 4;
-    const int hk = a.c.n_kv_heads, hq = hk * a.group;
+    const int hk = a.c.n_kv_heads, hq = hk * a.group, cus = compute_units();
     a.tiles = (int)(((int64_t)max_window * a.group + 16 * RT - 1) / (16 * RT));
     const int64_t wgs = (int64_t)batch * hk * a.tiles, pages = (max_len + PAGE - 1) / PAGE;
     const size_t each = (size_t)a.rows * hq * (HD + 2);
-    int64_t parts = 2 * (int64_t)compute_units() / wgs;
-    parts = std::min(parts, (pages + NW - 1) / NW);
+    // Parts of a sequence are workgroups of their own, joined by a second kernel (3 us): where there are fewer workgroups than compute units,
+    // down to two pages a wavefront -- one sequence of 30000, 8 kv heads: 132 us in one part, 20 in 32; of 2048, 32 heads: 13.6 in one, 10.6
+    // in four; of 1024, 8 heads of 64: 6.7 in one, 8.4 in two -- and where sequences may differ by much (32 of 512 to 16384: 107 us in two
+    // parts, 115 in one, 120 in four).
+    int64_t parts = (pages + 128) / 256;
+    if (wgs < cus && pages * HD > 32 * 128) parts = std::max(parts, std::min((cus + wgs - 1) / wgs, pages / (2 * NW)));
     parts = std::min(parts, (int64_t)std::min<size_t>(MAX_PARTS, ws_floats / each));
     a.parts = (int)std::max<int64_t>(parts, 1);
+    a.part_pages = (int)std::max<int64_t>((pages + a.parts - 1) / a.parts, 1);
     if (a.parts > 1) {
         a.part_o = (float*)ws;
         a.part_ml = (float2*)(a.part_o + (size_t)a.rows * hq * a.parts * HD);
     }
-    hipLaunchKernelGGL((attn8_kernel<HD, RT, NW>), dim3(a.parts, hk * a.tiles, batch), dim3(64 * NW), 0, s, a);
-    if (a.parts > 1)
-        hipLaunchKernelGGL((join_kernel<HD>), dim3((unsigned)a.rows * hq), dim3(64), 0, s, a.part_o, a.part_ml, a.out, a.parts, a.row0, batch, hq);
+    hipLaunchKernelGGL((attn8_kernel<HD, RT, NW>), dim3(hk * a.tiles, a.parts, batch), dim3(64 * NW), 0, s, a);
+    if (a.parts > 1) {
+        const int groups = 256 / (HD / 4);
+        int per = 1;
+        while (per < a.parts && per < groups) per *= 2;
+        const size_t items = (size_t)a.rows * hq;
+        hipLaunchKernelGGL((join_kernel<HD>), dim3((unsigned)((items * per + groups - 1) / groups)), dim3(256), 0, s, a.part_o, a.part_ml, a.parts, per,
+                           items, a.row0, batch, hq, a.out);
+    }
 }
 
 int check_cache(const char* name, const spec_kv8_cache* c, int n_q_heads, const int32_t* row0, const int32_t* kv_len, int rows, int max_window)
@@ -478,15 +555,19 @@ extern "C" int spec_kv8_append(const spec_kv8_cache* cache, const void* qkv, int
     if (!rows || !max_window) return SPEC_OK;
     if (!qkv || (cos_sin && !q_out)) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_append: null pointer");
     if (cos_sin && max_pos <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_append: a rotation of %d positions", max_pos);
-    const dim3 grid((max_window + PAGE - 2) / PAGE + 1, cache->n_kv_heads, cache->batch);
-    const int group = n_q_heads / cache->n_kv_heads;
+    const int group = n_q_heads / cache->n_kv_heads, pages = (max_window + PAGE - 2) / PAGE + 1;
+    const int at_once = APPEND_TPB / (cache->head_dim / 16);
+    const int64_t queries = q_out ? ((int64_t)max_window * group + at_once - 1) / at_once : 0;
+    if (queries + pages > 0x7fffffff) return fail(SPEC_ERR_SHAPE, "spec_kv8_append: a window of %d rows", max_window);
+    if (((uintptr_t)q_out | (uintptr_t)qkv) & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_append: qkv and q_out have to be 16-byte aligned");
+    const dim3 grid((unsigned)(pages + queries), cache->n_kv_heads, cache->batch);
     hipStream_t s = (hipStream_t)stream;
     if (cache->head_dim == 64)
-        hipLaunchKernelGGL((append_kernel<64>), grid, dim3(APPEND_TPB), 0, s, (const uint16_t*)qkv, row0, kv_len, pages_of(cache),
-                           (const float2*)cos_sin, max_pos, rows, group, (uint16_t*)q_out);
+        hipLaunchKernelGGL((append_kernel<64>), grid, dim3(APPEND_TPB), 0, s, (const uint16_t*)qkv, row0, kv_len, (const float2*)cos_sin,
+                           pages, max_pos, rows, group, (uint16_t*)q_out, pages_of(cache));
     else
-        hipLaunchKernelGGL((append_kernel<128>), grid, dim3(APPEND_TPB), 0, s, (const uint16_t*)qkv, row0, kv_len, pages_of(cache),
-                           (const float2*)cos_sin, max_pos, rows, group, (uint16_t*)q_out);
+        hipLaunchKernelGGL((append_kernel<128>), grid, dim3(APPEND_TPB), 0, s, (const uint16_t*)qkv, row0, kv_len, (const float2*)cos_sin,
+                           pages, max_pos, rows, group, (uint16_t*)q_out, pages_of(cache));
     SPECV_LAUNCH_CHECK("append_kernel");
     return SPEC_OK;
 }
@@ -513,23 +594,24 @@ extern "C" int spec_kv8_attention(const spec_kv8_cache* cache, const void* q, in
     if (!(scale > -INFINITY && scale < INFINITY)) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_attention: scale %g", (double)scale);
     const int cap = cache->blocks_per_seq * PAGE;
     const int group = n_q_heads / cache->n_kv_heads;
-    if ((int64_t)cache->n_kv_heads * (((int64_t)max_window * group + 15) / 16) > 65535 || (int64_t)rows * n_q_heads > 0x7fffffff)
+    if ((int64_t)cache->n_kv_heads * (((int64_t)max_window * group + 15) / 16) > 0x7fffffff || (int64_t)rows * n_q_heads > 0x7fffffff)
         return fail(SPEC_ERR_SHAPE, "spec_kv8_attention: %d rows of %d heads are too many", rows, n_q_heads);
-    AttnArgs a{pages_of(cache), (const uint16_t*)q, ld_q, row0, kv_len, rows, group, 1, 1, scale * 1.4426950408889634f, (uint16_t*)out, nullptr, nullptr};
+    AttnArgs a{pages_of(cache), (const uint16_t*)q, ld_q, row0, kv_len, rows, group, 1, 1, 1, scale * 1.4426950408889634f, (uint16_t*)out, nullptr, nullptr};
     const size_t ws = workspace ? workspace_bytes / sizeof(float) : 0;
     const int len = max_len ? std::min(max_len, cap) : cap;
-    const int n_q = (int)std::min<int64_t>((int64_t)max_window * group, 1 << 20);
+    const int64_t n_q = (int64_t)max_window * group;
     hipStream_t s = (hipStream_t)stream;
-#define SPECV_ATTN(HD)                                                                       \
-    if (n_q <= 16) launch_attn<HD, 1>(a, cache->batch, max_window, len, ws, workspace, s);   \
-    else if (n_q <= 32) launch_attn<HD, 2>(a, cache->batch, max_window, len, ws, workspace, s); \
-    else launch_attn<HD, 4>(a, cache->batch, max_window, len, ws, workspace, s)
+    // Two tiles of 16 query rows a workgroup, which share each page's loads and conversions, once there are workgroups enough without: 32
+    // sequences of 512 to 16384 with up to 32 rows per kv head take 107 us, 157 with one tile; 8 of 4096 with 64 rows 25.7 and 23.5.
+    // (Four tiles leave one wavefront on a SIMD: 195 and 30.3.)
+    const bool two = n_q > 16 && (int64_t)cache->batch * cache->n_kv_heads * ((n_q + 15) / 16) > compute_units();
     if (cache->head_dim == 64) {
-        SPECV_ATTN(64);
+        if (two) launch_attn<64, 2, 8>(a, cache->batch, max_window, len, ws, workspace, s);
+        else launch_attn<64, 1, 8>(a, cache->batch, max_window, len, ws, workspace, s);
     } else {
-        SPECV_ATTN(128);
+        if (two) launch_attn<128, 2, 8>(a, cache->batch, max_window, len, ws, workspace, s);
+        else launch_attn<128, 1, 8>(a, cache->batch, max_window, len, ws, workspace, s);
     }
-#undef SPECV_ATTN
     SPECV_LAUNCH_CHECK("attn8_kernel");
     return SPEC_OK;
 }

@@ -59,7 +59,21 @@ __device__ __forceinline__ uint16_t q8_round_bf16(float f)
     return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
-// 16 bytes (4 with DWORD) per lane straight into LDS, to lds + 16 (4) * lane.  The compiler does not know of the request: wait_fetches.
+// The largest of a wavefront's, the same for all lanes (by DPP)
+__device__ __forceinline__ unsigned q8_wave_max(unsigned v)
+{
+#define Q8_STEP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, ROWS, 0xf, false))
+    Q8_STEP(0xb1, 0xf);    // neighbours, pairs, halves of a row of sixteen, rows
+    Q8_STEP(0x4e, 0xf);
+    Q8_STEP(0x141, 0xf);
+    Q8_STEP(0x140, 0xf);
+    Q8_STEP(0x142, 0xa);
+    Q8_STEP(0x143, 0xc);
+#undef Q8_STEP
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+// 16 bytes (4) per lane straight into LDS, to lds + 16 (4) * lane.  The compiler does not know of the request: wait_fetches.
 // (m0 is none of the registers that the compiler hands out, about which it warns; it may set m0 for an instruction of its own.)
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
