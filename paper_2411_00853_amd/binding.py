@@ -447,29 +447,24 @@ def spec_decode_get_view(d: Decoder) -> spec_decode_view:
 
 
 # ---- 8-bit operators and filtered draws (include/spec_q8.h) ---------------------------------------
+# Types, shapes and strides are checked where the tensors are read: csrc/native.cpp.  A wrong one raises ValueError, a status
+# other than SPEC_OK raises SpecError.
 
 _F8 = torch.float8_e4m3fn
-_DTYPES = {torch.float32: SPEC_DTYPE_FP32, torch.bfloat16: SPEC_DTYPE_BF16}
+_native_module = None
 
 
-def _dtype(t: torch.Tensor) -> int:
-    code = _DTYPES.get(t.dtype)
-    if code is None:
-        raise ValueError(f"expected float32 or bfloat16, got {t.dtype}")
-    return code
-
-
-def _rows_ptr(t: torch.Tensor, cols: int) -> int:
-    """Device pointer of a [rows][cols] tensor whose rows are contiguous and any distance apart."""
-    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols or (t.stride(1) != 1 and cols > 1):
-        raise ValueError(f"expected a device tensor of rows of {cols} contiguous elements")
-    return t.data_ptr()
-
-
-def _expect(t: Optional[torch.Tensor], shape) -> Optional[torch.Tensor]:
-    if t is not None and t.shape != shape:
-        raise ValueError(f"expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+def _native():
+    global _native_module
+    if _native_module is None:
+        L = lib()
+        if not os.path.exists(_build.NATIVE):
+            _build.build_library()
+        from . import _native as m
+        m.bind(*(C.cast(f, C.c_void_p).value for f in (L.spec_q8_quantize, L.spec_q8_add_rmsnorm, L.spec_q8_swiglu, L.spec_q8_gemm,
+                                                       L.spec_kv8_append, L.spec_kv8_attention, L.spec_filter_sample)))
+        _native_module = m
+    return _native_module
 
 
 def _raw_stream(stream) -> Optional[int]:
@@ -479,22 +474,17 @@ def _raw_stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
-def _q8_out(rows: int, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor], device):
-    kp = (cols + 127) // 128 * 128
-    if q is None:
-        q = torch.empty((rows, kp), dtype=_F8, device=device)
-    if scales is None:
-        scales = torch.empty((kp // 128, rows), dtype=torch.float32, device=device)
-    return _expect(q, (rows, kp)), _expect(scales, (kp // 128, rows))
+def _q8_out(x: torch.Tensor, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor]):
+    rows, kp = x.shape[0], (cols + 127) // 128 * 128
+    return (torch.empty((rows, kp), dtype=_F8, device=x.device) if q is None else q,
+            torch.empty((kp // 128, rows), dtype=torch.float32, device=x.device) if scales is None else scales)
 
 
 def spec_q8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """Rows of x [rows][cols] (any row stride) -> (q e4m3 [rows][Kp], scales fp32 [Kp/128][rows])."""
-    rows, cols = x.shape
-    q, scales = _q8_out(rows, cols, q, scales, x.device)
-    ld = x.stride(0) if rows > 1 else cols
-    _check(lib().spec_q8_quantize(_rows_ptr(x, cols), _dtype(x), ld, rows, cols, _ptr(q, _F8),
-                                  _ptr(scales, torch.float32), _raw_stream(stream)))
+    if q is None or scales is None:
+        q, scales = _q8_out(x, x.shape[1], q, scales)
+    _check(_native().quantize(x, q, scales, _raw_stream(stream)))
     return q, scales
 
 
@@ -502,23 +492,17 @@ def spec_q8_add_rmsnorm(x: torch.Tensor, delta: Optional[torch.Tensor], gain: to
                         x_out: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
                         scales: Optional[torch.Tensor] = None, stream=None):
     """x + delta -> x_out (may be x; None: not kept); its RMSNorm times gain -> (q, scales)."""
-    rows, cols = x.shape
-    q, scales = _q8_out(rows, cols, q, scales, x.device)
-    _check(lib().spec_q8_add_rmsnorm(_ptr(x), _dtype(x), _ptr(_expect(delta, x.shape)), 0 if delta is None else _dtype(delta),
-                                     _ptr(_expect(gain, (cols,)), torch.float32), float(eps), rows, cols,
-                                     _ptr(_expect(x_out, x.shape), x.dtype), _ptr(q, _F8), _ptr(scales, torch.float32),
-                                     _raw_stream(stream)))
+    if q is None or scales is None:
+        q, scales = _q8_out(x, x.shape[1], q, scales)
+    _check(_native().add_rmsnorm(x, delta, gain, eps, x_out, q, scales, _raw_stream(stream)))
     return q, scales
 
 
 def spec_q8_swiglu(gate_up: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """silu(gate) * up of [rows][gate columns | up columns] -> (q, scales)."""
-    rows, cols = gate_up.shape
-    if cols % 2:
-        raise ValueError("gate_up needs as many up columns as gate columns")
-    q, scales = _q8_out(rows, cols // 2, q, scales, gate_up.device)
-    _check(lib().spec_q8_swiglu(_ptr(gate_up), _dtype(gate_up), rows, cols // 2, _ptr(q, _F8), _ptr(scales, torch.float32),
-                                _raw_stream(stream)))
+    if q is None or scales is None:
+        q, scales = _q8_out(gate_up, gate_up.shape[1] // 2, q, scales)
+    _check(_native().swiglu(gate_up, q, scales, _raw_stream(stream)))
     return q, scales
 
 
@@ -537,41 +521,24 @@ def spec_q8_pack_weight(src: torch.Tensor, stream=None) -> torch.Tensor:
 def spec_q8_gemm(q: torch.Tensor, scales: torch.Tensor, w_packed: torch.Tensor, w_scales: torch.Tensor, y: torch.Tensor, stream=None):
     """y [M][N] (float32 or bfloat16) = rows (q [M][Kp], scales [Kp/128][M]) times the packed matrix, w_scales
     [ceil(N/128)][Kp/128]."""
-    M, kp = q.shape
-    N = y.shape[1]
-    _expect(y, (M, N)), _expect(scales, (kp // 128, M)), _expect(w_scales, ((N + 127) // 128, kp // 128))
-    if w_packed.numel() != (N + 15) // 16 * 16 * kp or kp % 128:
-        raise ValueError(f"expected a packed matrix of {N} x {kp}")
-    _check(lib().spec_q8_gemm(_ptr(q, _F8), _ptr(scales, torch.float32), _ptr(w_packed, _F8), _ptr(w_scales, torch.float32), _ptr(y),
-                              _dtype(y), M, N, kp, _raw_stream(stream)))
+    _check(_native().gemm(q, scales, w_packed, w_scales, y, _raw_stream(stream)))
     return y
 
 
 class Kv8Cache:
     """One layer's 8-bit cache: data e4m3 [pages][kv heads][2][32 * head_dim], scales fp32 [pages][kv heads][2],
-    table int32 [batch][blocks].  Holds the tensors it points into."""
+    table int32 [batch][blocks]."""
+    __slots__ = ("data", "scales", "table", "head_dim")
 
     def __init__(self, data: torch.Tensor, scales: torch.Tensor, table: torch.Tensor, head_dim: int):
-        pages, heads = data.shape[0], data.shape[1]
-        _expect(data, (pages, heads, 2, 32 * head_dim)), _expect(scales, (pages, heads, 2))
-        self.data, self.scales, self.table = data, scales, table
-        self.c = spec_kv8_cache(_ptr(data, _F8), _ptr(scales, torch.float32), _ptr(table, torch.int32), pages, heads, head_dim,
-                                table.shape[0], table.shape[1])
+        self.data, self.scales, self.table, self.head_dim = data, scales, table, head_dim
 
 
 def spec_kv8_append(cache: Kv8Cache, qkv: torch.Tensor, row0: torch.Tensor, kv_len: torch.Tensor, n_q_heads: int, max_window: int,
                     cos_sin: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, stream=None):
     """The keys and values of qkv bf16 [rows][(q + 2 kv heads) * head_dim] -> the cache; rotated queries -> q_out."""
-    c = cache.c
-    rows = qkv.shape[0]
-    _expect(qkv, (rows, (n_q_heads + 2 * c.n_kv_heads) * c.head_dim)), _expect(row0, (c.batch + 1,)), _expect(kv_len, (c.batch,))
-    _expect(q_out, (rows, n_q_heads * c.head_dim))
-    max_pos = 0
-    if cos_sin is not None:
-        max_pos = cos_sin.shape[0]
-        _expect(cos_sin, (max_pos, c.head_dim // 2, 2))
-    _check(lib().spec_kv8_append(C.byref(c), _ptr(qkv, torch.bfloat16), n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
-                                 rows, max_window, _ptr(cos_sin, torch.float32), max_pos, _ptr(q_out, torch.bfloat16), _raw_stream(stream)))
+    _check(_native().append(cache.data, cache.scales, cache.table, cache.head_dim, qkv, row0, kv_len, n_q_heads, max_window, cos_sin,
+                            q_out, _raw_stream(stream)))
 
 
 def spec_kv8_workspace_bytes(rows: int, n_q_heads: int, head_dim: int) -> int:
@@ -581,16 +548,8 @@ def spec_kv8_workspace_bytes(rows: int, n_q_heads: int, head_dim: int) -> int:
 def spec_kv8_attention(cache: Kv8Cache, q: torch.Tensor, row0: torch.Tensor, kv_len: torch.Tensor, n_q_heads: int, max_window: int,
                        max_len: int, scale: float, out: torch.Tensor, workspace: Optional[torch.Tensor] = None, stream=None):
     """out bf16 [rows][n_q_heads * head_dim]; q: bf16 rows of as many elements, any multiple of 8 apart."""
-    c = cache.c
-    rows, cols = out.shape
-    _expect(out, (rows, n_q_heads * c.head_dim)), _expect(q, out.shape), _expect(row0, (c.batch + 1,)), _expect(kv_len, (c.batch,))
-    if q.dtype != torch.bfloat16:
-        raise ValueError(f"expected dtype {torch.bfloat16}, got {q.dtype}")
-    ld = q.stride(0) if rows > 1 else cols
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().spec_kv8_attention(C.byref(c), _rows_ptr(q, cols), ld, n_q_heads, _ptr(row0, torch.int32), _ptr(kv_len, torch.int32),
-                                    rows, max_window, max_len, scale, _ptr(out, torch.bfloat16), _ptr(workspace), nbytes,
-                                    _raw_stream(stream)))
+    _check(_native().attention(cache.data, cache.scales, cache.table, cache.head_dim, q, row0, kv_len, n_q_heads, max_window, max_len,
+                               scale, out, workspace, _raw_stream(stream)))
     return out
 
 
@@ -604,17 +563,8 @@ def spec_filter_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature
                        logits_out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """One draw per row of logits [rows][vocab] (float32 or bfloat16, any row stride); per-row parameters are device
     tensors, None switches a filter off.  logits_out fp32: the logits, -inf where not kept."""
-    rows, vocab = logits.shape
-    for t in (uniforms, temperature, tokens, top_k, top_p, min_p, logprob, n_kept):
-        _expect(t, (rows,))
-    _expect(logits_out, (rows, vocab))
-    ld = logits.stride(0) if rows > 1 else vocab
-    f = torch.float32
-    args = spec_filter_args(_rows_ptr(logits, vocab), _dtype(logits), rows, vocab, ld, _ptr(uniforms, f), _ptr(temperature, f),
-                            _ptr(top_k, torch.int32), _ptr(top_p, f), _ptr(min_p, f))
-    out = spec_filter_out(_ptr(tokens, torch.int32), _ptr(logprob, f), _ptr(n_kept, torch.int32), _ptr(logits_out, f))
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().spec_filter_sample(C.byref(args), C.byref(out), _ptr(workspace), nbytes, _raw_stream(stream)))
+    _check(_native().sample(logits, uniforms, temperature, tokens, top_k, top_p, min_p, logprob, n_kept, logits_out, workspace,
+                            _raw_stream(stream)))
     return tokens
 
 

@@ -1,4 +1,5 @@
-"""Builds libspecverify.so (HIP, gfx950) in-tree with hipcc."""
+"""Builds libspecverify.so (HIP, gfx950) in-tree with hipcc, and _native.so, the marshalling of tensors for its shortest
+calls, with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -9,6 +10,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecverify.so")
+NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["attention.hip", "attention_reuse.hip", "spec_verify.hip", "forward.hip", "sampler.hip", "gemm.hip",
            "elementwise.hip", "probe.hip", "decode.hip", "lookahead.hip", "q8_rows.hip", "q8_gemm.hip", "kv8.hip",
            "filter_sample.hip"]
@@ -35,10 +37,22 @@ def _hipcc() -> str:
     raise RuntimeError("hipcc not found: cannot build libspecverify.so")
 
 
+def _native_command() -> list:
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    cxx = shutil.which("g++") or shutil.which("c++") or "g++"
+    return [cxx, "-std=c++17", "-O2", "-shared", "-fPIC", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__=1",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{base}/include",
+            f"-I{base}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", "-o", NATIVE,
+            os.path.join(CSRC, "native.cpp"), f"-L{base}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
 def sources_newer_than_lib() -> bool:
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(NATIVE):
         return True
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(NATIVE))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
            [os.path.join(HERE, "..", "include", f) for f in os.listdir(os.path.join(HERE, "..", "include"))]
     return any(os.path.getmtime(d) > t for d in deps)
@@ -60,12 +74,16 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         cmd = [hipcc] + FLAGS + SOURCE_FLAGS.get(src, []) + ["-c", "-o", obj, os.path.join(CSRC, src)]
         return obj, subprocess.run(cmd, capture_output=True, text=True)
 
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as pool:   # one hipcc process per source
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as pool:   # one compiler process per source
+        native = pool.submit(subprocess.run, _native_command(), capture_output=True, text=True)
         done = list(pool.map(compile_one, SOURCES))
     for _, r in done:
         report(r)
+    report(native.result())
     if any(r.returncode for _, r in done):
         raise RuntimeError("hipcc failed building libspecverify.so")
+    if native.result().returncode:
+        raise RuntimeError("the host compiler failed building _native.so")
     r = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [o for o, _ in done],
                        capture_output=True, text=True)
     report(r)

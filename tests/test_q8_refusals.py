@@ -145,3 +145,23 @@ def test_the_binding_mirrors_the_structs(tmp_path):
         c = getattr(sv, n)
         want += [C.sizeof(c)] + [getattr(c, f).offset for f, _ in c._fields_]
     assert got == want
+
+
+def test_tensors_that_are_not_on_the_device():
+    """The binding reads no address of a host tensor."""
+    import torch
+    x, q, s = torch.zeros(2, 128), torch.zeros((2, 128), dtype=torch.uint8).view(torch.float8_e4m3fn), torch.zeros(1, 2)
+    i, b = torch.zeros(3, dtype=torch.int32), torch.zeros((2, 256), dtype=torch.bfloat16)
+    sv._raw_stream, keep = (lambda stream: None), sv._raw_stream
+    try:
+        cache = sv.Kv8Cache(q, s, i, 64)
+        for call in (lambda: sv.spec_q8_quantize(x, q, s), lambda: sv.spec_q8_add_rmsnorm(x, None, s, 1e-5, None, q, s),
+                     lambda: sv.spec_q8_swiglu(x, q, s), lambda: sv.spec_q8_gemm(q, s, q, s, x),
+                     lambda: sv.spec_kv8_append(cache, b, i, i, 4, 1), lambda: sv.spec_kv8_attention(cache, b, i, i, 4, 1, 0, 1.0, b),
+                     lambda: sv.spec_filter_sample(x, s, None, i)):
+            with pytest.raises(ValueError, match="device tensor"):
+                call()
+        with pytest.raises(ValueError, match="expected a tensor"):
+            sv.spec_filter_sample([1.0], s, None, i)
+    finally:
+        sv._raw_stream = keep
