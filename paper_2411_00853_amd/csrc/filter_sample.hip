@@ -13,6 +13,7 @@ constexpr int TPB = 1024, WAVES = TPB / 64;
 constexpr int BINS = 4096;      // of falling logits, over the 31 nats in which a token has mass
 constexpr int LIST = 2048;      // tokens that may matter, where that few are known to
 constexpr int SMALL = 1024;     // tokens of the bin that a cut falls into
+constexpr int SHORT = 256;      // tokens of a list that is put in order at once
 constexpr float NATS = 31.f;    // exp(-31) * 2^44 < 1
 constexpr float HALF_ONE = 0x1p22f;
 constexpr u64 MASS_ONE = 1ull << 44;
@@ -89,6 +90,8 @@ struct Lds {
     float sx[SMALL];
     int sid[SMALL];
     u64 sv[SMALL];
+    unsigned count[TPB];
+    u64 order[SHORT], ranked[SHORT], by_id[SHORT];
     Sums wave[WAVES];
     unsigned tops[WAVES];
     int n_list, n_small, bin;
@@ -112,72 +115,72 @@ struct Masses {
 };
 
 // ---- where tokens come from: registers, memory or the list in LDS ----------------------------------------------------------
-template <typename T>
-struct Vec;   // elements of a lane's load
-template <>
-struct Vec<float> {
-    static constexpr int N = 4;
-};
-template <>
-struct Vec<uint16_t> {
-    static constexpr int N = 8;
-};
-template <typename T>
+template <typename T, int N>
 struct __attribute__((packed, aligned(sizeof(T)))) Some {
-    T v[Vec<T>::N];
+    T v[N];
 };
 
-// A wavefront's load covers CHUNK consecutive ids; chunk c is wavefront c % WAVES's.  NV loads of a thread stay in registers, with NV = 0
-// every pass reads the row again.
-template <typename T, int NV>
+// A thread's load is N logits (vocab >= N), a wavefront's covers CHUNK consecutive ids; chunk c is wavefront c % WAVES's.  NV loads of a
+// thread stay in registers, with NV = 0 every pass reads the row again.
+template <typename T, int NV, int PER>
 struct Row {
-    static constexpr int N = Vec<T>::N, CHUNK = 64 * N;
+    static constexpr int N = PER, CHUNK = 64 * N;
     const T* x;
     int vocab;
     float v[NV ? NV : 1][N];
 
-    __device__ __forceinline__ void fetch(int k, float* to) const
+    // Load k of this thread.  It is never branched around, or every load would be waited for before the next: where less than a load is left
+    // it covers the row's last N logits, and those that are another load's become -inf.
+    __device__ __forceinline__ int first_id(int k) const { return min((k * TPB + (int)threadIdx.x) * N, vocab - N); }
+    __device__ __forceinline__ Some<T, N> fetch(int k) const { return *reinterpret_cast<const Some<T, N>*>(x + first_id(k)); }
+    __device__ __forceinline__ void widen(int k, const Some<T, N>& s, float* to) const
     {
-        const int i = (k * TPB + (int)threadIdx.x) * N;
-        if (i + N <= vocab) {
-            const Some<T> s = *reinterpret_cast<const Some<T>*>(x + i);
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), want = (k * TPB + (int)threadIdx.x) * N, i = first_id(k);
 #pragma unroll
-            for (int e = 0; e < N; ++e) to[e] = q8_widen(s.v[e]);
-        } else {
+        for (int e = 0; e < N; ++e) to[e] = q8_widen(s.v[e]);
+        if ((k * WAVES + wave + 1) * CHUNK > vocab) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) to[e] = i + e < vocab ? q8_widen(x[i + e]) : -INFINITY;
+            for (int e = 0; e < N; ++e) to[e] = i + e >= want ? to[e] : -INFINITY;
         }
     }
     __device__ __forceinline__ void load()
     {
+        Some<T, N> s[NV ? NV : 1];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) fetch(k, v[k]);
+        for (int k = 0; k < NV; ++k) s[k] = fetch(k);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) widen(k, s[k], v[k]);
     }
-    // f(chunk, id of the first, N logits): whole wavefronts
+    // f(chunk, id of the first, N logits): whole wavefronts.  A logit of -inf may stand for one that is not there.
     template <typename F>
     __device__ __forceinline__ void each_vec(F f) const
     {
-        const int wave = threadIdx.x >> 6;
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         if constexpr (NV > 0) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                f(k * WAVES + wave, (k * TPB + (int)threadIdx.x) * N, v[k]);
+                f(k * WAVES + wave, first_id(k), v[k]);
                 __builtin_amdgcn_sched_barrier(0);   // one load's masses at a time: side by side they do not fit the registers
             }
         } else {
-            constexpr int AHEAD = 16 / N;
+            constexpr int AHEAD = N >= 4 ? 32 / N : 8;
             const int n = (vocab + TPB * N - 1) / (TPB * N);
             for (int k = 0; k < n; k += AHEAD) {
-                float l[AHEAD][N];
+                Some<T, N> s[AHEAD];
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) fetch(k + j, l[j]);
+                for (int j = 0; j < AHEAD; ++j) s[j] = fetch(k + j);
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) f((k + j) * WAVES + wave, ((k + j) * TPB + (int)threadIdx.x) * N, l[j]);
+                for (int j = 0; j < AHEAD; ++j) {
+                    float l[N];
+                    widen(k + j, s[j], l);
+                    f((k + j) * WAVES + wave, first_id(k + j), l);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
         }
     }
     template <typename F>
-    __device__ __forceinline__ void each(F f) const   // f(logit, id); ids beyond the vocabulary come with -inf
+    __device__ __forceinline__ void each(F f) const   // f(logit, id)
     {
         each_vec([&](int, int i, const float* l) {
 #pragma unroll
@@ -364,12 +367,33 @@ __device__ bool cuts(const S& src, const Masses& m, const Params& a, Cut& c, int
     return true;
 }
 
+// The row with -inf where `kept` says no
+template <typename T, int NV, int N, typename F>
+__device__ __forceinline__ void write_row(const Row<T, NV, N>& r, float* out, F kept)
+{
+    if (!out) return;
+    r.each_vec([&](int chunk, int i0, const float* l) {
+        const int want = (chunk * 64 + (int)(threadIdx.x & 63)) * N;
+        if (want >= r.vocab) return;
+        if (want + N <= r.vocab) {
+            Some<float, N> a;
+#pragma unroll
+            for (int e = 0; e < N; ++e) a.v[e] = l[e] > -INFINITY && kept(l[e], i0 + e) ? l[e] : -INFINITY;
+            *reinterpret_cast<Some<float, N>*>(out + i0) = a;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (i0 + e >= want && i0 + e < r.vocab) out[i0 + e] = l[e] > -INFINITY && kept(l[e], i0 + e) ? l[e] : -INFINITY;
+    });
+}
+
 // The draw among the tokens of a cut, and the results.  `list` holds all of them, or is NULL.
-template <typename T, int NV>
-__device__ __forceinline__ void finish(const Row<T, NV>& r, const List* list, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
+template <typename T, int NV, int N>
+__device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List* list, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
                                        Lds& s)
 {
-    constexpr int N = Row<T, NV>::N, CHUNK = Row<T, NV>::CHUNK;
+    constexpr int CHUNK = Row<T, NV, N>::CHUNK;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     clear(s, 1024);   // the kept masses by chunk of ids
     u64 n = 0;
@@ -403,7 +427,7 @@ __device__ __forceinline__ void finish(const Row<T, NV>& r, const List* list, co
     crossing(s, 1024, target + 1);
     if (wave == 0) {
         u64 w[N], sum = 0;
-        const int i0 = s.bin * CHUNK + lane * N;
+        const int i0 = s.bin * CHUNK + lane * N;   // (in the order of the ids, also where a load was moved)
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float l = i0 + e < r.vocab ? q8_widen(r.x[i0 + e]) : -INFINITY;
@@ -430,17 +454,94 @@ __device__ __forceinline__ void finish(const Row<T, NV>& r, const List* list, co
             if (o.n_kept) *o.n_kept = (int)kept.n;
         }
     }
-    if (o.out)
-        r.each([&](float l, int i) {
-            if (i < r.vocab) o.out[i] = c.has(l, i) && m(l) >= a.least ? l : -INFINITY;
-        });
+    write_row(r, o.out, [&](float l, int i) { return c.has(l, i) && m(l) >= a.least; });
+}
+
+// Up to SHORT tokens that hold everything kept: each finds its place in the order of the logits and of the ids by looking at all
+// others, and everything else is two running sums.  Four wavefronts work, one a SIMD; the rest meet them at the barriers.
+template <typename T, int NV, int N>
+__device__ __forceinline__ void short_list(const Row<T, NV, N>& r, const Masses& m, const Params& a, float u, const Results& o, Lds& s)
+{
+    const int n = s.n_list, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const bool works = wave < SHORT / 64, on = tid < n;
+    u64* scan = s.hist;   // sums of the wavefronts
+    auto running = [&](u64 v, int slot) {   // inclusive, over the SHORT threads (one barrier)
+        u64 t = 0;
+        if (works) {
+            t = wave_scan(v);
+            if (lane == 63) scan[slot * (SHORT / 64) + wave] = t;
+        }
+        __syncthreads();
+        if (works)
+            for (int w = 0; w < wave; ++w) t += scan[slot * (SHORT / 64) + w];
+        return t;
+    };
+    auto total = [&](int slot) {
+        u64 t = 0;
+        for (int w = 0; w < SHORT / 64; ++w) t += scan[slot * (SHORT / 64) + w];
+        return t;
+    };
+    float l = -INFINITY;
+    int id = 0, rank = 0, place = 0;
+    u64 mass = 0, mine = 0;
+    if (works) {
+        if (on) {
+            l = s.lx[tid];
+            id = s.lid[tid];
+            mass = m(l);
+            mine = (u64)key_of(l) << 32 | (unsigned)~id;   // larger: ranked before
+        }
+        s.order[tid] = mine;   // (behind the list: 0, which no comparison counts)
+    }
+    __syncthreads();
+    if (works) {
+        for (int j = 0; j < n; j += 4)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const u64 other = s.order[j + e];
+                rank += other > mine;
+                place += (unsigned)other > (unsigned)mine;
+            }
+        if (on) s.ranked[rank] = mass;
+        else s.ranked[tid] = 0;
+    }
+    __syncthreads();
+    const bool masses = a.p < 1.f;
+    const u64 sorted = works ? s.ranked[tid] : 0;   // of rank tid
+    const bool in_k = a.k <= 0 || tid < a.k;
+    const u64 upto = running(in_k ? sorted : 0, 0);
+    const u64 need = masses ? share(a.p, total(0)) : 0;
+    const bool keep = works && in_k && sorted >= a.least && (!masses || upto - sorted < need);
+    __syncthreads();
+    if (works) {
+        s.ranked[tid] = keep ? sorted : 0;
+        s.by_id[tid] = 0;
+    }
+    __syncthreads();
+    u64 kept = on ? s.ranked[rank] : 0;
+    if (on) s.by_id[place] = kept;
+    running(works ? (u64)(kept > 0) : 0, 1);
+    const u64 mass_here = works ? s.by_id[tid] : 0, end = running(mass_here, 2), all = total(2);
+    const u64 target = min((u64)((double)u * (double)all), all - 1);
+    if (works && end - mass_here <= target && end > target) s.bin = tid;   // the place of the token drawn
+    __syncthreads();
+    if (on && place == s.bin) {
+        *o.token = id;
+        if (o.logprob) *o.logprob = (float)log((double)mass / (double)all);
+        if (o.n_kept) *o.n_kept = (int)total(1);
+    }
+    if (!o.out) return;
+    write_row(r, o.out, [&](float, int) { return false; });
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // another wavefront's -inf is not to land on a kept logit
+    __syncthreads();
+    if (on && kept) o.out[id] = l;
 }
 
 // A row with more equal logits than a bin's list takes
-template <typename T>
+template <typename T, int N>
 __device__ __forceinline__ void slow_row(const T* x, int vocab, const Masses& m, const Params& a, float u, const Results& o, Lds& s)
 {
-    const Row<T, 0> r = {x, vocab, {}};
+    const Row<T, 0, N> r = {x, vocab, {}};
     Cut c = {0, vocab - 1};
     Sums all = within(r, m, c, s);
     if (a.k > 0 && (u64)a.k < all.n) {
@@ -448,10 +549,10 @@ __device__ __forceinline__ void slow_row(const T* x, int vocab, const Masses& m,
         all = within(r, m, c, s);
     }
     if (a.p < 1.f) c = bisect(r, m, c, share(a.p, all.mass), true, vocab, s);
-    finish<T, 0>(r, nullptr, m, a, c, u, o, s);
+    finish(r, (const List*)nullptr, m, a, c, u, o, s);
 }
 
-template <typename T, int NV>
+template <typename T, int NV, int N>
 __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ uniforms,
                                                      const float* __restrict__ temperature, const int32_t* __restrict__ top_k,
                                                      const float* __restrict__ top_p, const float* __restrict__ min_p,
@@ -460,7 +561,7 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
 {
     __shared__ Lds s;
     const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Row<T, NV> r;
+    Row<T, NV, N> r;
     r.x = logits + (size_t)row * ld;
     r.vocab = vocab;
     r.load();
@@ -471,13 +572,22 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     const float mp = min_p ? min_p[row] : 0.f;
     a.least = mp > 0.f ? max((u64)ceil(fmin((double)mp, 1.0) * (double)MASS_ONE), (u64)1) : 1;
 
-    // the largest logit, each thread's own, and whether the row holds a NaN or a +inf
-    float mine = -INFINITY;
-    bool bad = false;
-    r.each([&](float l, int) {
-        bad |= !(l < INFINITY);
-        mine = fmaxf(mine, l);
+    // The largest logit, each thread's own, and whether the row holds a NaN or a +inf: by their bits, of which three are looked at at a time.
+    // The largest of them signed is the largest logit that is not negative, or a NaN or +inf; else the smallest unsigned is the largest
+    // logit; a negative NaN is the largest unsigned.
+    int most_signed = (int)0x80000000;
+    unsigned most = 0, least_bits = 0xffffffffu;
+    r.each_vec([&](int, int, const float* l) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const unsigned b = __float_as_uint(l[e]);
+            most_signed = max(most_signed, (int)b);
+            most = max(most, b);
+            least_bits = min(least_bits, b);
+        }
     });
+    const bool bad = most_signed >= 0x7f800000 || most > 0xff800000u;
+    const float mine = __uint_as_float(most_signed >= 0 ? (unsigned)most_signed : least_bits);
     {
         const unsigned w = wave_max(__any(bad) ? 0xffffffffu : key_of(mine));
         if (lane == 0) s.tops[wave] = w;
@@ -527,54 +637,91 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
             if (o.logprob) *o.logprob = 0.f;
             if (o.n_kept) *o.n_kept = 1;
         }
-        if (o.out)
-            r.each([&](float l, int i) {
-                if (i < vocab) o.out[i] = i == c.id ? l : -INFINITY;
-            });
+        write_row(r, o.out, [&](float, int i) { return i == c.id; });
         return;
     }
     bool listed = false;
     if (a.k > 1 && a.k <= TPB) {
-        // The k-th largest of the threads' largest logits is at most the k-th largest of all: what is as large makes the list.
-        clear(s, BINS);
-        const bool some = m(mine) > 0;
-        if (some) atomicAdd(&s.hist[m.bin(mine)], 1ull);
-        if (threadIdx.x == 0) s.bin = BINS - 1;
+        // The k-th largest of the threads' largest logits is at most the k-th largest of all: what is as large makes the list.  (By
+        // bins of 31 / 1024 nats, one a thread: the k-th is the smallest in its bin at the latest.)
+        s.count[threadIdx.x] = 0;
         __syncthreads();
-        crossing(s, BINS, (u64)a.k);
-        if (some && m.bin(mine) <= s.bin) atomicMin(&s.least_key, key_of(mine));
-        const bool few = __syncthreads_count(some) < a.k;   // then everything with mass may be among the first k
-        const float least = few ? -INFINITY : logit_of(s.least_key);
-        r.each([&](float l, int i) {
-            if (l < least || !(l > -INFINITY)) return;
-            const int at = atomicAdd(&s.n_list, 1);
-            if (at < LIST) {
-                s.lx[at] = l;
-                s.lid[at] = i;
-            }
+        const bool some = m(mine) > 0;
+        const int bin = min(m.bin(mine) / (BINS / TPB), TPB - 1);
+        if (some) atomicAdd(&s.count[bin], 1u);
+        __syncthreads();
+        unsigned upto = wave_scan(s.count[threadIdx.x]);
+        if (lane == 63) s.tops[wave] = upto;
+        __syncthreads();
+        unsigned before = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            before += w < wave ? s.tops[w] : 0u;
+            all += s.tops[w];
+        }
+        upto += before;
+        if (upto >= (unsigned)a.k && upto - s.count[threadIdx.x] < (unsigned)a.k) s.bin = threadIdx.x;
+        __syncthreads();
+        const bool few = all < (unsigned)a.k;   // then everything with mass may be among the first k
+        if (some && !few && bin <= s.bin) atomicMin(&s.least_key, key_of(mine));
+        __syncthreads();
+        const float least = few ? -0x1.fffffep127f : logit_of(s.least_key);
+        const int least_pos = least > 0.f ? __float_as_int(least) : 0x7fffffff;   // bits of numbers above 0 rise with them
+        r.each_vec([&](int, int i0, const float* l) {
+            int m0 = __float_as_int(l[0]);
+#pragma unroll
+            for (int e = 1; e < N; ++e) m0 = max(m0, __float_as_int(l[e]));
+            bool any = m0 >= least_pos;
+            if (least <= 0.f)
+#pragma unroll
+                for (int e = 0; e < N; ++e) any |= l[e] >= least;
+            if (!__any(any)) return;
+            int n = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) n += l[e] >= least;
+            const unsigned upto = wave_scan((unsigned)n);
+            int at = 0;
+            if (lane == 63) at = atomicAdd(&s.n_list, (int)upto);
+            at = __builtin_amdgcn_readlane(at, 63) + (int)upto - n;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (l[e] >= least) {
+                    if (at < LIST) {
+                        s.lx[at] = l[e];
+                        s.lid[at] = i0 + e;
+                    }
+                    ++at;
+                }
         });
         __syncthreads();
         listed = s.n_list <= LIST;
         if (!few) c.key = s.least_key;   // no token outside the list is in
     }
+    if (listed && s.n_list <= SHORT) {
+        short_list(r, m, a, u, o, s);
+        return;
+    }
     const List list = {&s, s.n_list};
     if (listed ? cuts(list, m, a, c, vocab, s) : cuts(r, m, a, c, vocab, s)) finish(r, listed ? &list : nullptr, m, a, c, u, o, s);
-    else slow_row<T>(r.x, vocab, m, a, u, o, s);
+    else slow_row<T, N>(r.x, vocab, m, a, u, o, s);
+}
+
+template <typename T, int NV, int N>
+void launch_filter(const spec_filter_args* a, const spec_filter_out* o, hipStream_t s)
+{
+    hipLaunchKernelGGL((filter_kernel<T, NV, N>), dim3(a->rows), dim3(TPB), 0, s, (const T*)a->logits, a->ld, a->vocab, a->uniforms, a->temperature,
+                       a->top_k, a->top_p, a->min_p, o->tokens, o->logprob, o->n_kept, o->logits_out);
 }
 
 template <typename T>
 void launch_filter(const spec_filter_args* a, const spec_filter_out* o, hipStream_t s)
 {
-    constexpr int PER = TPB * Vec<T>::N;
-    auto go = [&](auto nv) {
-        constexpr int NV = decltype(nv)::value;
-        hipLaunchKernelGGL((filter_kernel<T, NV>), dim3(a->rows), dim3(TPB), 0, s, (const T*)a->logits, a->ld, a->vocab, a->uniforms, a->temperature,
-                           a->top_k, a->top_p, a->min_p, o->tokens, o->logprob, o->n_kept, o->logits_out);
-    };
+    constexpr int N = 16 / sizeof(T);
     // rows of up to 32768 logits stay in registers
-    if (a->vocab <= 8192) go(std::integral_constant<int, 8192 / PER>());
-    else if (a->vocab <= 32768) go(std::integral_constant<int, 32768 / PER>());
-    else go(std::integral_constant<int, 0>());
+    if (a->vocab < N) launch_filter<T, 1, 1>(a, o, s);
+    else if (a->vocab <= 8192) launch_filter<T, 8192 / TPB / N, N>(a, o, s);
+    else if (a->vocab <= 32768) launch_filter<T, 32768 / TPB / N, N>(a, o, s);
+    else launch_filter<T, 0, N>(a, o, s);
 }
 
 }  // namespace
