@@ -450,6 +450,7 @@ def spec_decode_get_view(d: Decoder) -> spec_decode_view:
 # Types, shapes and strides are checked where the tensors are read: csrc/native.cpp.  A wrong one raises ValueError, a status
 # other than SPEC_OK raises SpecError.
 
+KV8_PAGE = 32   # positions of a page of the 8-bit cache
 _F8 = torch.float8_e4m3fn
 _native_module = None
 
