@@ -278,10 +278,11 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
     const char* const wl0 = lds + wc * CT * TILE + lane * 16;
     const char* const xl0 = lds + (BC + wr * RT) * TILE + r16 * 128 + ((g ^ (r16 & 7)) * 16);
     const char* const xh0 = lds + (BC + wr * RT) * TILE + r16 * 128 + (((g ^ (r16 & 7)) * 16) ^ 64);
-    for (int kb = 0; kb < n_blocks; ++kb) {
+    // Stage kb of the first ones, which request stage kb + S - 1 as they go, and of the last S - 1, which do not
+    auto stage = [&](auto requests) {
+        constexpr bool MORE = decltype(requests)::value;
         q8_wait_lds();   // what is read of stage kb - 1 is in registers
-        if (asked - 1 - kb >= S - 2) q8_wait_fetches<(S - 2) * PER>();
-        else q8_wait_fetches<0>();
+        q8_wait_fetches<MORE ? (S - 2) * PER : 0>();
         q8_barrier();   // stage kb is whole, and every wavefront is done with stage kb - 1
         const char *wl = wl0 + from, *xl = xl0 + from, *xh = xh0 + from;
         const float* sl = reinterpret_cast<const float*>(lds + from + KIB * 1024) + wr * RT * 16 + r16;
@@ -290,12 +291,10 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
         // largest accumulators, where either costs more registers than there are
         constexpr bool ROOM = RT * CT < 32;
         constexpr int AHEAD = ROOM ? 1 : 0;
-        const bool more = asked < n_blocks;
-        if (!ROOM && more) {
+        if (!ROOM && MORE) {
 #pragma unroll
             for (int u = 0; u < PER; ++u) request(u);
             advance();
-            ++asked;
         }
         typename Block<T>::Op wf[CT], xf[1 + AHEAD];
         if (AHEAD) xf[0] = read_x(0);
@@ -312,7 +311,7 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
             q8_floatx4 d[CT];
 #pragma unroll
             for (int b = 0; b < CT; ++b) d[b] = Block<T>::dot(wf[b], xf[a & AHEAD]);
-            if (ROOM && more) {
+            if (ROOM && MORE) {
 #pragma unroll
                 for (int u = a; u < PER; u += RT) request(u);
             }
@@ -321,12 +320,18 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[b][i], f, acc[a][b][i]);
         }
-        if (ROOM && more) {
-            advance();
-            ++asked;
-        }
+        if (ROOM && MORE) advance();
         from = from == (S - 1) * STAGE ? 0 : from + STAGE;
-    }
+        // No branch between a product and the sum that takes it: a result has to be waited for, for twelve states after these products, and
+        // the compiler, which moves sums into the next stage, does not count them along every path where branches meet.  So the sums are
+        // pinned to their stage.
+#pragma unroll
+        for (int a = 0; a < RT; ++a)
+#pragma unroll
+            for (int b = 0; b < CT; ++b) asm volatile("" : "+v"(acc[a][b]));
+    };
+    for (; asked < n_blocks; ++asked) stage(std::true_type());
+    for (int kb = max(0, n_blocks - (S - 1)); kb < n_blocks; ++kb) stage(std::false_type());
 #pragma unroll
     for (int a = 0; a < RT; ++a) {
         const int m = m0 + (wr * RT + a) * 16 + r16;
