@@ -203,22 +203,32 @@ __global__ void __launch_bounds__(64 * WAVES) skinny_kernel(const uint8_t* __res
 
 // ---- many rows: the matrix cores ----------------------------------------------------------------------------------------
 //
-// WR x WC wavefronts take 16 WR RT rows by 16 WC CT columns.  A stage holds one block of K of both operands as 2 KiB tiles, with the
-// scales behind them.  Stages are fetched S - 1 ahead, straight into LDS.
+// WR x WC wavefronts take 16 WR RT rows by 16 WC CT columns.  A stage holds one block of K of both operands as 2 KiB tiles; its scales
+// lie behind all stages.  Stages are fetched straight into LDS, S of them under way or in use.
+//
+// What bounds it, seen at 4096 x 8192 x 8192 with tiles of 256 x 256: the products alone would take 0.95 us a stage, the fetches of its
+// 64 KiB alone take 1.8 (a compute unit has some 8 KiB of them under way at 400 cycles), both together 1.9.  So the tile is as large as
+// the registers allow, and everything else hides behind the fetches: W's tiles of the next stage replace this one's in the registers
+// one by one, X's are read a row tile ahead, requests go out between products, and (SPLIT) the part of a stage that is free by half of
+// it -- W, and half of X's row tiles -- is requested half a stage earlier.  The requests in a row at a stage's start and one barrier:
+// 255 us, this 246 (2.2 PFLOP/s); 352 rows of 22016 x 4096: 66 and 59.  The smaller tiles have more stages under way and lose
+// by the second barrier (1024 rows of 4096 x 4096 25 us, 22.6 without).
 //
 // W's tiles are in operand order.  A tile of X is 16 rows of 128 bytes, the 16-byte pieces of row n in the order piece ^ (n & 7): eight
 // lanes then fetch a whole line of memory (four rows' pieces of 64 bytes a request come at a third of the rate: 9.6 TB/s from the
 // L2s where whole lines come at 28), and the eight lanes of an LDS cycle still read eight different groups of banks.
-template <int WR, int WC, int RT, int CT, int S, typename T>
+template <int WR, int WC, int RT, int CT, int S, bool SPLIT, typename T>
 __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
                                                        const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles,
                                                        int row_blocks, int col_blocks)
 {
     static_assert(CT * 16 <= 128 && 128 % (CT * 16) == 0, "a wavefront's columns share the scale of W");
-    constexpr int W = WR * WC, BR = WR * RT, BC = WC * CT, KIB = 2 * (BR + BC), U = (KIB + W - 1) / W, STAGE = KIB * 1024 + (BR + 3) / 4 * 256 + 256;
-    static_assert((BR + 3) / 4 < W && S * STAGE <= 160 * 1024, "tile shape");
-    constexpr int PER = U + 1;   // requests of a wavefront for a stage
-    __shared__ __attribute__((aligned(16))) char lds[S * STAGE];
+    constexpr int W = WR * WC, BR = WR * RT, BC = WC * CT, H = SPLIT ? RT / 2 : RT;
+    // KiB of a stage's first part, of its second part; requests of a wavefront for either (the first one's with the scales)
+    constexpr int KA = 2 * (BC + WR * H), KB = 2 * WR * (RT - H), UA = (KA + W - 1) / W, UB = (KB + W - 1) / W, PA = UA + 1, PB = UB;
+    constexpr int STAGE = 2 * (BR + BC) * 1024, S_STAGE = (BR + 3) / 4 * 256 + 256, SS = SPLIT ? S + 1 : S;
+    static_assert((BR + 3) / 4 < W && S * STAGE + SS * S_STAGE <= 160 * 1024, "tile shape");
+    __shared__ __attribute__((aligned(16))) char lds[S * STAGE + SS * S_STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int wr = wave / WC, wc = wave % WC;
     // The row blocks of a column block follow each other on one XCD: its L2 has W once
@@ -228,37 +238,60 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
     const size_t kp = (size_t)n_blocks * SPEC_Q8_BLOCK;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
 
-    // Request u of this wavefront is the KiB W u + wave of a stage: half of a tile, W's first.  Rows and columns beyond the end
-    // are the last ones again (never stored).
-    uint32_t offset[U];
+    // Request u of this wavefront is the KiB W u + wave of a part: half of a tile, in the first part W's first.  Rows and columns beyond
+    // the end are the last ones again (never stored).  W's requests differ by a scalar, X's by the row of each lane.
+    constexpr int UX = 2 * BC / W, UW = (2 * BC + W - 1) / W;   // requests from UX on may be X's, up to UW W's
+    auto a_kib = [&](int u) { return min(W * u + wave, KA - 1); };   // (a wavefront without one repeats the last)
+    auto b_kib = [&](int u) { return min(W * u + wave, KB - 1); };
+    auto a_tile = [&](int kib) { const int t = (kib >> 1) - BC; return t / H * RT + t % H; };   // of the row block's
+    auto b_tile = [&](int kib) { const int t = kib >> 1; return t / max(RT - H, 1) * RT + H + t % max(RT - H, 1); };
+    auto x_row = [&](int tile, int kib) {
+        return (uint32_t)(min(m0 + 16 * tile + 8 * (kib & 1) + (lane >> 3), M - 1) - m0) * (uint32_t)kp + (((lane & 7) ^ (lane >> 3)) * 16);
+    };
+    uint32_t xa_offset[UA - UX], xb_offset[UB + 1];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int kib = min(W * u + wave, KIB - 1), tile = kib >> 1, half = kib & 1;   // (a wavefront without one repeats the last)
-        if (tile < BC) offset[u] = (uint32_t)min(j0 + tile, n_tiles - 1) * TILE + half * 1024 + lane * 16;
-        else offset[u] = (uint32_t)(min(m0 + 16 * (tile - BC) + 8 * half + (lane >> 3), M - 1) - m0) * (uint32_t)kp + (((lane & 7) ^ (lane >> 3)) * 16);
-    }
-    const uint8_t* xb = x + (size_t)m0 * kp;
-    const uint8_t* wb = w;
+    for (int u = UX; u < UA; ++u) xa_offset[u - UX] = a_kib(u) < 2 * BC ? 0 : x_row(a_tile(a_kib(u)), a_kib(u));
+#pragma unroll
+    for (int u = 0; u < UB; ++u) xb_offset[u] = x_row(b_tile(b_kib(u)), b_kib(u));
+    const uint8_t *xa = x + (size_t)m0 * kp, *xb = xa, *wb = w;
     // 64 scales a wavefront: the rows', and by those left over the columns' blocks' (j0 is a multiple of eight tiles or within one)
     const bool rows_scales = wave * 4 < BR;
     const float* sb = rows_scales ? sx : sw;
     const size_t s_step = rows_scales ? (size_t)M : 1;
     const uint32_t s_off = rows_scales ? (uint32_t)min(m0 + wave * 64 + lane, M - 1) * 4u : (uint32_t)(min((j0 >> 3) + lane, (n_tiles - 1) >> 3) * n_blocks) * 4u;
-    const uint32_t s_to = lds0 + KIB * 1024 + (rows_scales ? wave * 256 : (BR + 3) / 4 * 256);
-    uint32_t slot_to = 0;
-    auto request = [&](int u) {
-        if (u < U) {
-            const int kib = min(W * u + wave, KIB - 1);
-            q8_fetch_lds((W * u + W - 1) / 2 < BC || kib / 2 < BC ? wb : xb, offset[u], lds0 + slot_to + kib * 1024);
+    const uint32_t s_to = lds0 + S * STAGE + (rows_scales ? wave * 256 : (BR + 3) / 4 * 256);
+    uint32_t a_to = 0, b_to = 0, scales_to = 0;   // where the next part, the next scales go
+    auto request_a = [&](int u) {
+        if (u < UA) {
+            const int kib = a_kib(u);
+            if (u < UX || (u < UW && kib < 2 * BC))
+                q8_fetch_lds(wb + ((uint32_t)min(j0 + kib / 2, n_tiles - 1) * TILE + (kib & 1) * 1024), lane * 16, lds0 + a_to + kib * 1024);
+            else q8_fetch_lds(xa, xa_offset[u < UX ? 0 : u - UX], lds0 + a_to + ((BC + a_tile(kib)) * 2 + (kib & 1)) * 1024);
         } else {
-            q8_fetch_lds_dword(sb, s_off, s_to + slot_to);
+            q8_fetch_lds_dword(sb, s_off, s_to + scales_to);
         }
     };
-    auto advance = [&]() {
+    auto request_b = [&](int u) { q8_fetch_lds(xb, xb_offset[u], lds0 + b_to + ((BC + b_tile(b_kib(u))) * 2 + (b_kib(u) & 1)) * 1024); };
+    auto advance_a = [&]() {
         wb += (size_t)n_tiles * TILE;
-        xb += SPEC_Q8_BLOCK;
+        xa += SPEC_Q8_BLOCK;
         sb += s_step;
-        slot_to = slot_to == (S - 1) * STAGE ? 0 : slot_to + STAGE;
+        a_to = a_to == (S - 1) * STAGE ? 0 : a_to + STAGE;
+        scales_to = scales_to == (SS - 1) * S_STAGE ? 0 : scales_to + S_STAGE;
+    };
+    auto advance_b = [&]() {
+        xb += SPEC_Q8_BLOCK;
+        b_to = b_to == (S - 1) * STAGE ? 0 : b_to + STAGE;
+    };
+    auto all_a = [&]() {
+#pragma unroll
+        for (int u = 0; u < PA; ++u) request_a(u);
+        advance_a();
+    };
+    auto all_b = [&]() {
+#pragma unroll
+        for (int u = 0; u < PB; ++u) request_b(u);
+        advance_b();
     };
 
     const int w_scale = ((j0 + wc * CT) >> 3) - (j0 >> 3);
@@ -268,70 +301,113 @@ __global__ void __launch_bounds__(64 * WR * WC, WR * WC == 8 ? 2 : 1) tiled_kern
 #pragma unroll
         for (int b = 0; b < CT; ++b) acc[a][b] = (q8_floatx4){0.f, 0.f, 0.f, 0.f};
 
-    int asked = 0;
-    for (; asked < min(n_blocks, S - 1); ++asked) {
-#pragma unroll
-        for (int u = 0; u < PER; ++u) request(u);
-        advance();
+    for (int k = 0; k < min(n_blocks, S); ++k) {
+        all_a();
+        all_b();
     }
-    uint32_t from = 0;
-    const char* const wl0 = lds + wc * CT * TILE + lane * 16;
-    const char* const xl0 = lds + (BC + wr * RT) * TILE + r16 * 128 + ((g ^ (r16 & 7)) * 16);
-    const char* const xh0 = lds + (BC + wr * RT) * TILE + r16 * 128 + (((g ^ (r16 & 7)) * 16) ^ 64);
-    // Stage kb of the first ones, which request stage kb + S - 1 as they go, and of the last S - 1, which do not
-    auto stage = [&](auto requests) {
-        constexpr bool MORE = decltype(requests)::value;
-        q8_wait_lds();   // what is read of stage kb - 1 is in registers
-        q8_wait_fetches<MORE ? (S - 2) * PER : 0>();
-        q8_barrier();   // stage kb is whole, and every wavefront is done with stage kb - 1
-        const char *wl = wl0 + from, *xl = xl0 + from, *xh = xh0 + from;
-        const float* sl = reinterpret_cast<const float*>(lds + from + KIB * 1024) + wr * RT * 16 + r16;
-        auto read_x = [&](int a) { return Block<T>::op(operand((const uint8_t*)xl + a * TILE, (const uint8_t*)xh + a * TILE)); };
-        // X tiles read ahead, and requests between the products rather than in front of the LDS reads, which they hold up: not with the
-        // largest accumulators, where either costs more registers than there are
-        constexpr bool ROOM = RT * CT < 32;
-        constexpr int AHEAD = ROOM ? 1 : 0;
-        if (!ROOM && MORE) {
-#pragma unroll
-            for (int u = 0; u < PER; ++u) request(u);
-            advance();
-        }
-        typename Block<T>::Op wf[CT], xf[1 + AHEAD];
-        if (AHEAD) xf[0] = read_x(0);
+    const char* const wl = lds + wc * CT * TILE + lane * 16;
+    const char* const xl = lds + (BC + wr * RT) * TILE + r16 * 128 + ((g ^ (r16 & 7)) * 16);
+    const char* const xh = lds + (BC + wr * RT) * TILE + r16 * 128 + (((g ^ (r16 & 7)) * 16) ^ 64);
+    const char* const sl = lds + S * STAGE + (wr * RT * 16 + r16) * 4;
+    const char* const wsl = lds + S * STAGE + (BR + 3) / 4 * 256 + 4 * w_scale;
+    // What is read ahead of a step (one row tile times CT column tiles): its row tile, and in a stage's last step the next one's columns
+    constexpr int AHEAD = RT % 2 == 0 ? 1 : 2, XN = AHEAD + 1, MID = H - AHEAD;   // MID: the step that reads the first row tile of the second part
+    static_assert(RT % XN == 0 && (!SPLIT || MID >= 0), "the same registers for the same tile of every stage");
+    typename Block<T>::Op wf[CT];
+    q8_intx8 xf[XN];
+    float f[XN], ws[2];   // ws: this stage's, the next one's
+    uint32_t from = 0, scales_from = 0;
+    auto read_w = [&](int b) { wf[b] = Block<T>::op(operand((const uint8_t*)wl + from + b * TILE, (const uint8_t*)wl + from + b * TILE + 1024)); };
+    auto read_x = [&](int a) {
+        xf[a % XN] = operand((const uint8_t*)xl + from + a * TILE, (const uint8_t*)xh + from + a * TILE);
+        f[a % XN] = *reinterpret_cast<const float*>(sl + scales_from + 64 * a);
+    };
+    auto step = [&](int a, float w_factor, bool ahead) {
+        if (ahead) read_x((a + AHEAD) % RT);
+        const typename Block<T>::Op xo = Block<T>::op(xf[a % XN]);
+        const float factor = f[a % XN] * w_factor;
+        q8_floatx4 d[CT];
 #pragma unroll
         for (int b = 0; b < CT; ++b) {
-            const char* p = wl + b * TILE;
-            wf[b] = Block<T>::op(operand((const uint8_t*)p, (const uint8_t*)p + 1024));
+            d[b] = Block<T>::dot(wf[b], xo);
+            if (ahead && a == RT - 1) read_w(b);
         }
-        const float ws = *reinterpret_cast<const float*>(lds + from + KIB * 1024 + (BR + 3) / 4 * 256 + 4 * w_scale);
 #pragma unroll
-        for (int a = 0; a < RT; ++a) {
-            if (a + AHEAD < RT) xf[(a + AHEAD) & AHEAD] = read_x(a + AHEAD);
-            const float f = sl[16 * a] * ws;
-            q8_floatx4 d[CT];
+        for (int b = 0; b < CT; ++b)
 #pragma unroll
-            for (int b = 0; b < CT; ++b) d[b] = Block<T>::dot(wf[b], xf[a & AHEAD]);
-            if (ROOM && MORE) {
-#pragma unroll
-                for (int u = a; u < PER; u += RT) request(u);
-            }
-#pragma unroll
-            for (int b = 0; b < CT; ++b)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[b][i], f, acc[a][b][i]);
-        }
-        if (ROOM && MORE) advance();
-        from = from == (S - 1) * STAGE ? 0 : from + STAGE;
+            for (int i = 0; i < 4; ++i) acc[a][b][i] = fmaf(d[b][i], factor, acc[a][b][i]);
+    };
+    auto pin = [&]() {
         // No branch between a product and the sum that takes it: a result has to be waited for, for twelve states after these products, and
-        // the compiler, which moves sums into the next stage, does not count them along every path where branches meet.  So the sums are
-        // pinned to their stage.
+        // the compiler, which moves sums across the loop's end, does not count them along every path where branches meet.
 #pragma unroll
         for (int a = 0; a < RT; ++a)
 #pragma unroll
             for (int b = 0; b < CT; ++b) asm volatile("" : "+v"(acc[a][b]));
     };
-    for (; asked < n_blocks; ++asked) stage(std::true_type());
-    for (int kb = max(0, n_blocks - (S - 1)); kb < n_blocks; ++kb) stage(std::false_type());
+    // Every wavefront has read what it needs of the part that is requested next; the part that is read next is whole
+    auto meet = [&](auto requests) {
+        constexpr bool MORE = decltype(requests)::value;
+        q8_wait_lds();
+        q8_wait_fetches<!MORE ? 0 : SPLIT ? (S - 1) * (PA + PB) : (S - 2) * PA>();
+        q8_barrier();
+    };
+    // From the point where all of stage kb is in registers or used up to the same point of stage kb + 1.  A place is requested anew as
+    // soon as it is free, between the products (requests in front of the LDS reads would hold those up): a stage's second part here,
+    // stage kb + S's; a first part, with W, which is in registers all through a stage, half a stage earlier, for stage kb + 1 + S.
+    auto turn = [&](auto requests, auto last, int kb) {
+        constexpr bool MORE = decltype(requests)::value, LAST = decltype(last)::value;
+        if (!LAST) {
+            meet(requests);
+            if (SPLIT && !MORE && kb + S < n_blocks) all_b();
+            from = from == (S - 1) * STAGE ? 0 : from + STAGE;
+            scales_from = scales_from == (SS - 1) * S_STAGE ? 0 : scales_from + S_STAGE;
+            ws[1] = *reinterpret_cast<const float*>(wsl + scales_from);
+        }
+#pragma unroll
+        for (int i = 0; i < (LAST ? AHEAD : RT); ++i) {
+            const int a = (RT - AHEAD + i) % RT;
+            if (SPLIT && !LAST && i >= AHEAD && a == MID) meet(requests);
+            step(a, ws[i < AHEAD ? 0 : 1], !LAST);
+            if (MORE && SPLIT && i < AHEAD + MID) {
+#pragma unroll
+                for (int u = i; u < PB; u += AHEAD + MID) request_b(u);
+            } else if (MORE) {
+                constexpr int I0 = SPLIT ? AHEAD + MID : 0;
+#pragma unroll
+                for (int u = i - I0; u < PA; u += RT - I0) request_a(u);
+            }
+        }
+        if (MORE) {
+            advance_a();
+            if (SPLIT) advance_b();
+        }
+        ws[0] = ws[1];
+        pin();
+    };
+    if (n_blocks >= S) q8_wait_fetches<(S - 1) * (PA + PB)>();
+    else q8_wait_fetches<0>();
+    q8_barrier();
+#pragma unroll
+    for (int b = 0; b < CT; ++b) read_w(b);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) read_x(a);
+    ws[0] = *reinterpret_cast<const float*>(wsl);
+#pragma unroll
+    for (int a = 0; a < RT - AHEAD; ++a) {
+        if (SPLIT && a == MID) {
+            pin();
+            q8_wait_lds();
+            q8_barrier();
+            if (S < n_blocks) all_a();
+        }
+        step(a, ws[0], true);
+    }
+    pin();
+    int kb = 0;
+    for (; kb + S + SPLIT < n_blocks; ++kb) turn(std::true_type(), std::false_type(), kb);
+    for (; kb + 1 < n_blocks; ++kb) turn(std::false_type(), std::false_type(), kb);
+    turn(std::false_type(), std::true_type(), kb);
 #pragma unroll
     for (int a = 0; a < RT; ++a) {
         const int m = m0 + (wr * RT + a) * 16 + r16;
@@ -349,12 +425,12 @@ void launch_skinny(const void* x, const void* w, const float* sx, const float* s
                        (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks, n_tiles);
 }
 
-template <int WR, int WC, int RT, int CT, int S, typename T>
+template <int WR, int WC, int RT, int CT, int S, bool SPLIT, typename T>
 void launch_tiled(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
 {
     constexpr int BR = WR * RT, BC = WC * CT;
     const int n_tiles = (N + 15) / 16, row_blocks = (M + 16 * BR - 1) / (16 * BR), col_blocks = (n_tiles + BC - 1) / BC;
-    auto kernel = tiled_kernel<WR, WC, RT, CT, S, T>;
+    auto kernel = tiled_kernel<WR, WC, RT, CT, S, SPLIT, T>;
     hipLaunchKernelGGL(kernel, dim3(row_blocks * col_blocks), dim3(64 * WR * WC), 0, s, (const uint8_t*)x, (const uint8_t*)w, sx, sw, (T*)y, M, N, n_blocks,
                        n_tiles, row_blocks, col_blocks);
 }
@@ -374,11 +450,11 @@ void launch_few(const void* x, const void* w, const float* sx, const float* sw, 
         else if (n_blocks < 48) launch_skinny<1, 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
         else launch_skinny<1, 1, 16, T>(x, w, sx, sw, y, M, N, n_blocks, s);
     } else {
-        if (n_tiles > 1536 && near) launch_tiled<1, 8, RT, 1, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-        else if (n_tiles > 1024 && near) launch_tiled<1, 6, RT, 1, 5, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-        else if (n_tiles > 512 && near) launch_tiled<1, 4, RT, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        if (n_tiles > 1536 && near) launch_tiled<1, 8, RT, 1, 3, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 1024 && near) launch_tiled<1, 6, RT, 1, 5, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 512 && near) launch_tiled<1, 4, RT, 1, 4, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
         else if (n_tiles > 256 && RT < 4) launch_skinny<RT, RT < 4 ? 2 : 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-        else if (n_tiles > 256 && near) launch_tiled<2, 4, 2, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        else if (n_tiles > 256 && near) launch_tiled<2, 4, 2, 1, 4, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
         else launch_skinny<RT, 1, 8, T>(x, w, sx, sw, y, M, N, n_blocks, s);
     }
 }
@@ -388,7 +464,7 @@ struct TileShape {
     int rows, cols;
     float us;
 };
-constexpr TileShape SHAPES[] = {{64, 64, 0.35f}, {64, 128, 0.45f}, {128, 128, 0.7f}, {256, 128, 1.1f}, {256, 256, 2.1f}};
+constexpr TileShape SHAPES[] = {{64, 64, 0.36f}, {64, 128, 0.48f}, {128, 128, 0.74f}, {256, 128, 1.1f}, {256, 256, 1.9f}};
 
 template <typename T>
 void launch_gemm(const void* x, const void* w, const float* sx, const float* sw, void* y, int M, int N, int n_blocks, hipStream_t s)
@@ -411,12 +487,12 @@ void launch_gemm(const void* x, const void* w, const float* sx, const float* sw,
         }
     }
     if constexpr (sizeof(T) == 2) {
-        if (best == 4) return launch_tiled<2, 4, 8, 4, 2, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-        if (best == 3) return launch_tiled<4, 2, 4, 4, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        if (best == 4) return launch_tiled<2, 4, 8, 4, 2, true, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+        if (best == 3) return launch_tiled<4, 2, 4, 4, 3, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
     }
-    if (best == 2) launch_tiled<2, 4, 4, 2, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    else if (best == 1) launch_tiled<2, 4, 2, 2, 3, T>(x, w, sx, sw, y, M, N, n_blocks, s);
-    else launch_tiled<2, 4, 2, 1, 4, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    if (best == 2) launch_tiled<2, 4, 4, 2, 4, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else if (best == 1) launch_tiled<2, 4, 2, 2, 3, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
+    else launch_tiled<2, 4, 2, 1, 4, false, T>(x, w, sx, sw, y, M, N, n_blocks, s);
 }
 
 // One thread copies sixteen bytes of the packed order

@@ -104,3 +104,11 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(y, sv.spec_q8_gemm(q, s, p, ws, torch.empty_like(y)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,N", [(130, 4000), (350, 4090), (1024, 4096), (2047, 4100), (2040, 8190), (33, 25000), (60, 9000)])
+@pytest.mark.parametrize("K", [100, 250, 380, 500, 640, 770, 896])
+def test_a_few_blocks_of_k(M, N, K, dtype):
+    """As many blocks as the kernels fetch ahead, fewer and more."""
+    check(M, N, K, dtype)
