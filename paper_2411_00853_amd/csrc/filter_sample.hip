@@ -388,6 +388,45 @@ __device__ __forceinline__ void write_row(const Row<T, NV, N>& r, float* out, F 
     });
 }
 
+// The draw: s.hist[0 .. 1024) holds the kept masses by chunk of 64 N ids
+template <typename T, int N>
+__device__ __forceinline__ void draw_from_chunks(const T* x, int vocab, const Masses& m, const Params& a, const Cut& c, float u, const Sums& kept,
+                                                 const Results& o, Lds& s)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const u64 target = min((u64)((double)u * (double)kept.mass), kept.mass - 1);
+    crossing(s, 1024, target + 1);
+    if (wave == 0) {
+        u64 w[N], sum = 0;
+        const int i0 = s.bin * 64 * N + lane * N;   // (in the order of the ids, also where a load was moved)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float l = i0 + e < vocab ? q8_widen(x[i0 + e]) : -INFINITY;
+            w[e] = m(l);
+            if (w[e] < a.least || !c.has(l, i0 + e)) w[e] = 0;
+            sum += w[e];
+        }
+        const u64 before = s.above + wave_scan(sum) - sum;
+        if (before <= target && before + sum > target) {
+            int at = 0;   // the first whose running sum exceeds the target
+            u64 drawn = 0, upto = before;
+            bool done = false;
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                upto += w[e];
+                if (!done && upto > target) {
+                    at = e;
+                    drawn = w[e];
+                    done = true;
+                }
+            }
+            *o.token = i0 + at;
+            if (o.logprob) *o.logprob = (float)log((double)drawn / (double)kept.mass);
+            if (o.n_kept) *o.n_kept = (int)kept.n;
+        }
+    }
+}
+
 // The draw among the tokens of a cut, and the results.  `list` holds all of them, or is NULL.
 template <typename T, int NV, int N>
 __device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List* list, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
@@ -423,37 +462,7 @@ __device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List* list,
     }
     __syncthreads();
     const Sums kept = block_sums(n, s.hist[threadIdx.x], s);
-    const u64 target = min((u64)((double)u * (double)kept.mass), kept.mass - 1);
-    crossing(s, 1024, target + 1);
-    if (wave == 0) {
-        u64 w[N], sum = 0;
-        const int i0 = s.bin * CHUNK + lane * N;   // (in the order of the ids, also where a load was moved)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float l = i0 + e < r.vocab ? q8_widen(r.x[i0 + e]) : -INFINITY;
-            w[e] = m(l);
-            if (w[e] < a.least || !c.has(l, i0 + e)) w[e] = 0;
-            sum += w[e];
-        }
-        const u64 before = s.above + wave_scan(sum) - sum;
-        if (before <= target && before + sum > target) {
-            int at = 0;   // the first whose running sum exceeds the target
-            u64 drawn = 0, upto = before;
-            bool done = false;
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                upto += w[e];
-                if (!done && upto > target) {
-                    at = e;
-                    drawn = w[e];
-                    done = true;
-                }
-            }
-            *o.token = i0 + at;
-            if (o.logprob) *o.logprob = (float)log((double)drawn / (double)kept.mass);
-            if (o.n_kept) *o.n_kept = (int)kept.n;
-        }
-    }
+    draw_from_chunks<T, N>(r.x, r.vocab, m, a, c, u, kept, o, s);
     write_row(r, o.out, [&](float l, int i) { return c.has(l, i) && m(l) >= a.least; });
 }
 
@@ -706,6 +715,347 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     else slow_row<T, N>(r.x, vocab, m, a, u, o, s);
 }
 
+// ---- rows shared out among workgroups -------------------------------------------------------------------------------------
+//
+// Without top-k nothing says early which tokens matter, and every pass goes over the whole row.  Then each pass is a launch of its own, in
+// which a workgroup takes a slice of a row; sums over slices are sums of whole numbers, added up in any order.  A workgroup
+// takes slices of whole chunks (64 loads), a wavefront a chunk at a time.
+constexpr int PART_TPB = 256, PART_WAVES = PART_TPB / 64, MAX_PARTS = 64;
+constexpr int MANY = 2048;      // tokens of the bin that top-p's cut falls into
+
+struct Shared {                 // of a row, in the workspace
+    u64 hist[BINS];             // mass by bins, for top-p
+    u64 chunk[1024];            // mass kept, by chunk of ids; without the cut's bin
+    float lx[MANY];             // that bin's tokens
+    int lid[MANY];
+    u64 n_above;                // tokens kept, without the cut's bin
+    u64 above, need;            // mass before that bin, mass that top-p asks for
+    unsigned tops[MAX_PARTS];   // key of a slice's largest logit, ~0: a NaN or +inf
+    unsigned n_list, first, done;   // first: the smallest id of the largest logit, where that one alone is kept
+    Cut cut;
+};
+
+template <typename T>
+struct Part {
+    static constexpr int N = 16 / sizeof(T), CHUNK = 64 * N, AHEAD = 4;
+    const T* x;
+    int vocab, c0, c1;
+    // f(chunk, id of the first, N logits) as Row's
+    template <typename F>
+    __device__ __forceinline__ void each_vec(F f) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+        for (int c = c0 + wave; c < c1; c += PART_WAVES * AHEAD) {
+            Some<T, N> s[AHEAD];
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                s[j] = *reinterpret_cast<const Some<T, N>*>(x + min((c + j * PART_WAVES) * CHUNK + lane * N, vocab - N));
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j) {
+                const int chunk = c + j * PART_WAVES;
+                if (chunk >= c1) break;
+                const int want = chunk * CHUNK + lane * N, i = min(want, vocab - N);
+                float l[N];
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    l[e] = q8_widen(s[j].v[e]);
+                    l[e] = i + e >= want ? l[e] : -INFINITY;
+                }
+                f(chunk, i, l);
+            }
+        }
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ Part<T> part_of(const T* logits, int64_t ld, int vocab)
+{
+    const int n = (vocab + Part<T>::CHUNK - 1) / Part<T>::CHUNK, per = (n + gridDim.x - 1) / gridDim.x, c0 = blockIdx.x * per;
+    return {logits + (size_t)blockIdx.y * ld, vocab, c0, min(c0 + per, n)};
+}
+
+// The row's masses; false: it has none
+__device__ __forceinline__ bool masses_of(const Shared& g, int parts, float t0, Masses& m, unsigned& top)
+{
+    const int lane = threadIdx.x & 63;
+    top = wave_max(lane < parts ? g.tops[lane] : 0u);
+    m.top = logit_of(top);
+    m.t = t0 > 0.f ? fminf(t0, 0x1.fffffep127f) : 1.f;
+    m.r = 1.f / m.t;
+    m.per_nat = (float)BINS / (NATS * m.t);
+    return top != 0xffffffffu && m.top > -INFINITY;
+}
+__device__ __forceinline__ u64 least_mass(const float* min_p, int row)
+{
+    const float mp = min_p ? min_p[row] : 0.f;
+    return mp > 0.f ? max((u64)ceil(fmin((double)mp, 1.0) * (double)MASS_ONE), (u64)1) : 1;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_TPB) part_tops_kernel(const T* __restrict__ logits, int64_t ld, int vocab, Shared* __restrict__ shared)
+{
+    __shared__ unsigned tops[PART_WAVES];
+    Shared& g = shared[blockIdx.y];
+    unsigned top = 0;
+    part_of(logits, ld, vocab).each_vec([&](int, int, const float* l) {
+#pragma unroll
+        for (int e = 0; e < Part<T>::N; ++e) top = max(top, l[e] < INFINITY ? key_of(l[e]) : 0xffffffffu);
+    });
+    top = wave_max(top);
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    for (int i = blockIdx.x * PART_TPB + threadIdx.x; i < BINS; i += gridDim.x * PART_TPB) g.hist[i] = 0;
+    __syncthreads();
+    if (threadIdx.x) return;
+    g.tops[blockIdx.x] = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+    if (blockIdx.x == 0) {
+        g.n_above = 0;
+        g.n_list = 0;
+        g.first = 0x7fffffffu;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_TPB) part_bins_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ temperature,
+                                                             const float* __restrict__ top_p, Shared* __restrict__ shared)
+{
+    __shared__ u64 hist[BINS];
+    Shared& g = shared[blockIdx.y];
+    const float t0 = temperature ? temperature[blockIdx.y] : 1.f;
+    Masses m;
+    unsigned top;
+    if (!masses_of(g, gridDim.x, t0, m, top) || !(t0 > 0.f) || !(top_p[blockIdx.y] < 1.f)) return;   // the workgroup as one
+    for (int i = threadIdx.x; i < BINS; i += PART_TPB) hist[i] = 0;
+    __syncthreads();
+    part_of(logits, ld, vocab).each_vec([&](int, int, const float* l) {
+#pragma unroll
+        for (int e = 0; e < Part<T>::N; ++e) {
+            const u64 w = m(l[e]);
+            if (w) atomicAdd(&hist[m.bin(l[e])], w);
+        }
+    });
+    __syncthreads();
+    for (int i = threadIdx.x; i < BINS; i += PART_TPB)
+        if (hist[i]) atomicAdd(&g.hist[i], hist[i]);
+}
+
+// Mass kept, by chunk: of all bins before the one that top-p's cut falls into (without top-p of all), whose tokens are listed
+template <typename T>
+__global__ void __launch_bounds__(PART_TPB) part_masses_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ temperature,
+                                                               const float* __restrict__ top_p, const float* __restrict__ min_p,
+                                                               Shared* __restrict__ shared)
+{
+    __shared__ u64 waves[PART_WAVES];
+    __shared__ int cut_bin;
+    Shared& g = shared[blockIdx.y];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const float t0 = temperature ? temperature[blockIdx.y] : 1.f, p = top_p ? top_p[blockIdx.y] : 1.f;
+    const u64 least = least_mass(min_p, blockIdx.y);
+    const Part<T> part = part_of(logits, ld, vocab);
+    Masses m;
+    unsigned top;
+    if (!masses_of(g, gridDim.x, t0, m, top)) return;
+    if (!(t0 > 0.f)) {   // the first token alone
+        unsigned first = 0x7fffffffu;
+        part.each_vec([&](int, int i0, const float* l) {
+#pragma unroll
+            for (int e = 0; e < Part<T>::N; ++e)
+                if (l[e] == m.top) first = min(first, (unsigned)(i0 + e));
+        });
+        first = 0x7fffffffu - wave_max(0x7fffffffu - first);
+        if (lane == 0 && first != 0x7fffffffu) atomicMin(&g.first, first);
+        return;
+    }
+    int bin = BINS;
+    if (p < 1.f) {
+        constexpr int PER = BINS / PART_TPB;
+        u64 h[PER], mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) mine += h[i] = g.hist[threadIdx.x * PER + i];
+        const u64 upto = wave_scan(mine);
+        if (lane == 63) waves[wave] = upto;
+        __syncthreads();
+        u64 all = 0, before = upto - mine;
+        for (int w = 0; w < PART_WAVES; ++w) {
+            before += w < wave ? waves[w] : 0;
+            all += waves[w];
+        }
+        const u64 need = share(p, all);
+        if (before < need && before + mine >= need) {
+            int i = 0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const bool on = i == k && before + h[k] < need;
+                before += on ? h[k] : 0;
+                i += on;
+            }
+            cut_bin = threadIdx.x * PER + i;
+            if (blockIdx.x == 0) {
+                g.above = before;
+                g.need = need;
+            }
+        }
+        __syncthreads();
+        bin = cut_bin;
+    }
+    unsigned n = 0;
+    part.each_vec([&](int chunk, int i0, const float* l) {
+        unsigned hi = 0, lo = 0;   // of 512 masses at most: no carry out of either half
+#pragma unroll
+        for (int e = 0; e < Part<T>::N; ++e) {
+            const u64 w = m(l[e]);
+            const int b = bin < BINS ? w ? m.bin(l[e]) : BINS : 0;
+            if (b == bin) {
+                const unsigned at = atomicAdd(&g.n_list, 1u);
+                if (at < MANY) {
+                    g.lx[at] = l[e];
+                    g.lid[at] = i0 + e;
+                }
+            }
+            if (b >= bin || w < least) continue;
+            ++n;
+            hi += (unsigned)(w >> 22);
+            lo += (unsigned)w & 0x3fffffu;
+        }
+        hi = wave_sum(hi);
+        lo = wave_sum(lo);
+        if (lane == 0) g.chunk[chunk] = ((u64)hi << 22) + lo;
+    });
+    n = wave_sum(n);
+    if (lane == 0 && n) atomicAdd(&g.n_above, (u64)n);
+}
+
+// One workgroup a row: the cut within its bin, and the draw
+template <typename T>
+__global__ void __launch_bounds__(TPB) part_draw_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ uniforms,
+                                                        const float* __restrict__ temperature, const float* __restrict__ top_p,
+                                                        const float* __restrict__ min_p, int parts, int32_t* __restrict__ tokens,
+                                                        float* __restrict__ logprob, int32_t* __restrict__ n_kept, float* __restrict__ out,
+                                                        Shared* __restrict__ shared)
+{
+    constexpr int N = Part<T>::N, CHUNK = Part<T>::CHUNK;
+    __shared__ Lds s;
+    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_chunks = (vocab + CHUNK - 1) / CHUNK;
+    Shared& g = shared[row];
+    const float t0 = temperature ? temperature[row] : 1.f, u = uniforms[row];
+    const Results o = {tokens + row, logprob ? logprob + row : nullptr, n_kept ? n_kept + row : nullptr, out ? out + (size_t)row * vocab : nullptr};
+    const Params a = {0, top_p ? top_p[row] : 1.f, least_mass(min_p, row)};
+    Masses m;
+    unsigned top;
+    const bool any = masses_of(g, parts, t0, m, top);
+    if (!any || !(t0 > 0.f)) {
+        if (threadIdx.x == 0) {
+            *o.token = any ? (int)g.first : -1;
+            if (o.logprob) *o.logprob = any ? 0.f : __uint_as_float(0x7fc00000u);
+            if (o.n_kept) *o.n_kept = any;
+            g.cut = any ? Cut{top, (int)g.first} : Cut{0xffffffffu, -1};
+            g.done = 0;
+        }
+        return;
+    }
+    Cut c = {0, vocab - 1};
+    const int n = a.p < 1.f ? (int)g.n_list : 0;
+    if (n > MANY) {   // as many equal logits make
+        slow_row<T, N>(logits + (size_t)row * ld, vocab, m, a, u, o, s);
+        if (threadIdx.x == 0) g.done = 1;
+        return;
+    }
+    if (a.p < 1.f) {
+        // each of the bin's tokens against each: larger orders are ranked before
+        const u64 above = g.above, need = g.need;
+        u64 *const order = s.hist, *const mass = s.hist + MANY;
+        static_assert(2 * MANY <= BINS && MANY <= LIST, "the list's place");
+        const int n4 = (n + 3) & ~3;
+        for (int i = threadIdx.x; i < n4; i += TPB) {
+            const float l = i < n ? g.lx[i] : -INFINITY;
+            const int id = i < n ? g.lid[i] : 0;
+            s.lx[i] = l;
+            s.lid[i] = id;
+            order[i] = (u64)key_of(l) << 32 | (unsigned)~id;
+            mass[i] = m(l);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += TPB) {
+            const u64 mine = order[i];
+            u64 upto = above;
+            for (int j = 0; j < n4; j += 4)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) upto += order[j + e] >= mine ? mass[j + e] : 0;
+            if (upto >= need && upto - mass[i] < need) s.cut = {key_of(s.lx[i]), s.lid[i]};
+        }
+        __syncthreads();
+        c = s.cut;
+    }
+    clear(s, 1024);
+    if ((int)threadIdx.x < n_chunks) s.hist[threadIdx.x] = g.chunk[threadIdx.x];
+    __syncthreads();
+    u64 more = 0;
+    for (int i = threadIdx.x; i < n; i += TPB) {
+        const u64 w = m(s.lx[i]);
+        if (w < a.least || !c.has(s.lx[i], s.lid[i])) continue;
+        ++more;
+        atomicAdd(&s.hist[s.lid[i] / CHUNK], w);
+    }
+    __syncthreads();
+    Sums kept = block_sums(more, s.hist[threadIdx.x], s);
+    kept.n += g.n_above;
+    draw_from_chunks<T, N>(logits + (size_t)row * ld, vocab, m, a, c, u, kept, o, s);
+    if (threadIdx.x == 0) {
+        g.cut = c;
+        g.done = 0;
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(PART_TPB) part_write_kernel(const T* __restrict__ logits, int64_t ld, int vocab, const float* __restrict__ temperature,
+                                                              const float* __restrict__ min_p, float* __restrict__ out,
+                                                              const Shared* __restrict__ shared)
+{
+    constexpr int N = Part<T>::N;
+    const Shared& g = shared[blockIdx.y];
+    if (g.done) return;
+    const float t0 = temperature ? temperature[blockIdx.y] : 1.f;
+    const u64 least = t0 > 0.f ? least_mass(min_p, blockIdx.y) : 1;
+    const Cut c = g.cut;
+    Masses m;
+    unsigned top;
+    masses_of(g, gridDim.x, t0, m, top);
+    float* const o = out + (size_t)blockIdx.y * vocab;
+    part_of(logits, ld, vocab).each_vec([&](int chunk, int i0, const float* l) {
+        const int want = (chunk * 64 + (int)(threadIdx.x & 63)) * N;
+        Some<float, N> v;
+#pragma unroll
+        for (int e = 0; e < N; ++e) v.v[e] = l[e] > -INFINITY && c.has(l[e], i0 + e) && m(l[e]) >= least ? l[e] : -INFINITY;
+        if (want + N <= vocab) *reinterpret_cast<Some<float, N>*>(o + i0) = v;
+        else
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (i0 + e >= want && want < vocab) o[i0 + e] = v.v[e];
+    });
+}
+
+// Workgroups a row; 1: the row is one workgroup's
+int parts_of(int rows, int vocab, int dtype)
+{
+    // us, one workgroup a row and shared out, top-p 0.9: 1 row of 8192 32 and 23, of 32000 98 and 26, of 128256 311 and 32; 64 rows of 128256
+    // 340 and 74; 256 rows of 32000 159 and 73.  No filter: 1 row of 8192 14 and 15, of 128256 123 and 19, 256 rows of 128256 178 and 147.
+    const int chunk = 64 * (dtype == SPEC_DTYPE_BF16 ? 8 : 4);
+    if (vocab < 8192 || rows > 256) return 1;
+    return std::min(std::min(768 / rows, MAX_PARTS), vocab / (8 * chunk));
+}
+
+template <typename T>
+void launch_parts(const spec_filter_args* a, const spec_filter_out* o, int parts, Shared* g, hipStream_t s)
+{
+    const T* x = (const T*)a->logits;
+    const dim3 grid(parts, a->rows);
+    hipLaunchKernelGGL((part_tops_kernel<T>), grid, dim3(PART_TPB), 0, s, x, a->ld, a->vocab, g);
+    if (a->top_p) hipLaunchKernelGGL((part_bins_kernel<T>), grid, dim3(PART_TPB), 0, s, x, a->ld, a->vocab, a->temperature, a->top_p, g);
+    hipLaunchKernelGGL((part_masses_kernel<T>), grid, dim3(PART_TPB), 0, s, x, a->ld, a->vocab, a->temperature, a->top_p, a->min_p, g);
+    hipLaunchKernelGGL((part_draw_kernel<T>), dim3(a->rows), dim3(TPB), 0, s, x, a->ld, a->vocab, a->uniforms, a->temperature, a->top_p, a->min_p, parts,
+                       o->tokens, o->logprob, o->n_kept, o->logits_out, g);
+    if (o->logits_out) hipLaunchKernelGGL((part_write_kernel<T>), grid, dim3(PART_TPB), 0, s, x, a->ld, a->vocab, a->temperature, a->min_p, o->logits_out, g);
+}
+
 template <typename T, int NV, int N>
 void launch_filter(const spec_filter_args* a, const spec_filter_out* o, hipStream_t s)
 {
@@ -731,14 +1081,12 @@ using namespace specv;
 
 extern "C" size_t spec_filter_workspace_bytes(int32_t rows, int32_t vocab)
 {
-    (void)rows;
-    (void)vocab;
-    return 0;
+    // (of either type: fp32 rows are shared out among more workgroups)
+    return rows > 0 && vocab > 0 && parts_of(rows, vocab, SPEC_DTYPE_FP32) > 1 ? (size_t)rows * sizeof(Shared) : 0;
 }
 
 extern "C" int spec_filter_sample(const spec_filter_args* a, const spec_filter_out* o, void* workspace, size_t workspace_bytes, void* stream)
 {
-    (void)workspace_bytes;
     if (!a || !o) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: null pointer");
     if (a->rows < 0 || a->vocab <= 0 || a->ld < a->vocab)
         return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: %d rows of %d logits, %lld elements apart", a->rows, a->vocab, (long long)a->ld);
@@ -747,7 +1095,11 @@ extern "C" int spec_filter_sample(const spec_filter_args* a, const spec_filter_o
     if (!a->rows) return SPEC_OK;
     if (!a->logits || !a->uniforms || !o->tokens) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: null pointer");
     if ((uintptr_t)workspace & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: the workspace is not 16-byte aligned");
-    if (a->dtype == SPEC_DTYPE_BF16) launch_filter<uint16_t>(a, o, (hipStream_t)stream);
+    const int parts = !a->top_k && workspace && workspace_bytes >= a->rows * sizeof(Shared) ? parts_of(a->rows, a->vocab, a->dtype) : 1;
+    const bool bf16 = a->dtype == SPEC_DTYPE_BF16;
+    if (parts > 1 && bf16) launch_parts<uint16_t>(a, o, parts, (Shared*)workspace, (hipStream_t)stream);
+    else if (parts > 1) launch_parts<float>(a, o, parts, (Shared*)workspace, (hipStream_t)stream);
+    else if (bf16) launch_filter<uint16_t>(a, o, (hipStream_t)stream);
     else launch_filter<float>(a, o, (hipStream_t)stream);
     SPECV_LAUNCH_CHECK("filter_kernel");
     return SPEC_OK;

@@ -179,3 +179,35 @@ def test_a_filtered_row_is_what_the_verify_step_takes():
         for i in range(a + 1):
             assert float(target.view(B, K + 1, V)[b, i, int(ot[b, i])]) > -math.inf
     h.close()
+
+
+@pytest.mark.parametrize("workspace", [True, False])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_edges_of_long_rows(dtype, workspace):
+    """Rows long enough to be shared out among workgroups, without top-k: what test_excluded_and_extreme_logits and others do to short ones."""
+    vocab = 40003
+    x, u, g = inputs(21, 9, vocab + 9, dtype)
+    x = x[:, 5:vocab + 5]                      # rows that start nowhere in particular
+    x[0, torch.arange(vocab) != 39999] = -math.inf
+    x[1, ::2] = -math.inf
+    x[2, 5:] = torch.finfo(x.dtype).min
+    x[3] = torch.finfo(x.dtype).min
+    x[4, 1::3] = -0.0
+    x[4, ::3] = 0.0
+    x[5, 40002] = math.nan
+    x[6, 0] = math.inf
+    x[7] = -math.inf
+    x[8, 20000] = x[8, 39000] = 50.0
+    t, _, p, mp = params(g, 9, "pm")
+    for top_p, min_p in ((None, None), (p, None), (None, mp), (p, mp)):
+        tokens, kept, lp, lo = draw(x, u, t, None, top_p, min_p, True, workspace)
+        assert tokens[5:8].tolist() == [-1] * 3 and kept[5:8].tolist() == [0] * 3 and bool(lp[5:8].isnan().all())
+        assert torch.all(lo[5:8] == -math.inf)
+        assert int(tokens[0]) == 39999 and int(kept[0]) == 1 and int(tokens[1]) % 2 == 1 and int(tokens[2]) < 5
+        rows = torch.tensor([0, 1, 2, 3, 4, 8], device="cuda")
+        at = lambda v: None if v is None else v[rows].contiguous()  # noqa: E731
+        check(x[rows], at(u), at(t), None, at(top_p), at(min_p), True, workspace)
+    none = torch.zeros(9, device="cuda")
+    tokens, kept, lp, lo = draw(x, u, none, None, p, None, True, workspace)
+    assert int(tokens[8]) == 20000 and int(tokens[0]) == 39999 and tokens[5:8].tolist() == [-1] * 3
+    assert kept.tolist() == [1] * 5 + [0] * 3 + [1] and torch.equal((lo > -math.inf).sum(1).int(), kept)
