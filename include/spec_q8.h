@@ -92,14 +92,17 @@ typedef struct {
  * Keys (rotated, in fp32) and values are rounded to 8 bits once.  A page's scale is set by its new positions where
  * it holds no older one (position < kv_len), else it never shrinks; when it grows, the older positions are rounded
  * again.  A NaN or an infinity is stored as NaN and does not touch the scale.
- * A row whose position is negative, beyond the table or beyond max_pos is not written, and its q_out row is zero. */
+ * A row whose position is negative, beyond the table or beyond max_pos is not written, and its q_out row is zero.  qkv and
+ * q_out 16-byte aligned, cos_sin 8-byte. */
 int spec_kv8_append(const spec_kv8_cache* cache, const void* qkv, int32_t n_q_heads, const int32_t* row0,
                     const int32_t* kv_len, int32_t rows, int32_t max_window, const float* cos_sin, int32_t max_pos,
                     void* q_out, void* stream);
 
 /* out bf16 [rows][n_q_heads * head_dim] = softmax(scale * q . k) v, row j of a window over positions 0 .. kv_len[b] + j.
  * q: bf16, rows ld_q elements apart (a multiple of 8, and q 16-byte aligned).  A row that sees no position (a negative
- * kv_len, no valid page) is zero.  Rows of no sequence are not written.  max_len: the largest kv_len + window that the
+ * kv_len, no valid page) is zero.  A position that a row does not see adds nothing to it, whatever the cache holds there.  Scores, weights
+ * and sums are fp32, the weights that meet the values fp16 (eleven bits, of which out keeps eight); a value scale below 2^-80
+ * counts as 2^-80.  Rows of no sequence are not written.  out 16-byte aligned.  max_len: the largest kv_len + window that the
  * caller expects; it decides only how the work is split (0: the table's capacity).  workspace: device scratch for the
  * parts of long sequences, 16-byte aligned; with less than spec_kv8_workspace_bytes fewer parts are made (NULL: none). */
 size_t spec_kv8_workspace_bytes(int32_t rows, int32_t n_q_heads, int32_t head_dim);
@@ -114,7 +117,7 @@ int spec_kv8_attention(const spec_kv8_cache* cache, const void* q, int64_t ld_q,
  *     top_k:  its rank is below top_k[r]                                                    (top_k[r] <= 0: all)
  *     top_p:  the mass ranked before it is below top_p[r] times the mass that top_k leaves   (top_p[r] >= 1: all)
  *     min_p:  its mass is at least min_p[r] times the largest                                (min_p[r] <= 0: all)
- * (the first token always is).  temperature[r] <= 0 keeps the first token alone.  The token drawn is the first id whose
+ * (the first token always is).  temperature[r] <= 0 (or NaN) keeps the first token alone, a NaN in top_p or min_p all.  The token drawn is the first id whose
  * inclusive prefix sum of kept masses exceeds floor(uniforms[r] * kept mass).  Excluded logits may be -inf; a row
  * with a NaN, a +inf or no finite logit gives token -1, n_kept 0, logprob NaN and a filtered row of -inf. */
 typedef struct {
@@ -135,8 +138,9 @@ typedef struct {
     float* logits_out;           /* device fp32[rows][vocab], or NULL: the logits, -inf where not kept */
 } spec_filter_out;
 
-/* workspace: device scratch, 16-byte aligned, for rows shared out among workgroups; with less than
- * spec_filter_workspace_bytes a row is one workgroup's (NULL: none).  Calls that overlap in time need their own. */
+/* workspace: device scratch, 16-byte aligned, through which calls without top_k share a row out among workgroups; with less than
+ * spec_filter_workspace_bytes (0 where that would not pay) a row is one workgroup's (NULL: none).  Calls that overlap in time need
+ * their own. */
 size_t spec_filter_workspace_bytes(int32_t rows, int32_t vocab);
 int spec_filter_sample(const spec_filter_args* args, const spec_filter_out* out, void* workspace, size_t workspace_bytes,
                        void* stream);

@@ -2,6 +2,12 @@
 //
 // A token's mass is a whole number, so sums over any set are exact in whatever order they are taken.  Tokens are ranked by
 // falling logit and rising id; what top-k and top-p keep is a prefix of that order, i.e. everything up to a cut (key, id).
+//
+// Bound by what a workgroup does one thing after another, not by memory (64 rows of 128256 are 33 MB, 7 us).  With top-k few tokens
+// matter, and they are known after one pass: the k-th largest of the threads' own largest logits is a bound, what reaches it makes a
+// list (some dozen tokens for k = 50 of 32000), and the rest is work on that list: 17.5 us for one row of 32000 with its filtered
+// row, 27 for 64 rows of 128256 (38 with a histogram over the row).  A histogram of 4096 bins and the tokens of one of them find a cut in
+// longer lists and in whole rows; without top-k the passes over the row are shared out, see below.
 #include "q8.h"
 
 namespace specv {
