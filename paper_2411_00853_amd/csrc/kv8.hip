@@ -204,7 +204,7 @@ struct AttnArgs {
     int64_t ld_q;
     const int32_t* row0;
     const int32_t* kv_len;
-    int rows, group, parts, part_pages, tiles;   // part_pages: of each part but a sequence's last, which takes what is left
+    int rows, group, parts, part_pages, tiles, cus;   // part_pages: of each part but a sequence's last, which takes what is left
     float scale;          // of the scores, times log2(e)
     uint16_t* out;
     float* part_o;        // [rows][heads][parts][HD]
@@ -236,7 +236,10 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     __shared__ float2 ml[NW][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     // (heads fastest: consecutive workgroups go to different XCDs, and a part that many sequences lack would leave one of them idle)
-    const int b = blockIdx.z, hk = a.c.n_kv_heads, h = blockIdx.x % hk, q0 = (blockIdx.x / hk) * (16 * RT), part = blockIdx.y;
+    const int b = blockIdx.z, hk = a.c.n_kv_heads, h = blockIdx.x % hk, q0 = (blockIdx.x / hk) * (16 * RT);
+    // (A compute unit's second workgroup takes another part than its first, earlier parts are the longer ones: 106.5 us against 108.6 for 32
+    // sequences of 512 to 16384; all first parts first: 115.)
+    const int part = (int)((blockIdx.y + gridDim.x * gridDim.y * (unsigned)b / (unsigned)a.cus) % gridDim.y);
     int r0, w;
     if (!window_of(a.row0, b, a.rows, &r0, &w)) return;
     const int n_q = w * a.group;
@@ -508,8 +511,8 @@ void launch_attn(AttnArgs a, int batch, int max_window, int max_len, size_t ws_f
     const size_t each = (size_t)a.rows * hq * (HD + 2);
     // Parts of a sequence are workgroups of their own, joined by a second kernel (3 us): where there are fewer workgroups than compute units,
     // down to two pages a wavefront -- one sequence of 30000, 8 kv heads: 132 us in one part, 20 in 32; of 2048, 32 heads: 13.6 in one, 10.6
-    // in four; of 1024, 8 heads of 64: 6.7 in one, 8.4 in two -- and where sequences may differ by much (32 of 512 to 16384: 107 us in two
-    // parts, 115 in one, 120 in four).
+    // in four; of 1024, 8 heads of 64: 6.7 in one, 8.4 in two -- and where sequences may differ by much (32 of 512 to 16384: 106 us in two
+    // parts, 107 to 115 in one, 115 in four).
     int64_t parts = (pages + 128) / 256;
     if (wgs < cus && pages * HD > 32 * 128) parts = std::max(parts, std::min((cus + wgs - 1) / wgs, pages / (2 * NW)));
     parts = std::min(parts, (int64_t)std::min<size_t>(MAX_PARTS, ws_floats / each));
@@ -604,7 +607,7 @@ extern "C" int spec_kv8_attention(const spec_kv8_cache* cache, const void* q, in
     const int group = n_q_heads / cache->n_kv_heads;
     if ((int64_t)cache->n_kv_heads * (((int64_t)max_window * group + 15) / 16) > 0x7fffffff || (int64_t)rows * n_q_heads > 0x7fffffff)
         return fail(SPEC_ERR_SHAPE, "spec_kv8_attention: %d rows of %d heads are too many", rows, n_q_heads);
-    AttnArgs a{pages_of(cache), (const uint16_t*)q, ld_q, row0, kv_len, rows, group, 1, 1, 1, scale * 1.4426950408889634f, (uint16_t*)out, nullptr, nullptr};
+    AttnArgs a{pages_of(cache), (const uint16_t*)q, ld_q, row0, kv_len, rows, group, 1, 1, 1, compute_units(), scale * 1.4426950408889634f, (uint16_t*)out, nullptr, nullptr};
     const size_t ws = workspace ? workspace_bytes / sizeof(float) : 0;
     const int len = max_len ? std::min(max_len, cap) : cap;
     const int64_t n_q = (int64_t)max_window * group;
