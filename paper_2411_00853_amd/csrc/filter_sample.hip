@@ -85,6 +85,27 @@ struct Cut {        // tokens of a larger key are in, those of this key up to id
     }
 };
 
+// Larger orders are ranked before
+__device__ __forceinline__ u64 order_of(float l, int id) { return (u64)key_of(l) << 32 | (unsigned)~id; }
+__device__ __forceinline__ Cut cut_at(u64 order) { return {(unsigned)(order >> 32), (int)~(unsigned)order}; }
+// The values of a list (in LDS, its last eight filled up with zeros) up to an order.  All eight are read before one is looked at: read only
+// where they count, each would be waited for (153 tokens: 8.5 us, 3 this way).
+__device__ __forceinline__ u64 up_to(const u64* order, const u64* value, int n, u64 mine)
+{
+    u64 sum = 0;
+    for (int j = 0; j < n; j += 8) {
+        u64 other[8], v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            other[e] = order[j + e];
+            v[e] = value[j + e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += v[e] & (0 - (u64)(other[e] >= mine));
+    }
+    return sum;
+}
+
 struct Sums {
     u64 n, mass;
 };
@@ -93,9 +114,7 @@ struct Lds {
     u64 hist[BINS];
     float lx[LIST];
     int lid[LIST];
-    float sx[SMALL];
-    int sid[SMALL];
-    u64 sv[SMALL];
+    u64 small[SMALL], value[SMALL];
     unsigned count[TPB];
     u64 order[SHORT], ranked[SHORT], by_id[SHORT];
     Sums wave[WAVES];
@@ -307,20 +326,17 @@ __device__ bool shortest(const S& src, const Masses& m, Cut& c, u64 need, bool b
         if (!w) return;
         const int at = atomicAdd(&s.n_small, 1);
         if (at >= SMALL) return;
-        s.sx[at] = l;
-        s.sid[at] = i;
-        s.sv[at] = by_mass ? w : 1;
+        s.small[at] = order_of(l, i);
+        s.value[at] = by_mass ? w : 1;
     });
     __syncthreads();
     const int n = s.n_small;
     if (n > SMALL) return false;
+    if (threadIdx.x < 8 && n + threadIdx.x < SMALL) s.small[n + threadIdx.x] = s.value[n + threadIdx.x] = 0;   // (eight are read at a time)
+    __syncthreads();
     if ((int)threadIdx.x < n) {
-        const Cut me = {key_of(s.sx[threadIdx.x]), s.sid[threadIdx.x]};
-        const u64 v = s.sv[threadIdx.x];
-        u64 upto = above;
-        for (int j = 0; j < n; ++j)
-            if (me.has(s.sx[j], s.sid[j])) upto += s.sv[j];
-        if (upto >= need && upto - v < need) s.cut = me;
+        const u64 mine = s.small[threadIdx.x], upto = above + up_to(s.small, s.value, n, mine);
+        if (upto >= need && upto - s.value[threadIdx.x] < need) s.cut = cut_at(mine);
     }
     __syncthreads();
     c = s.cut;
@@ -504,19 +520,22 @@ __device__ __forceinline__ void short_list(const Row<T, NV, N>& r, const Masses&
             l = s.lx[tid];
             id = s.lid[tid];
             mass = m(l);
-            mine = (u64)key_of(l) << 32 | (unsigned)~id;   // larger: ranked before
+            mine = order_of(l, id);
         }
         s.order[tid] = mine;   // (behind the list: 0, which no comparison counts)
     }
     __syncthreads();
     if (works) {
-        for (int j = 0; j < n; j += 4)
+        for (int j = 0; j < n; j += 8) {
+            u64 other[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const u64 other = s.order[j + e];
-                rank += other > mine;
-                place += (unsigned)other > (unsigned)mine;
+            for (int e = 0; e < 8; ++e) other[e] = s.order[j + e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                rank += other[e] > mine;
+                place += (unsigned)other[e] > (unsigned)mine;
             }
+        }
         if (on) s.ranked[rank] = mass;
         else s.ranked[tid] = 0;
     }
@@ -940,16 +959,19 @@ __global__ void __launch_bounds__(TPB) part_draw_kernel(const T* __restrict__ lo
 {
     constexpr int N = Part<T>::N, CHUNK = Part<T>::CHUNK;
     __shared__ Lds s;
-    const int row = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_chunks = (vocab + CHUNK - 1) / CHUNK;
+    const int row = blockIdx.x, tid = threadIdx.x, n_chunks = (vocab + CHUNK - 1) / CHUNK;
     Shared& g = shared[row];
-    const float t0 = temperature ? temperature[row] : 1.f, u = uniforms[row];
+    // everything that the workspace has for this row, asked for at once: whether it is needed shows later
+    const u64 chunk_mass = tid < n_chunks ? g.chunk[tid] : 0, n_above = g.n_above, above = g.above, need = g.need;
+    const float t0 = temperature ? temperature[row] : 1.f, u = uniforms[row], first_l = g.lx[tid];
+    const int n_list = (int)g.n_list, first_id = g.lid[tid];
     const Results o = {tokens + row, logprob ? logprob + row : nullptr, n_kept ? n_kept + row : nullptr, out ? out + (size_t)row * vocab : nullptr};
     const Params a = {0, top_p ? top_p[row] : 1.f, least_mass(min_p, row)};
     Masses m;
     unsigned top;
     const bool any = masses_of(g, parts, t0, m, top);
     if (!any || !(t0 > 0.f)) {
-        if (threadIdx.x == 0) {
+        if (tid == 0) {
             *o.token = any ? (int)g.first : -1;
             if (o.logprob) *o.logprob = any ? 0.f : __uint_as_float(0x7fc00000u);
             if (o.n_kept) *o.n_kept = any;
@@ -959,40 +981,36 @@ __global__ void __launch_bounds__(TPB) part_draw_kernel(const T* __restrict__ lo
         return;
     }
     Cut c = {0, vocab - 1};
-    const int n = a.p < 1.f ? (int)g.n_list : 0;
+    const int n = a.p < 1.f ? n_list : 0;
     if (n > MANY) {   // as many equal logits make
         slow_row<T, N>(logits + (size_t)row * ld, vocab, m, a, u, o, s);
-        if (threadIdx.x == 0) g.done = 1;
+        if (tid == 0) g.done = 1;
         return;
     }
     if (a.p < 1.f) {
-        // each of the bin's tokens against each: larger orders are ranked before
-        const u64 above = g.above, need = g.need;
+        // each of the bin's tokens against each
         u64 *const order = s.hist, *const mass = s.hist + MANY;
         static_assert(2 * MANY <= BINS && MANY <= LIST, "the list's place");
-        const int n4 = (n + 3) & ~3;
-        for (int i = threadIdx.x; i < n4; i += TPB) {
-            const float l = i < n ? g.lx[i] : -INFINITY;
-            const int id = i < n ? g.lid[i] : 0;
+        const int n8 = (n + 7) & ~7;
+        for (int i = tid; i < n8; i += TPB) {
+            const float l = i >= n ? -INFINITY : i == tid ? first_l : g.lx[i];
+            const int id = i >= n ? 0 : i == tid ? first_id : g.lid[i];
             s.lx[i] = l;
             s.lid[i] = id;
-            order[i] = (u64)key_of(l) << 32 | (unsigned)~id;
+            order[i] = i < n ? order_of(l, id) : 0;
             mass[i] = m(l);
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < n; i += TPB) {
-            const u64 mine = order[i];
-            u64 upto = above;
-            for (int j = 0; j < n4; j += 4)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) upto += order[j + e] >= mine ? mass[j + e] : 0;
-            if (upto >= need && upto - mass[i] < need) s.cut = {key_of(s.lx[i]), s.lid[i]};
+        for (int i = tid; i < n; i += TPB) {
+            const u64 mine = order[i], upto = above + up_to(order, mass, n, mine);
+            if (upto >= need && upto - mass[i] < need) s.cut = cut_at(mine);
         }
         __syncthreads();
         c = s.cut;
     }
-    clear(s, 1024);
-    if ((int)threadIdx.x < n_chunks) s.hist[threadIdx.x] = g.chunk[threadIdx.x];
+    __syncthreads();
+    s.hist[tid] = chunk_mass;
+    static_assert(TPB == 1024, "a thread for each chunk");
     __syncthreads();
     u64 more = 0;
     for (int i = threadIdx.x; i < n; i += TPB) {
@@ -1002,8 +1020,8 @@ __global__ void __launch_bounds__(TPB) part_draw_kernel(const T* __restrict__ lo
         atomicAdd(&s.hist[s.lid[i] / CHUNK], w);
     }
     __syncthreads();
-    Sums kept = block_sums(more, s.hist[threadIdx.x], s);
-    kept.n += g.n_above;
+    Sums kept = block_sums(more, s.hist[tid], s);
+    kept.n += n_above;
     draw_from_chunks<T, N>(logits + (size_t)row * ld, vocab, m, a, c, u, kept, o, s);
     if (threadIdx.x == 0) {
         g.cut = c;
@@ -1042,8 +1060,8 @@ __global__ void __launch_bounds__(PART_TPB) part_write_kernel(const T* __restric
 // Workgroups a row; 1: the row is one workgroup's
 int parts_of(int rows, int vocab, int dtype)
 {
-    // us, one workgroup a row and shared out, top-p 0.9: 1 row of 8192 32 and 23, of 32000 98 and 26, of 128256 311 and 32; 64 rows of 128256
-    // 340 and 74; 256 rows of 32000 159 and 73.  No filter: 1 row of 8192 14 and 15, of 128256 123 and 19, 256 rows of 128256 178 and 147.
+    // us, one workgroup a row and shared out, top-p 0.9: 1 row of 8192 31 and 22, of 32000 96 and 25, of 128256 304 and 27; 64 rows of 128256
+    // 334 and 70; 256 rows of 32000 157 and 73.  No filter: 1 row of 8192 14 and 15, of 128256 123 and 19, 256 rows of 128256 178 and 147.
     const int chunk = 64 * (dtype == SPEC_DTYPE_BF16 ? 8 : 4);
     if (vocab < 8192 || rows > 256) return 1;
     return std::min(std::min(768 / rows, MAX_PARTS), vocab / (8 * chunk));
