@@ -5,8 +5,9 @@
 //
 // Bound by what a workgroup does one thing after another, not by memory (64 rows of 128256 are 33 MB, 7 us).  With top-k few tokens
 // matter, and they are known after one pass: the k-th largest of the threads' own largest logits is a bound, what reaches it makes a
-// list (some dozen tokens for k = 50 of 32000), and the rest is work on that list: 17.5 us for one row of 32000 with its filtered
-// row, 27 for 64 rows of 128256 (38 with a histogram over the row).  A histogram of 4096 bins and the tokens of one of them find a cut in
+// list (some dozen tokens for k = 50 of 32000), and the rest is work on that list: 9.6 us for one row of 32000 with its filtered
+// row, 21 for 64 rows of 128256 (38 with a histogram over the row).  A vector instruction costs the workgroup sixteen cycles, its sixteen
+// wavefronts four times four, so that what is done for each logit is counted in instructions.  A histogram of 4096 bins and the tokens of one of them find a cut in
 // longer lists and in whole rows; without top-k the passes over the row are shared out, see below.
 #include "q8.h"
 
@@ -20,6 +21,7 @@ constexpr int BINS = 4096;      // of falling logits, over the 31 nats in which 
 constexpr int LIST = 2048;      // tokens that may matter, where that few are known to
 constexpr int SMALL = 1024;     // tokens of the bin that a cut falls into
 constexpr int SHORT = 256;      // tokens of a list that is put in order at once
+constexpr int GROUPS = SPEC_FILTER_MAX_VOCAB / (TPB * 32);   // of 32 logits a thread
 constexpr float NATS = 31.f;    // exp(-31) * 2^44 < 1
 constexpr float HALF_ONE = 0x1p22f;
 constexpr u64 MASS_ONE = 1ull << 44;
@@ -65,6 +67,10 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
     v = max(v, dpp<DPP_BCAST31, 0xc>(v));
     return last_lane(v);
 }
+
+// What LDS holds for the whole workgroup, as a scalar: a branch on it is one, and what only one side needs is not kept through the other
+__device__ __forceinline__ int same_for_all(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ unsigned same_for_all(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
 
 // ---- what a workgroup knows of its row ----------------------------------------------------------------------------------
 // Ascending with the logit; -0 and 0 are one value
@@ -116,6 +122,7 @@ struct Lds {
     int lid[LIST];
     u64 small[SMALL], value[SMALL];
     unsigned count[TPB];
+    float most[GROUPS][TPB];        // of each group of loads of a row that is not kept in registers
     u64 order[SHORT], ranked[SHORT], by_id[SHORT];
     Sums wave[WAVES];
     unsigned tops[WAVES];
@@ -188,20 +195,28 @@ struct Row {
                 __builtin_amdgcn_sched_barrier(0);   // one load's masses at a time: side by side they do not fit the registers
             }
         } else {
-            constexpr int AHEAD = N >= 4 ? 32 / N : 8;
-            const int n = (vocab + TPB * N - 1) / (TPB * N);
-            for (int k = 0; k < n; k += AHEAD) {
-                Some<T, N> s[AHEAD];
+            for (int k = 0; k < loads(); k += AHEAD) group(k, true, f);
+        }
+    }
+    // NV = 0: the row goes by groups of AHEAD loads a thread
+    static constexpr int AHEAD = N >= 4 ? 32 / N : 8;
+    __device__ __forceinline__ int loads() const { return (vocab + TPB * N - 1) / (TPB * N); }
+    // each_vec's f for the group of load k; lanes that do not want it read a place that all of them read, and get -inf
+    template <typename F>
+    __device__ __forceinline__ void group(int k, bool want, F f) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        Some<T, N> s[AHEAD];
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) s[j] = fetch(k + j);
+        for (int j = 0; j < AHEAD; ++j) s[j] = *reinterpret_cast<const Some<T, N>*>(x + (want ? first_id(k + j) : 0));
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) {
-                    float l[N];
-                    widen(k + j, s[j], l);
-                    f((k + j) * WAVES + wave, first_id(k + j), l);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
+        for (int j = 0; j < AHEAD; ++j) {
+            float l[N];
+            widen(k + j, s[j], l);
+#pragma unroll
+            for (int e = 0; e < N; ++e) l[e] = want ? l[e] : -INFINITY;
+            f((k + j) * WAVES + wave, first_id(k + j), l);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     template <typename F>
@@ -272,7 +287,7 @@ __device__ __forceinline__ void clear(Lds& s, int n)
 
 // The shortest prefix that holds `need` (tokens, or mass), by bisection: for a bin of more tokens than SMALL, as many equal logits make
 template <typename S>
-__device__ Cut bisect(const S& src, const Masses& m, const Cut c, u64 need, bool by_mass, int vocab, Lds& s)
+__device__ __forceinline__ Cut bisect(const S& src, const Masses& m, const Cut c, u64 need, bool by_mass, int vocab, Lds& s)
 {
     auto value = [&](float l) {
         const u64 w = m(l);
@@ -308,7 +323,7 @@ __device__ Cut bisect(const S& src, const Masses& m, const Cut c, u64 need, bool
 // The same for a source that holds all tokens of logit `lowest` and more, where the prefix lies: a histogram of falling logits, and the
 // tokens of the bin that it ends in, each against each.  c holds as much as needed and becomes the cut; false: the bin is too full.
 template <typename S>
-__device__ bool shortest(const S& src, const Masses& m, Cut& c, u64 need, bool by_mass, float lowest, Lds& s)
+__device__ __forceinline__ bool shortest(const S& src, const Masses& m, Cut& c, u64 need, bool by_mass, float lowest, Lds& s)
 {
     clear(s, BINS);
     src.each([&](float l, int i) {
@@ -330,7 +345,7 @@ __device__ bool shortest(const S& src, const Masses& m, Cut& c, u64 need, bool b
         s.value[at] = by_mass ? w : 1;
     });
     __syncthreads();
-    const int n = s.n_small;
+    const int n = same_for_all(s.n_small);
     if (n > SMALL) return false;
     if (threadIdx.x < 8 && n + threadIdx.x < SMALL) s.small[n + threadIdx.x] = s.value[n + threadIdx.x] = 0;   // (eight are read at a time)
     __syncthreads();
@@ -373,7 +388,7 @@ __device__ __forceinline__ u64 share(float p, u64 mass) { return max((u64)ceil((
 
 // Top-k (if it cuts) and top-p within a source
 template <typename S>
-__device__ bool cuts(const S& src, const Masses& m, const Params& a, Cut& c, int vocab, Lds& s)
+__device__ __forceinline__ bool cuts(const S& src, const Masses& m, const Params& a, Cut& c, int vocab, Lds& s)
 {
     if (a.k <= 0 && !(a.p < 1.f)) return true;
     Sums all = within(src, m, c, s);
@@ -391,9 +406,10 @@ __device__ bool cuts(const S& src, const Masses& m, const Params& a, Cut& c, int
 
 // The row with -inf where `kept` says no
 template <typename T, int NV, int N, typename F>
-__device__ __forceinline__ void write_row(const Row<T, NV, N>& r, float* out, F kept)
+__device__ __forceinline__ void write_row(Row<T, NV, N> r, float* out, F kept)
 {
     if (!out) return;
+    asm("" : "+s"(r.vocab));   // (places counted anew: kept from the loads until here they would not fit the registers)
     r.each_vec([&](int chunk, int i0, const float* l) {
         const int want = (chunk * 64 + (int)(threadIdx.x & 63)) * N;
         if (want >= r.vocab) return;
@@ -449,17 +465,17 @@ __device__ __forceinline__ void draw_from_chunks(const T* x, int vocab, const Ma
     }
 }
 
-// The draw among the tokens of a cut, and the results.  `list` holds all of them, or is NULL.
+// The draw among the tokens of a cut, and the results.  `list` holds all of them if `listed`.
 template <typename T, int NV, int N>
-__device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List* list, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
+__device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List& list, bool listed, const Masses& m, const Params& a, const Cut& c, float u, const Results& o,
                                        Lds& s)
 {
     constexpr int CHUNK = Row<T, NV, N>::CHUNK;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     clear(s, 1024);   // the kept masses by chunk of ids
     u64 n = 0;
-    if (list) {
-        list->each([&](float l, int i) {
+    if (listed) {
+        list.each([&](float l, int i) {
             if (!c.has(l, i)) return;
             const u64 w = m(l);
             if (w < a.least) return;
@@ -489,11 +505,12 @@ __device__ __forceinline__ void finish(const Row<T, NV, N>& r, const List* list,
 }
 
 // Up to SHORT tokens that hold everything kept: each finds its place in the order of the logits and of the ids by looking at all
-// others, and everything else is two running sums.  Four wavefronts work, one a SIMD; the rest meet them at the barriers.
+// others, four threads a token, and everything else is two running sums, for which four wavefronts work, one a SIMD, and the
+// rest meet them at the barriers.
 template <typename T, int NV, int N>
-__device__ __forceinline__ void short_list(const Row<T, NV, N>& r, const Masses& m, const Params& a, float u, const Results& o, Lds& s)
+__device__ __forceinline__ void short_list(const Row<T, NV, N>& r, const Masses& m, const Params& a, float u, int n, const Results& o, Lds& s)
 {
-    const int n = s.n_list, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool works = wave < SHORT / 64, on = tid < n;
     u64* scan = s.hist;   // sums of the wavefronts
     auto running = [&](u64 v, int slot) {   // inclusive, over the SHORT threads (one barrier)
@@ -525,17 +542,24 @@ __device__ __forceinline__ void short_list(const Row<T, NV, N>& r, const Masses&
         s.order[tid] = mine;   // (behind the list: 0, which no comparison counts)
     }
     __syncthreads();
-    if (works) {
-        for (int j = 0; j < n; j += 8) {
-            u64 other[8];
+    {   // four threads an element
+        const u64 its = s.order[tid / 4];
+        unsigned found = 0;   // rank, and place in the upper half
+        for (int j = tid % 4 * 4; j < n; j += 16) {
+            u64 other[4];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) other[e] = s.order[j + e];
+            for (int e = 0; e < 4; ++e) other[e] = s.order[j + e];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                rank += other[e] > mine;
-                place += (unsigned)other[e] > (unsigned)mine;
-            }
+            for (int e = 0; e < 4; ++e) found += (other[e] > its) + ((unsigned)((unsigned)other[e] > (unsigned)its) << 16);
         }
+        found += dpp<DPP_XOR1, 0xf>(found);
+        found += dpp<DPP_XOR2, 0xf>(found);
+        if (tid % 4 == 0) s.count[tid / 4] = found;
+    }
+    __syncthreads();
+    if (works) {
+        rank = (int)(s.count[tid] & 0xffffu);
+        place = (int)(s.count[tid] >> 16);
         if (on) s.ranked[rank] = mass;
         else s.ranked[tid] = 0;
     }
@@ -583,7 +607,7 @@ __device__ __forceinline__ void slow_row(const T* x, int vocab, const Masses& m,
         all = within(r, m, c, s);
     }
     if (a.p < 1.f) c = bisect(r, m, c, share(a.p, all.mass), true, vocab, s);
-    finish(r, (const List*)nullptr, m, a, c, u, o, s);
+    finish(r, List{&s, 0}, false, m, a, c, u, o, s);
 }
 
 template <typename T, int NV, int N>
@@ -598,12 +622,15 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     Row<T, NV, N> r;
     r.x = logits + (size_t)row * ld;
     r.vocab = vocab;
+    // The parameters that are there, all asked for before the first is waited for (one that is not is read in a place that is)
+    const float t_read = (temperature ? temperature : uniforms)[row], p_read = (top_p ? top_p : uniforms)[row];
+    const float mp_read = (min_p ? min_p : uniforms)[row], u = uniforms[row];
+    const int k_read = (top_k ? top_k : (const int32_t*)uniforms)[row];
     r.load();
-    const float t0 = temperature ? temperature[row] : 1.f, u = uniforms[row];
+    const float t0 = temperature ? t_read : 1.f, mp = min_p ? mp_read : 0.f;
     Params a;
-    a.k = t0 > 0.f ? top_k ? top_k[row] : 0 : 1;
-    a.p = top_p ? top_p[row] : 1.f;
-    const float mp = min_p ? min_p[row] : 0.f;
+    a.k = t0 > 0.f ? top_k ? k_read : 0 : 1;
+    a.p = top_p ? p_read : 1.f;
     a.least = mp > 0.f ? max((u64)ceil(fmin((double)mp, 1.0) * (double)MASS_ONE), (u64)1) : 1;
 
     // The largest logit, each thread's own, and whether the row holds a NaN or a +inf: by their bits, of which three are looked at at a time.
@@ -611,15 +638,24 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     // logit; a negative NaN is the largest unsigned.
     int most_signed = (int)0x80000000;
     unsigned most = 0, least_bits = 0xffffffffu;
-    r.each_vec([&](int, int, const float* l) {
+    float most_here = -INFINITY;
+    auto look = [&](int, int, const float* l) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const unsigned b = __float_as_uint(l[e]);
             most_signed = max(most_signed, (int)b);
             most = max(most, b);
             least_bits = min(least_bits, b);
+            most_here = fmaxf(most_here, l[e]);
         }
-    });
+    };
+    if constexpr (NV > 0) r.each_vec(look);
+    else
+        for (int k = 0; k < r.loads(); k += r.AHEAD) {
+            r.group(k, true, look);
+            s.most[k / r.AHEAD][threadIdx.x] = most_here;
+            most_here = -INFINITY;
+        }
     const bool bad = most_signed >= 0x7f800000 || most > 0xff800000u;
     const float mine = __uint_as_float(most_signed >= 0 ? (unsigned)most_signed : least_bits);
     {
@@ -634,6 +670,7 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     unsigned top = 0;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) top = max(top, s.tops[w]);
+    top = same_for_all(top);
     Masses m;
     m.top = logit_of(top);
     if (top == 0xffffffffu || !(m.top > -INFINITY)) {
@@ -675,6 +712,7 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
         return;
     }
     bool listed = false;
+    int n_list = 0;
     if (a.k > 1 && a.k <= TPB) {
         // The k-th largest of the threads' largest logits is at most the k-th largest of all: what is as large makes the list.  (By
         // bins of 31 / 1024 nats, one a thread: the k-th is the smallest in its bin at the latest.)
@@ -700,44 +738,72 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
         if (some && !few && bin <= s.bin) atomicMin(&s.least_key, key_of(mine));
         __syncthreads();
         const float least = few ? -0x1.fffffep127f : logit_of(s.least_key);
-        const int least_pos = least > 0.f ? __float_as_int(least) : 0x7fffffff;   // bits of numbers above 0 rise with them
-        r.each_vec([&](int, int i0, const float* l) {
-            int m0 = __float_as_int(l[0]);
-#pragma unroll
-            for (int e = 1; e < N; ++e) m0 = max(m0, __float_as_int(l[e]));
-            bool any = m0 >= least_pos;
-            if (least <= 0.f)
-#pragma unroll
-                for (int e = 0; e < N; ++e) any |= l[e] >= least;
-            if (!__any(any)) return;
-            int n = 0;
-#pragma unroll
-            for (int e = 0; e < N; ++e) n += l[e] >= least;
-            const unsigned upto = wave_scan((unsigned)n);
+        // Each wavefront lists its own first, in a place that it has in s.hist: no lane waits for a count to come back.  A lane looks at up to 32
+        // logits, a bit each, and what it found is read again: a hit or two, where logit by logit every lane would go through the motions
+        // of listing for any other lane's (64 rows of 128256: 23.3 us that way).
+        constexpr int OWN = BINS / WAVES;
+        u64* const own = s.hist + wave * OWN;
+        int n_own = 0;
+        auto hand_over = [&]() {
             int at = 0;
-            if (lane == 63) at = atomicAdd(&s.n_list, (int)upto);
-            at = __builtin_amdgcn_readlane(at, 63) + (int)upto - n;
+            if (lane == 0) at = atomicAdd(&s.n_list, n_own);
+            at = __builtin_amdgcn_readfirstlane(at);
+            for (int i = lane; i < n_own && at + i < LIST; i += 64) {
+                s.lx[at + i] = __uint_as_float((unsigned)(own[i] >> 32));
+                s.lid[at + i] = (int)own[i];
+            }
+            n_own = 0;
+        };
+        unsigned found;
+        int at_bit;
+        auto look_again = [&](int, int, const float* l) {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (l[e] >= least) {
-                    if (at < LIST) {
-                        s.lx[at] = l[e];
-                        s.lid[at] = i0 + e;
-                    }
-                    ++at;
+            for (int e = 0; e < N; ++e) found |= (unsigned)(l[e] >= least) << (at_bit + e);
+            at_bit += N;
+        };
+        auto collect = [&](int k) {
+            u64 which;
+            while ((which = __ballot(found != 0)) != 0) {
+                const int n = __popcll(which), bit = __builtin_ctz(found | 0x80000000u), id = r.first_id(k + bit / N) + bit % N;
+                if (n_own + n > OWN) hand_over();
+                if (found) {
+                    const int at = n_own + __builtin_amdgcn_mbcnt_hi((unsigned)(which >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)which, 0));
+                    own[at] = (u64)__float_as_uint(q8_widen(r.x[id])) << 32 | (unsigned)id;
                 }
-        });
+                n_own += n;
+                found &= found - 1;
+            }
+        };
+        static_assert(NV * N <= 32, "a bit each");
+        for (int k = 0; k < (NV ? 1 : r.loads()); k += r.AHEAD) {
+            found = 0;
+            at_bit = 0;
+            if constexpr (NV > 0) {
+                r.each_vec(look_again);
+            } else {   // only lanes that hold one read again
+                const bool mine = s.most[k / r.AHEAD][threadIdx.x] >= least;
+                if (!__any(mine)) continue;
+                r.group(k, mine, look_again);
+            }
+            collect(k);
+        }
+        hand_over();
         __syncthreads();
-        listed = s.n_list <= LIST;
+        n_list = same_for_all(s.n_list);
+        listed = n_list <= LIST;
         if (!few) c.key = s.least_key;   // no token outside the list is in
     }
-    if (listed && s.n_list <= SHORT) {
-        short_list(r, m, a, u, o, s);
+    if (listed && n_list <= SHORT) {
+        short_list(r, m, a, u, n_list, o, s);
         return;
     }
-    const List list = {&s, s.n_list};
-    if (listed ? cuts(list, m, a, c, vocab, s) : cuts(r, m, a, c, vocab, s)) finish(r, listed ? &list : nullptr, m, a, c, u, o, s);
-    else slow_row<T, N>(r.x, vocab, m, a, u, o, s);
+    // From here on the row is read again: its registers would not be registers if whatever follows held on to them.
+    const T* x = r.x;
+    asm("" : "+s"(x));   // (or the compiler knows what it would read)
+    const List list = {&s, n_list};
+    const Row<T, 0, N> again = {x, vocab, {}};
+    if (listed ? cuts(list, m, a, c, vocab, s) : cuts(again, m, a, c, vocab, s)) finish(again, list, listed, m, a, c, u, o, s);
+    else slow_row<T, N>(x, vocab, m, a, u, o, s);
 }
 
 // ---- rows shared out among workgroups -------------------------------------------------------------------------------------
@@ -1058,12 +1124,13 @@ __global__ void __launch_bounds__(PART_TPB) part_write_kernel(const T* __restric
 }
 
 // Workgroups a row; 1: the row is one workgroup's
-int parts_of(int rows, int vocab, int dtype)
+int parts_of(int rows, int vocab, int dtype, bool top_p)
 {
-    // us, one workgroup a row and shared out, top-p 0.9: 1 row of 8192 31 and 22, of 32000 96 and 25, of 128256 304 and 27; 64 rows of 128256
-    // 334 and 70; 256 rows of 32000 157 and 73.  No filter: 1 row of 8192 14 and 15, of 128256 123 and 19, 256 rows of 128256 178 and 147.
+    // us, one workgroup a row and shared out, top-p 0.9: 1 row of 8192 29 and 22, of 32000 48 and 25, of 128256 160 and 27; 64 rows of 32000
+    // 50 and 42, of 128256 168 and 70; 256 rows of 32000 58 and 71.  No filter: 1 row of 8192 14 and 15, of 32000 24 and 17, of
+    // 128256 78 and 19; 64 rows of 128256 84 and 45, 256 rows 120 and 145.
     const int chunk = 64 * (dtype == SPEC_DTYPE_BF16 ? 8 : 4);
-    if (vocab < 8192 || rows > 256) return 1;
+    if (vocab < (top_p ? 8192 : 16384) || rows > 128) return 1;
     return std::min(std::min(768 / rows, MAX_PARTS), vocab / (8 * chunk));
 }
 
@@ -1106,7 +1173,7 @@ using namespace specv;
 extern "C" size_t spec_filter_workspace_bytes(int32_t rows, int32_t vocab)
 {
     // (of either type: fp32 rows are shared out among more workgroups)
-    return rows > 0 && vocab > 0 && parts_of(rows, vocab, SPEC_DTYPE_FP32) > 1 ? (size_t)rows * sizeof(Shared) : 0;
+    return rows > 0 && vocab > 0 && parts_of(rows, vocab, SPEC_DTYPE_FP32, true) > 1 ? (size_t)rows * sizeof(Shared) : 0;
 }
 
 extern "C" int spec_filter_sample(const spec_filter_args* a, const spec_filter_out* o, void* workspace, size_t workspace_bytes, void* stream)
@@ -1119,7 +1186,7 @@ extern "C" int spec_filter_sample(const spec_filter_args* a, const spec_filter_o
     if (!a->rows) return SPEC_OK;
     if (!a->logits || !a->uniforms || !o->tokens) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: null pointer");
     if ((uintptr_t)workspace & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_filter_sample: the workspace is not 16-byte aligned");
-    const int parts = !a->top_k && workspace && workspace_bytes >= a->rows * sizeof(Shared) ? parts_of(a->rows, a->vocab, a->dtype) : 1;
+    const int parts = !a->top_k && workspace && workspace_bytes >= a->rows * sizeof(Shared) ? parts_of(a->rows, a->vocab, a->dtype, a->top_p != nullptr) : 1;
     const bool bf16 = a->dtype == SPEC_DTYPE_BF16;
     if (parts > 1 && bf16) launch_parts<uint16_t>(a, o, parts, (Shared*)workspace, (hipStream_t)stream);
     else if (parts > 1) launch_parts<float>(a, o, parts, (Shared*)workspace, (hipStream_t)stream);
