@@ -115,19 +115,26 @@ __global__ void __launch_bounds__(1024) norm_kernel(const TX* x, const TD* __res
         const int col = (k * blockDim.x + threadIdx.x) * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[k][i] = 0.f;
-        if (col >= cols) continue;
-        load_cols(xr, col, cols, h[k]);
-        if (delta) {
-            float d[8];
-            load_cols(delta + (size_t)row * cols, col, cols, d);
+        if (col < cols) {
+            load_cols(xr, col, cols, h[k]);
+            if (delta) {
+                float d[8];
+                load_cols(delta + (size_t)row * cols, col, cols, d);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[k][i] += d[i];
-        }
-        if (x_out) {
-            TX* o = x_out + (size_t)row * cols + col;
-            if (col + 8 <= cols) store8<TX>(o, h[k]);
-            else
-                for (int i = 0; i < cols - col; ++i) o[i] = narrow<TX>(h[k][i]);
+                for (int i = 0; i < 8; ++i) h[k][i] += d[i];
+            }
+            if (x_out) {
+                TX* o = x_out + (size_t)row * cols + col;
+                if (col + 8 <= cols) {
+                    store8<TX>(o, h[k]);
+                } else if constexpr (NV == 1) {
+                    for (int i = 0; i < cols - col; ++i) o[i] = narrow<TX>(h[k][i]);
+                } else {   // (an index that is no constant would put all of h into memory: 64 rows of 65536 47 us, 25 this way)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (col + i < cols) o[i] = narrow<TX>(h[k][i]);
+                }
+            }
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += h[k][i] * h[k][i];

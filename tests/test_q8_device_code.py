@@ -3,10 +3,13 @@
 * The operands of a 16x16x128 product are eight registers each.  Where such operands are carried round a loop, the compiler has
   placed a product's result over an operand that a later product still read: the sums were wrong for some tile shapes only.
   The source hides each operand's origin from the compiler (Block<uint16_t>::op); here the code is searched for what it prevents.
+* Arrays of a thread are registers, not memory of its own.
 * The product takes eight passes: twelve wait states before another vector instruction reads its result."""
+import re
+
 import pytest
 
-from test_device_code import Code, _is_store, _regs, _vector, fewest_wait_states, kernels, objects  # noqa: F401
+from test_device_code import Code, _is_store, _regs, _tool, _vector, fewest_wait_states, kernels, objects  # noqa: F401
 
 WAIT_STATES = 12
 
@@ -77,3 +80,16 @@ def test_a_result_over_its_operand_alone_is_no_fault():
     lines = ["v_mfma_f32_16x16x128_f8f6f4 v[8:11], v[8:15], v[16:23], 0", "v_mfma_f32_16x16x128_f8f6f4 v[40:43], v[32:39], v[24:31], 0"]
     text = ["\t%s // %012X: 00000000" % (l, 0x100 + 8 * i) for i, l in enumerate(lines)]
     assert not overwritten_operands(Code("f", text))
+
+
+def test_no_8_bit_or_draw_kernel_has_private_memory(objects):
+    """A thread's arrays are registers.  A row of logits that a function was called with was not: it lay in memory, at half the speed."""
+    ours = ("rows_kernel", "norm_kernel", "skinny_kernel", "tiled_kernel", "append_kernel", "attn8_kernel", "join_kernel", "filter_kernel", "part_")
+    seen = {}
+    for o in objects:
+        notes = _tool("llvm-readelf", "--notes", o)
+        for name, size in re.findall(r"\.name:\s+(\S+).*?\.private_segment_fixed_size:\s+(\d+)", notes, re.S):
+            if any(k in name for k in ours) and "rope_append" not in name:
+                seen[name] = int(size)
+    assert len(seen) > 40
+    assert not {n: v for n, v in seen.items() if v}
