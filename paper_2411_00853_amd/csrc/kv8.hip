@@ -83,9 +83,9 @@ __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __re
     static_assert(AT_ONCE >= PAGE, "a page's positions at once");
     __shared__ unsigned top[2][APPEND_TPB / 64];
     const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, hk = c.n_kv_heads, hq = hk * group, oct = tid % OCTETS, d = oct * 8;
+    const int n = kv_len[b], ld = (hq + 2 * hk) * HD;
     int r0, w;
     if (!window_of(row0, b, rows, &r0, &w)) return;
-    const int n = kv_len[b], ld = (hq + 2 * hk) * HD;
     const int limit = min(c.blocks * PAGE, cos_sin ? max_pos : 0x7fffffff);   // positions there is a place for
     if ((int)blockIdx.x >= pages) {
         const int i = ((int)blockIdx.x - pages) * AT_ONCE + tid / OCTETS, j = i / group, head = h * group + i % group;
@@ -240,11 +240,15 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     // (A compute unit's second workgroup takes another part than its first, earlier parts are the longer ones: 106.5 us against 108.6 for 32
     // sequences of 512 to 16384; all first parts first: 115.)
     const int part = (int)((blockIdx.y + gridDim.x * gridDim.y * (unsigned)b / (unsigned)a.cus) % gridDim.y);
+    // Asked for at once: the window, the length, and the numbers of the first pages, which the part decides
+    const int c0 = part * a.part_pages, given = a.kv_len[b];
+    const int32_t* pages = a.c.table + (size_t)b * a.c.blocks;
+    const int first_page = pages[min(c0 + wave + lane * NW, a.c.blocks - 1)];
     int r0, w;
     if (!window_of(a.row0, b, a.rows, &r0, &w)) return;
     const int n_q = w * a.group;
     if (q0 >= n_q) return;
-    const int cap = a.c.blocks * PAGE, given = a.kv_len[b], n = min(given, cap);
+    const int cap = a.c.blocks * PAGE, n = min(given, cap);
     const int j_lo = q0 / a.group, j_hi = min(n_q - 1, q0 + 16 * RT - 1) / a.group;
     const int len = given < 0 ? 0 : (int)min((long)n + j_hi + 1, (long)cap), n_blk = (len + PAGE - 1) / PAGE;
     if (part > 0 && part * a.part_pages >= n_blk) {   // nothing to do: says so
@@ -254,7 +258,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
         }
         return;
     }
-    const int c0 = part * a.part_pages, c1 = part == a.parts - 1 ? n_blk : min(n_blk, c0 + a.part_pages);
+    const int c1 = part == a.parts - 1 ? n_blk : min(n_blk, c0 + a.part_pages);
 
     q8_bf16x8 qf[RT][KC][2];
     int lim[RT];
@@ -280,7 +284,6 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[t][d] = zero;
     }
-    const int32_t* pages = a.c.table + (size_t)b * a.c.blocks;
     struct Page {
         q8_intx4 k[2][KC], v[DT / 2];
     };
@@ -393,7 +396,8 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     // This wavefront's next 64 pages, one a lane: their numbers and scales.  A page that is not there is read as page 0 and left out.
     for (int first_blk = c0 + wave; first_blk < c1; first_blk += 64 * NW) {
         const int blk = first_blk + lane * NW, n_mine = min(64, (c1 - first_blk + NW - 1) / NW);
-        int page = blk < c1 ? pages[blk] : -1;
+        int page = first_blk == c0 + wave ? first_page : pages[min(blk, c1 - 1)];
+        page = blk < c1 ? page : -1;
         const bool there = page >= 0 && page < a.c.n_pages;
         page = there ? page : 0;
         const float2 s2 = *reinterpret_cast<const float2*>(a.c.scales + ((size_t)page * hk + h) * 2);

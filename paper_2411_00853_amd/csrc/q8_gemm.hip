@@ -105,7 +105,8 @@ constexpr int TILE = 16 * SPEC_Q8_BLOCK;   // bytes of a 16 x 128 tile of W
 // ---- few rows: the stream of W ------------------------------------------------------------------------------------------
 //
 // A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out the blocks of K and add their sums up in LDS.  Both
-// operands go straight into registers, the next block's while this one's products run.
+// operands go straight into registers, the next block's while this one's products run.  Bound by the stream of W: one row of
+// 22016 x 4096 in 15.7 us (5.7 TB/s), 8 of 12288 x 4096 in 10.2 (5.0); below some 20 MB by latency: one row of 4096 x 4096 4.8 us.
 template <int RT, int NT, int WAVES, typename T>
 __global__ void __launch_bounds__(64 * WAVES) skinny_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ w, const float* __restrict__ sx,
                                                      const float* __restrict__ sw, T* __restrict__ y, int M, int N, int n_blocks, int n_tiles)
