@@ -136,6 +136,13 @@ struct Lds {
 // with it gives what a division does, at a third of the instructions.
 struct Masses {
     float top, t, r, per_nat;   // per_nat: bins of one unit of logit
+    // (Were 1 / t infinite, as it is for a t of 2^-128 and less, the top's own quotient would be 0 * inf and no token would have mass.)
+    __device__ __forceinline__ void set(float temperature)
+    {
+        t = temperature > 0.f ? fminf(fmaxf(temperature, 0x1p-126f), 0x1.fffffep127f) : 1.f;
+        r = 1.f / t;
+        per_nat = fminf((float)BINS / (NATS * t), 0x1.fffffep127f);
+    }
     __device__ __forceinline__ u64 operator()(float l) const
     {
         const float d = l - top, q = d * r;
@@ -257,6 +264,7 @@ __device__ __forceinline__ Sums block_sums(u64 n, u64 mass, Lds& s)
 }
 
 // The entry of hist[0 .. n) (n a multiple of TPB) in which the running sum reaches `need`, and the sum before it, to s.bin and s.above
+// (the first entry, should none reach it)
 __device__ __forceinline__ void crossing(Lds& s, int n, u64 need)
 {
     const int per = n / TPB, i0 = threadIdx.x * per, wave = threadIdx.x >> 6;
@@ -265,6 +273,10 @@ __device__ __forceinline__ void crossing(Lds& s, int n, u64 need)
     const u64 upto = wave_scan(mine);
     __syncthreads();
     if ((threadIdx.x & 63) == 63) s.wave[wave].n = upto;
+    if (threadIdx.x == 0) {
+        s.bin = 0;
+        s.above = 0;
+    }
     __syncthreads();
     u64 before = upto - mine;
     for (int w = 0; w < wave; ++w) before += s.wave[w].n;
@@ -347,6 +359,7 @@ __device__ __forceinline__ bool shortest(const S& src, const Masses& m, Cut& c, 
     __syncthreads();
     const int n = same_for_all(s.n_small);
     if (n > SMALL) return false;
+    if (threadIdx.x == 0) s.cut = c;
     if (threadIdx.x < 8 && n + threadIdx.x < SMALL) s.small[n + threadIdx.x] = s.value[n + threadIdx.x] = 0;   // (eight are read at a time)
     __syncthreads();
     if ((int)threadIdx.x < n) {
@@ -665,6 +678,7 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
     if (threadIdx.x == 0) {
         s.n_list = 0;
         s.n_small = 0;
+        s.bin = 0;
         s.least_key = 0xffffffffu;
     }
     __syncthreads();
@@ -684,9 +698,7 @@ __global__ void __launch_bounds__(TPB) filter_kernel(const T* __restrict__ logit
             for (int i = threadIdx.x; i < vocab; i += TPB) out[(size_t)row * vocab + i] = -INFINITY;
         return;
     }
-    m.t = t0 > 0.f ? fminf(t0, 0x1.fffffep127f) : 1.f;
-    m.r = 1.f / m.t;
-    m.per_nat = (float)BINS / (NATS * m.t);
+    m.set(t0);
 
     Cut c = {0, vocab - 1};
     if (a.k == 1) {   // the first token alone
@@ -915,9 +927,7 @@ __device__ __forceinline__ bool masses_of(const Shared& g, int parts, float t0, 
     const int lane = threadIdx.x & 63;
     top = wave_max(lane < parts ? g.tops[lane] : 0u);
     m.top = logit_of(top);
-    m.t = t0 > 0.f ? fminf(t0, 0x1.fffffep127f) : 1.f;
-    m.r = 1.f / m.t;
-    m.per_nat = (float)BINS / (NATS * m.t);
+    m.set(t0);
     return top != 0xffffffffu && m.top > -INFINITY;
 }
 __device__ __forceinline__ u64 least_mass(const float* min_p, int row)
@@ -1008,6 +1018,7 @@ __global__ void __launch_bounds__(PART_TPB) part_masses_kernel(const T* __restri
         for (int i = 0; i < PER; ++i) mine += h[i] = g.hist[threadIdx.x * PER + i];
         const u64 upto = wave_scan(mine);
         if (lane == 63) waves[wave] = upto;
+        if (threadIdx.x == 0) cut_bin = BINS;
         __syncthreads();
         u64 all = 0, before = upto - mine;
         for (int w = 0; w < PART_WAVES; ++w) {
@@ -1101,6 +1112,7 @@ __global__ void __launch_bounds__(TPB) part_draw_kernel(const T* __restrict__ lo
         // each of the bin's tokens against each
         u64 *const order = s.hist, *const mass = s.hist + MANY;
         static_assert(2 * MANY <= BINS && MANY <= LIST, "the list's place");
+        if (tid == 0) s.cut = c;
         const int n8 = (n + 7) & ~7;
         for (int i = tid; i < n8; i += TPB) {
             const float l = i >= n ? -INFINITY : i == tid ? first_l : g.lx[i];
