@@ -460,7 +460,7 @@ def _native():
     if _native_module is None:
         L = lib()
         if not os.path.exists(_build.NATIVE):
-            _build.build_library()
+            _build.build_native()
         from . import _native as m
         m.bind(*(C.cast(f, C.c_void_p).value for f in (L.spec_q8_quantize, L.spec_q8_add_rmsnorm, L.spec_q8_swiglu, L.spec_q8_gemm,
                                                        L.spec_kv8_append, L.spec_kv8_attention, L.spec_filter_sample)))

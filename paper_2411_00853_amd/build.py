@@ -1,5 +1,5 @@
 """Builds libspecverify.so (HIP, gfx950) in-tree with hipcc, and _native.so, the marshalling of tensors for its shortest
-calls, with the host compiler."""
+calls, with the host compiler.  The library needs neither that compiler nor the headers of torch and Python."""
 from __future__ import annotations
 
 import os
@@ -42,55 +42,65 @@ def _native_command() -> list:
 
     import torch
     base = os.path.dirname(torch.__file__)
-    cxx = shutil.which("g++") or shutil.which("c++") or "g++"
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        raise RuntimeError("no host compiler found: cannot build _native.so")
     return [cxx, "-std=c++17", "-O2", "-shared", "-fPIC", "-DUSE_ROCM", "-D__HIP_PLATFORM_AMD__=1",
             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{base}/include",
             f"-I{base}/include/torch/csrc/api/include", f"-I{sysconfig.get_paths()['include']}", "-o", NATIVE,
             os.path.join(CSRC, "native.cpp"), f"-L{base}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]
 
 
-def sources_newer_than_lib() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(NATIVE):
+def sources_newer_than_lib(built: str = LIB) -> bool:
+    if not os.path.exists(built):
         return True
-    t = min(os.path.getmtime(LIB), os.path.getmtime(NATIVE))
+    t = os.path.getmtime(built)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + \
            [os.path.join(HERE, "..", "include", f) for f in os.listdir(os.path.join(HERE, "..", "include"))]
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _report(r, verbose: bool) -> None:
+    noise = "packed-fp32-ops"
+    if verbose or r.returncode:
+        print("\n".join(l for l in (r.stdout + r.stderr).splitlines() if noise not in l and l.strip()))
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
-    if not force and not sources_newer_than_lib():
+    if not force and not sources_newer_than_lib(LIB):
         return LIB
     os.makedirs(OBJ_DIR, exist_ok=True)
     hipcc = _hipcc()
-    noise = "packed-fp32-ops"
-
-    def report(r):
-        if verbose or r.returncode:
-            print("\n".join(l for l in (r.stdout + r.stderr).splitlines() if noise not in l and l.strip()))
 
     def compile_one(src):
         obj = os.path.join(OBJ_DIR, src.replace(".hip", ".o"))
         cmd = [hipcc] + FLAGS + SOURCE_FLAGS.get(src, []) + ["-c", "-o", obj, os.path.join(CSRC, src)]
         return obj, subprocess.run(cmd, capture_output=True, text=True)
 
-    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES) + 1)) as pool:   # one compiler process per source
-        native = pool.submit(subprocess.run, _native_command(), capture_output=True, text=True)
+    with ThreadPoolExecutor(max_workers=min(8, len(SOURCES))) as pool:   # one hipcc process per source
         done = list(pool.map(compile_one, SOURCES))
     for _, r in done:
-        report(r)
-    report(native.result())
+        _report(r, verbose)
     if any(r.returncode for _, r in done):
         raise RuntimeError("hipcc failed building libspecverify.so")
-    if native.result().returncode:
-        raise RuntimeError("the host compiler failed building _native.so")
     r = subprocess.run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + [o for o, _ in done],
                        capture_output=True, text=True)
-    report(r)
+    _report(r, verbose)
     if r.returncode:
         raise RuntimeError("hipcc failed linking libspecverify.so")
     return LIB
 
 
+def build_native(force: bool = False, verbose: bool = False) -> str:
+    if not force and not sources_newer_than_lib(NATIVE):
+        return NATIVE
+    r = subprocess.run(_native_command(), capture_output=True, text=True)
+    _report(r, verbose)
+    if r.returncode:
+        raise RuntimeError("the host compiler failed building _native.so")
+    return NATIVE
+
+
 if __name__ == "__main__":
     print(build_library(force=True, verbose=True))
+    print(build_native(force=True, verbose=True))
