@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __re
 // for behind its last use: 37.7 us for the first of the two, with the append, against 29); and what runs meanwhile is little: two conversions
 // and four products of 16 rows for each 1 KiB.
 
-constexpr float REF_NONE = -1e30f;
+constexpr float REF_NONE = -0x1.fffffep127f;   // no score is below it
 constexpr float REF_SLACK = 15.f, REF_BELOW = 6.f;
 constexpr float LOG2_VS_LEAST = -80.f;
 
