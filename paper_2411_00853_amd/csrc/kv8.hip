@@ -185,8 +185,13 @@ __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __re
 // values are exact in it too, and the weights keep eleven bits.
 //
 // The scale of a page's values goes into the exponent: the weight that meets the values is exp2(t - ref) with t = score + log2(vs),
-// and the sum of weights takes it times 1/vs.  So there is one running reference, of the products' magnitude, and fp16
-// holds weights from 2^15 down to 2^-14 above its small numbers: the reference moves only when a weight would pass 2^15.
+// and the sum of weights takes it times base/vs, with base the scale of the wavefront's first page.  So there is one running reference, of
+// the products' magnitude, and fp16 holds weights from 2^15 down to 2^-14 above its small numbers: the reference moves only when a weight
+// would pass 2^15.  Scales further apart than 2^+-40 from base would leave weights out of the sum (2^-126 is the least that an exponential
+// gives): from the first such page on a wavefront takes t = score + log2(base) against the reference, sums that, and the factor vs/base
+// of the weights that meet the values has a running reference of its own, `lift`.  In either case
+//     sum of weights = sum * 2^(ref - log2(base)),   O = o * 2^(ref + lift),   out = o / sum * 2^(lift + log2(base)),
+// and results are joined by S = ref - log2(base) and E = lift + log2(base), small numbers that no large score swallows.
 //
 // Bound by the stream of the cache: 8 sequences of 2048 with 32 kv heads of 128, 136 MB in 24 us (5.6 TB/s); 32 of 512 to 16384 with 8, 549 MB
 // in 104 us (5.3 TB/s).  So every byte is read once for all query heads and window rows that share it; a page's registers are
@@ -196,7 +201,33 @@ __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __re
 
 constexpr float REF_NONE = -0x1.fffffep127f;   // no score is below it
 constexpr float REF_SLACK = 15.f, REF_BELOW = 6.f;
-constexpr float LOG2_VS_LEAST = -80.f;
+constexpr float LOG2_VS_LEAST = -80.f, LOG2_VS_APART = 40.f;
+
+// A result over some positions: the sum of weights is sum * 2^s, the weighted sum of values o * 2^(s + e)
+struct Partial {
+    float s, sum, e, unused;
+};
+// Joined: o = sum of o_k * weight_k, out = o * factor(o) (in two steps: 2^most is no fp32 number for the largest scales)
+template <typename F>
+__device__ __forceinline__ void join_references(int n, F part, float* top, float* most, float* den)
+{
+    *top = REF_NONE;
+    for (int k = 0; k < n; ++k) *top = fmaxf(*top, part(k).s);
+    *most = REF_NONE;
+    *den = 0.f;
+    for (int k = 0; k < n; ++k) {
+        const Partial x = part(k);
+        *den = fmaf(x.sum, __builtin_amdgcn_exp2f(x.s - *top), *den);
+        *most = x.sum == 0.f ? *most : fmaxf(*most, x.s - *top + x.e);
+    }
+}
+__device__ __forceinline__ float join_weight(const Partial& x, float top, float most) { return x.sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(x.s - top + x.e - most); }
+__device__ __forceinline__ uint2 finished(const q8_floatx4& o, float most, float den)
+{
+    const float up = exp2f(0.5f * most), f = den == 0.f ? 0.f : up / den;
+    return make_uint2(q8_round_bf16(o[0] * up * f) | (unsigned)q8_round_bf16(o[1] * up * f) << 16,
+                      q8_round_bf16(o[2] * up * f) | (unsigned)q8_round_bf16(o[3] * up * f) << 16);
+}
 
 struct AttnArgs {
     Pages c;
@@ -208,7 +239,7 @@ struct AttnArgs {
     float scale;          // of the scores, times log2(e)
     uint16_t* out;
     float* part_o;        // [rows][heads][parts][HD]
-    float2* part_ml;      // [rows][heads][parts] reference, sum of weights
+    Partial* part_ml;     // [rows][heads][parts]
 };
 
 __device__ __forceinline__ q8_bf16x8 keys8(unsigned a, unsigned b)
@@ -233,7 +264,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 {
     constexpr int KC = HD / 64, DT = HD / 16;
     __shared__ q8_floatx4 merged[NW][DT][64];
-    __shared__ float2 ml[NW][16];
+    __shared__ Partial ml[NW][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     // (heads fastest: consecutive workgroups go to different XCDs, and a part that many sequences lack would leave one of them idle)
     const int b = blockIdx.z, hk = a.c.n_kv_heads, h = blockIdx.x % hk, q0 = (blockIdx.x / hk) * (16 * RT);
@@ -254,7 +285,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     if (part > 0 && part * a.part_pages >= n_blk) {   // nothing to do: says so
         for (int i = threadIdx.x; i < min(16 * RT, n_q - q0); i += 64 * NW) {
             const int qi = q0 + i;
-            a.part_ml[((size_t)(r0 + qi / a.group) * hk * a.group + h * a.group + qi % a.group) * a.parts + part] = make_float2(REF_NONE, 0.f);
+            a.part_ml[((size_t)(r0 + qi / a.group) * hk * a.group + h * a.group + qi % a.group) * a.parts + part] = {REF_NONE, 0.f, 0.f, 0.f};
         }
         return;
     }
@@ -276,11 +307,11 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     }
     const q8_floatx4 zero = {0.f, 0.f, 0.f, 0.f};
     q8_floatx4 o[RT][DT];
-    float ref[RT], sum[RT];
+    float ref[RT], sum[RT], lift[RT], base = 0.f;   // base: log2 of the scale that the sums are in, the same for the whole wavefront
 #pragma unroll
     for (int t = 0; t < RT; ++t) {
         ref[t] = REF_NONE;
-        sum[t] = 0.f;
+        sum[t] = lift[t] = 0.f;
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[t][d] = zero;
     }
@@ -302,7 +333,8 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
     // Scores of page blk against all rows, weights, and the weighted values; the registers of its keys and values take page `next`
     // as soon as they are free.  (These loads are never branched around, or every wait would be for all of them: behind the last page it
     // is read again.)
-    auto take = [&](Page& pg, int blk, bool there, float ks, float lv, float inv, int next) {
+    auto take = [&](auto scales_apart, Page& pg, int blk, bool there, float ks, float lv, float inv, int next) {
+        constexpr bool APART = decltype(scales_apart)::value;
         const auto& kr = pg.k;
         auto& vr = pg.v;
         q8_floatx4 sc[RT][2];
@@ -331,17 +363,26 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
             for (int s = 0; s < 2; ++s)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float v = fmaf(sc[t][s][i], ks, lv);
+                    float v = fmaf(sc[t][s][i], ks, APART ? base : lv);
                     if (masked) v = there && first + 16 * s + 4 * g + i <= lim[t] ? v : -INFINITY;
                     x[4 * s + i] = v;
                     m = fmaxf(m, v);
                 }
-            if (__any(m > ref[t] + REF_SLACK)) {
+            float up = 0.f;   // log2 of vs / base in units of 2^lift
+            if (APART || __any(m > ref[t] + REF_SLACK)) {
                 m = fmaxf(m, __shfl_xor(m, 16));
                 m = fmaxf(m, __shfl_xor(m, 32));
-                const float now = m > ref[t] + REF_SLACK ? m - REF_BELOW : ref[t], f = exp2f(ref[t] - now);
-                ref[t] = now;
+                const float now = m > ref[t] + REF_SLACK ? m - REF_BELOW : ref[t];
+                float f = exp2f(ref[t] - now);
                 sum[t] *= f;
+                if (APART) {
+                    // o stays as the reference moves, and follows the largest product; what has no weight yet has no product either
+                    const float was = fmaxf(lift[t] + (ref[t] - now), -1e30f), most = m - now + lv - base;
+                    lift[t] = most > was + REF_SLACK ? most - REF_BELOW : was;
+                    f = exp2f(was - lift[t]);
+                    up = lv - base - lift[t];
+                }
+                ref[t] = now;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[t][d] *= f;
             }
@@ -350,9 +391,9 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
             for (int e = 0; e < 8; ++e) {
                 const float v = __builtin_amdgcn_exp2f(x[e] - ref[t]);
                 add += v;
-                p[t][e] = (_Float16)v;
+                p[t][e] = (_Float16)(APART ? __builtin_amdgcn_exp2f(x[e] - ref[t] + up) : v);   // (a small weight of a large scale counts)
             }
-            sum[t] = fmaf(add, inv, sum[t]);
+            sum[t] = APART ? sum[t] + add : fmaf(add, inv, sum[t]);
         }
         if (masked) {
             unsigned f = 0;
@@ -394,23 +435,35 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
         fetch_v(pg, next);
     };
     // This wavefront's next 64 pages, one a lane: their numbers and scales.  A page that is not there is read as page 0 and left out.
-    for (int first_blk = c0 + wave; first_blk < c1; first_blk += 64 * NW) {
-        const int blk = first_blk + lane * NW, n_mine = min(64, (c1 - first_blk + NW - 1) / NW);
-        int page = first_blk == c0 + wave ? first_page : pages[min(blk, c1 - 1)];
-        page = blk < c1 ? page : -1;
-        const bool there = page >= 0 && page < a.c.n_pages;
-        page = there ? page : 0;
-        const float2 s2 = *reinterpret_cast<const float2*>(a.c.scales + ((size_t)page * hk + h) * 2);
-        const float ks = s2.x * a.scale, lv = there ? fmaxf(__log2f(s2.y), LOG2_VS_LEAST) : 0.f, inv = exp2f(-lv);
-        const int last = n_mine - 1;
-        auto number = [&](int i) { return __builtin_amdgcn_readlane(page, min(i, last)); };
-        auto of = [&](float f, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)); };
-        Page pg;
-        fetch_k(pg, number(0));
-        fetch_v(pg, number(0));
-        for (int i = 0; i <= last; ++i)
-            take(pg, first_blk + i * NW, __builtin_amdgcn_readlane((int)there, i), of(ks, i), of(lv, i), of(inv, i), number(i + 1));
-    }
+    int first_blk = c0 + wave;
+    auto batches = [&](auto scales_apart) {
+        constexpr bool APART = decltype(scales_apart)::value;
+        for (; first_blk < c1; first_blk += 64 * NW) {
+            const int blk = first_blk + lane * NW, n_mine = min(64, (c1 - first_blk + NW - 1) / NW);
+            int page = first_blk == c0 + wave ? first_page : pages[min(blk, c1 - 1)];
+            page = blk < c1 ? page : -1;
+            const bool there = page >= 0 && page < a.c.n_pages;
+            page = there ? page : 0;
+            const float2 s2 = *reinterpret_cast<const float2*>(a.c.scales + ((size_t)page * hk + h) * 2);
+            const float ks = s2.x * a.scale, lv = there ? fmaxf(__log2f(s2.y), LOG2_VS_LEAST) : 0.f;
+            if (!APART) {
+                const unsigned long long held = __ballot(there);
+                if (first_blk == c0 + wave && held) base = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(lv), __builtin_ctzll(held)));
+                if (__any(there && fabsf(lv - base) > LOG2_VS_APART)) return;
+            }
+            const float inv = there && !APART ? exp2f(base - lv) : 1.f;
+            const int last = n_mine - 1;
+            auto number = [&](int i) { return __builtin_amdgcn_readlane(page, min(i, last)); };
+            auto of = [&](float f, int i) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), i)); };
+            Page pg;
+            fetch_k(pg, number(0));
+            fetch_v(pg, number(0));
+            for (int i = 0; i <= last; ++i)
+                take(scales_apart, pg, first_blk + i * NW, __builtin_amdgcn_readlane((int)there, i), of(ks, i), of(lv, i), of(inv, i), number(i + 1));
+        }
+    };
+    batches(std::false_type());
+    batches(std::true_type());   // from the first batch on that has scales apart
 
     // The wavefronts' results, 16 query rows at a time
 #pragma unroll
@@ -419,34 +472,25 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
         if (t) __syncthreads();
-        if (lane < 16) ml[wave][lane] = make_float2(ref[t], l);
+        if (lane < 16) ml[wave][lane] = {ref[t] - base, l, lift[t] + base, 0.f};
 #pragma unroll
         for (int d = 0; d < DT; ++d) merged[wave][d][lane] = o[t][d];
         __syncthreads();
         for (int i = threadIdx.x; i < DT * 64; i += 64 * NW) {
             const int d = i >> 6, ln = i & 63, qi = q0 + 16 * t + (ln & 15);
             if (qi >= n_q) continue;
-            float m = REF_NONE, den = 0.f;
-            for (int k = 0; k < NW; ++k) m = fmaxf(m, ml[k][ln & 15].x);
+            float top, most, den;
+            join_references(NW, [&](int k) { return ml[k][ln & 15]; }, &top, &most, &den);
             q8_floatx4 v = zero;
-            for (int k = 0; k < NW; ++k) {
-                const float2 x = ml[k][ln & 15];
-                const float f = exp2f(x.x - m);
-                den = fmaf(x.y, f, den);
-                v += merged[k][d][ln] * f;
-            }
+            for (int k = 0; k < NW; ++k) v += merged[k][d][ln] * join_weight(ml[k][ln & 15], top, most);
             const int row = r0 + qi / a.group, head = h * a.group + qi % a.group, dim = 16 * d + 4 * (ln >> 4), hq = hk * a.group;
             const size_t at = (size_t)row * hq + head;
             if (a.parts == 1) {
-                const float f = den == 0.f ? 0.f : 1.f / den;
-                uint16_t* dst = a.out + at * HD + dim;
-                const unsigned x = q8_round_bf16(v[0] * f) | (unsigned)q8_round_bf16(v[1] * f) << 16;
-                const unsigned y = q8_round_bf16(v[2] * f) | (unsigned)q8_round_bf16(v[3] * f) << 16;
-                *reinterpret_cast<uint2*>(dst) = make_uint2(x, y);
+                *reinterpret_cast<uint2*>(a.out + at * HD + dim) = finished(v, most, den);
             } else {
                 const size_t pt = at * a.parts + part;
                 *reinterpret_cast<q8_floatx4*>(a.part_o + pt * HD + dim) = v;
-                if (dim == 0) a.part_ml[pt] = make_float2(m, den);
+                if (dim == 0) a.part_ml[pt] = {top, den, most, 0.f};
             }
         }
     }
@@ -455,13 +499,13 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 constexpr int MAX_PARTS = 64;
 
 // `per` (a power of two) groups of HD/4 threads join the parts of one (row, head): a thread has four dimensions of every per-th part.
-// o = sum of 2^(ref_k - m) o_k / sum of 2^(ref_k - m) l_k.  Latency: two rounds of loads, 4.3 us for 286 rows of 32 heads in two parts.
+// Latency: two rounds of loads, 4.3 us for 286 rows of 32 heads in two parts.
 template <int HD>
-__global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ part_o, const float2* __restrict__ part_ml, int parts, int per,
+__global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ part_o, const Partial* __restrict__ part_ml, int parts, int per,
                                                    size_t items, const int32_t* __restrict__ row0, int batch, int hq, uint16_t* __restrict__ out)
 {
     constexpr int LANES = HD / 4, GROUPS = 256 / LANES;
-    __shared__ float2 ml[GROUPS][MAX_PARTS];
+    __shared__ Partial ml[GROUPS][MAX_PARTS];
     __shared__ q8_floatx4 sums[GROUPS][LANES];
     const int tid = threadIdx.x, grp = tid / LANES, dim = (tid % LANES) * 4, item = grp / per, sub = grp % per;
     const size_t at = (size_t)blockIdx.x * (GROUPS / per) + item;
@@ -470,27 +514,21 @@ __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ par
         for (int k = tid - item * per * LANES; k < parts; k += per * LANES) ml[item][k] = part_ml[at * parts + k];
     __syncthreads();
     q8_floatx4 o = {0.f, 0.f, 0.f, 0.f};
-    float den = 0.f;
+    float top, most = 0.f, den = 0.f;
     if (on) {
-        float m = REF_NONE;
-        for (int k = 0; k < parts; ++k) m = fmaxf(m, ml[item][k].x);
-        for (int k = 0; k < parts; ++k) den = fmaf(ml[item][k].y, exp2f(ml[item][k].x - m), den);
+        join_references(parts, [&](int k) { return ml[item][k]; }, &top, &most, &den);
 #pragma unroll 4
         for (int k = sub; k < parts; k += per) {
-            const float2 x = ml[item][k];
-            const float f = exp2f(x.x - m);
+            const Partial x = ml[item][k];
             const q8_floatx4 v = *reinterpret_cast<const q8_floatx4*>(part_o + (at * parts + k) * HD + dim);
-            o += x.y == 0.f ? (q8_floatx4){0.f, 0.f, 0.f, 0.f} : v * f;   // a part without a position has written nothing else
+            o += x.sum == 0.f ? (q8_floatx4){0.f, 0.f, 0.f, 0.f} : v * join_weight(x, top, most);   // a part without a position has written nothing else
         }
     }
     sums[grp][tid % LANES] = o;
     __syncthreads();
     if (!on || sub) return;
     for (int i = 1; i < per; ++i) o += sums[grp + i][tid % LANES];
-    const float f = den == 0.f ? 0.f : 1.f / den;
-    const unsigned x = q8_round_bf16(o[0] * f) | (unsigned)q8_round_bf16(o[1] * f) << 16;
-    const unsigned y = q8_round_bf16(o[2] * f) | (unsigned)q8_round_bf16(o[3] * f) << 16;
-    *reinterpret_cast<uint2*>(out + at * HD + dim) = make_uint2(x, y);
+    *reinterpret_cast<uint2*>(out + at * HD + dim) = finished(o, most, den);
 }
 
 int compute_units()
@@ -512,7 +550,7 @@ void launch_attn(AttnArgs a, int batch, int max_window, int max_len, size_t ws_f
     const int hk = a.c.n_kv_heads, hq = hk * a.group, cus = compute_units();
     a.tiles = (int)(((int64_t)max_window * a.group + 16 * RT - 1) / (16 * RT));
     const int64_t wgs = (int64_t)batch * hk * a.tiles, pages = (max_len + PAGE - 1) / PAGE;
-    const size_t each = (size_t)a.rows * hq * (HD + 2);
+    const size_t each = (size_t)a.rows * hq * (HD + 4);
     // Parts of a sequence are workgroups of their own, joined by a second kernel (3 us): where there are fewer workgroups than compute units,
     // down to two pages a wavefront -- one sequence of 30000, 8 kv heads: 132 us in one part, 20 in 32; of 2048, 32 heads: 13.6 in one, 10.6
     // in four; of 1024, 8 heads of 64: 6.7 in one, 8.4 in two -- and where sequences may differ by much (32 of 512 to 16384: 106 us in two
@@ -524,7 +562,7 @@ void launch_attn(AttnArgs a, int batch, int max_window, int max_len, size_t ws_f
     a.part_pages = (int)std::max<int64_t>((pages + a.parts - 1) / a.parts, 1);
     if (a.parts > 1) {
         a.part_o = (float*)ws;
-        a.part_ml = (float2*)(a.part_o + (size_t)a.rows * hq * a.parts * HD);
+        a.part_ml = (Partial*)(a.part_o + (size_t)a.rows * hq * a.parts * HD);
     }
     hipLaunchKernelGGL((attn8_kernel<HD, RT, NW>), dim3(hk * a.tiles, a.parts, batch), dim3(64 * NW), 0, s, a);
     if (a.parts > 1) {
@@ -591,7 +629,7 @@ extern "C" size_t spec_kv8_workspace_bytes(int32_t rows, int32_t n_q_heads, int3
 {
     if (rows <= 0 || n_q_heads <= 0 || head_dim <= 0) return 0;
     // few rows are split the most; many rows fill the chip by themselves
-    const size_t each = (size_t)rows * n_q_heads * (head_dim + 2) * sizeof(float);
+    const size_t each = (size_t)rows * n_q_heads * (head_dim + 4) * sizeof(float);
     return std::min(each * MAX_PARTS, std::max(each * 2, (size_t)64 << 20));
 }
 
