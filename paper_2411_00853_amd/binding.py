@@ -448,7 +448,7 @@ def spec_decode_get_view(d: Decoder) -> spec_decode_view:
 
 # ---- 8-bit operators and filtered draws (include/spec_q8.h) ---------------------------------------
 # Types, shapes and strides are checked where the tensors are read: csrc/native.cpp.  A wrong one raises ValueError, a status
-# other than SPEC_OK raises SpecError.
+# other than SPEC_OK raises SpecError.  Outputs that a call makes itself are tensors of the stream that it is given.
 
 KV8_PAGE = 32   # positions of a page of the 8-bit cache
 _F8 = torch.float8_e4m3fn
@@ -475,16 +475,22 @@ def _raw_stream(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
-def _q8_out(x: torch.Tensor, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor]):
+def _new(shape, dtype, device, stream) -> torch.Tensor:
+    """An output of a call on `stream`: memory of that stream's, or it could be memory that work queued on the current one still uses."""
+    with torch.cuda.stream(stream):     # (None: the current one)
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _q8_out(x: torch.Tensor, cols: int, q: Optional[torch.Tensor], scales: Optional[torch.Tensor], stream):
     rows, kp = x.shape[0], (cols + 127) // 128 * 128
-    return (torch.empty((rows, kp), dtype=_F8, device=x.device) if q is None else q,
-            torch.empty((kp // 128, rows), dtype=torch.float32, device=x.device) if scales is None else scales)
+    return (_new((rows, kp), _F8, x.device, stream) if q is None else q,
+            _new((kp // 128, rows), torch.float32, x.device, stream) if scales is None else scales)
 
 
 def spec_q8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """Rows of x [rows][cols] (any row stride) -> (q e4m3 [rows][Kp], scales fp32 [Kp/128][rows])."""
     if q is None or scales is None:
-        q, scales = _q8_out(x, x.shape[1], q, scales)
+        q, scales = _q8_out(x, x.shape[1], q, scales, stream)
     _check(_native().quantize(x, q, scales, _raw_stream(stream)))
     return q, scales
 
@@ -494,7 +500,7 @@ def spec_q8_add_rmsnorm(x: torch.Tensor, delta: Optional[torch.Tensor], gain: to
                         scales: Optional[torch.Tensor] = None, stream=None):
     """x + delta -> x_out (may be x; None: not kept); its RMSNorm times gain -> (q, scales)."""
     if q is None or scales is None:
-        q, scales = _q8_out(x, x.shape[1], q, scales)
+        q, scales = _q8_out(x, x.shape[1], q, scales, stream)
     _check(_native().add_rmsnorm(x, delta, gain, eps, x_out, q, scales, _raw_stream(stream)))
     return q, scales
 
@@ -502,7 +508,7 @@ def spec_q8_add_rmsnorm(x: torch.Tensor, delta: Optional[torch.Tensor], gain: to
 def spec_q8_swiglu(gate_up: torch.Tensor, q: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """silu(gate) * up of [rows][gate columns | up columns] -> (q, scales)."""
     if q is None or scales is None:
-        q, scales = _q8_out(gate_up, gate_up.shape[1] // 2, q, scales)
+        q, scales = _q8_out(gate_up, gate_up.shape[1] // 2, q, scales, stream)
     _check(_native().swiglu(gate_up, q, scales, _raw_stream(stream)))
     return q, scales
 
@@ -514,7 +520,7 @@ def spec_q8_packed_weight_bytes(n_out: int, n_in: int) -> int:
 def spec_q8_pack_weight(src: torch.Tensor, stream=None) -> torch.Tensor:
     """Row-major e4m3 [n_out][n_in] -> new device buffer in the tile order of spec_q8_gemm."""
     n_out, n_in = src.shape
-    dst = torch.empty(spec_q8_packed_weight_bytes(n_out, n_in), dtype=_F8, device=src.device)
+    dst = _new((spec_q8_packed_weight_bytes(n_out, n_in),), _F8, src.device, stream)
     _check(lib().spec_q8_pack_weight(_ptr(src, _F8), _ptr(dst), n_out, n_in, _raw_stream(stream)))
     return dst
 
