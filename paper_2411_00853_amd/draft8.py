@@ -37,7 +37,8 @@ def rope_table(max_pos: int, head_dim: int, theta: float, device="cuda") -> torc
 
 class Draft8:
     """A decoder of workload.ModelShape `shape` in 8 bits.  weights: as workload.make_weights gives them, on the device (kept in bf16:
-    the embedding only).  Nothing is allocated after __init__, so `feed` and `propose` can be captured into a HIP graph."""
+    the embedding only).  Device memory is allocated in __init__ alone, so `feed` and `propose` can be captured into a HIP graph by any
+    means.  max_window: the longest window of a `feed`; `propose` needs 2."""
 
     def __init__(self, shape, weights: dict, batch: int, max_kv_len: int, max_window: int, temperature: float = 1.0,
                  top_k: Optional[int] = None, top_p: Optional[float] = None, min_p: Optional[float] = None):
@@ -56,6 +57,7 @@ class Draft8:
         self.cos_sin = rope_table(max_kv_len, hd, shape.rope_theta, dev)
         R = batch * max_window
         new = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device=dev)
+        self.embedded, self.first, self.at = new(R, d, dtype=self.embed.dtype), new(batch, 2, dtype=torch.int32), new(batch, dtype=torch.int32)
         self.x, self.delta, self.qkv = new(R, d, dtype=torch.float32), new(R, d), new(R, shape.d_q + 2 * shape.d_kv)
         self.q, self.attn, self.gate_up = new(R, shape.d_q), new(R, shape.d_q), new(R, 2 * F)
         self.logits = new(R, V, dtype=torch.float32)
@@ -80,13 +82,15 @@ class Draft8:
         return q[:rows * kp].view(rows, kp), s[:rows * kp // 128].view(kp // 128, rows)
 
     def feed(self, tokens: torch.Tensor, kv_len: torch.Tensor, max_len: int = 0, logits: bool = True):
-        """tokens int32 [batch][w], the next w tokens of every sequence, at positions kv_len[b] + 0 .. w-1 -> fp32 logits
+        """tokens int32 [batch][w] (copied if not contiguous), the next w tokens of every sequence, at positions kv_len[b] + 0 .. w-1 -> fp32 logits
         [batch * w][vocab] of this object (None with logits=False).  kv_len is not changed."""
         s, w = self.shape, tokens.shape[1]
+        if not 1 <= w <= self.max_window:
+            raise ValueError(f"a window of {w} tokens, at most {self.max_window}")
         R = self.batch * w
         d, F, row0 = s.d_model, s.d_ffn, self.row0[w]
         x, delta = self.x[:R], None
-        x.copy_(self.embed.index_select(0, tokens.reshape(-1)))
+        x.copy_(torch.index_select(self.embed, 0, tokens.reshape(-1), out=self.embedded[:R]))
         for cache, (attn_norm, w_qkv, w_o, ffn_norm, w_gate_up, w_down) in zip(self.caches, self.layers):
             a = sv.spec_q8_add_rmsnorm(x, delta, attn_norm, s.rms_eps, x, *self._operand(R, d))
             qkv = sv.spec_q8_gemm(*a, *w_qkv, self.qkv[:R])
@@ -107,9 +111,11 @@ class Draft8:
         """K = tokens.shape[1] proposals after `last`, the token at position kv_len[b] of each sequence: tokens int32 [batch][K] and the
         filtered rows they were drawn from, logits fp32 [batch][K][vocab].  prev: the token before last, whose keys the cache may
         not hold yet (the target's round may have ended on a proposal that was never fed).  uniforms: [K][batch]."""
-        step = torch.stack((prev, last), 1)
+        if self.max_window < 2:
+            raise ValueError("proposals begin with a window of 2 tokens, max_window is 1")
+        step = torch.stack((prev, last), 1, out=self.first)
         for i in range(tokens.shape[1]):
-            rows = self.feed(step, kv_len - 1 if i == 0 else kv_len + i, max_len)
+            rows = self.feed(step, torch.add(kv_len, i if i else -1, out=self.at), max_len)
             if i == 0:
                 rows = rows.view(self.batch, 2, -1)[:, 1]
             sv.spec_filter_sample(rows, uniforms[i], self.temperature, self.drawn, logits_out=self.filtered, workspace=self.draw_work,
