@@ -208,13 +208,15 @@ struct Partial {
     float s, sum, e, unused;
 };
 // Joined: o = sum of o_k * weight_k, out = o * factor(o) (in two steps: 2^most is no fp32 number for the largest scales)
-template <typename F>
+template <int UNROLL, typename F>
 __device__ __forceinline__ void join_references(int n, F part, float* top, float* most, float* den)
 {
     *top = REF_NONE;
+#pragma unroll UNROLL
     for (int k = 0; k < n; ++k) *top = fmaxf(*top, part(k).s);
     *most = REF_NONE;
     *den = 0.f;
+#pragma unroll UNROLL
     for (int k = 0; k < n; ++k) {
         const Partial x = part(k);
         *den = fmaf(x.sum, __builtin_amdgcn_exp2f(x.s - *top), *den);
@@ -264,7 +266,8 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 {
     constexpr int KC = HD / 64, DT = HD / 16;
     __shared__ q8_floatx4 merged[NW][DT][64];
-    __shared__ Partial ml[NW][16];
+    __shared__ Partial ml[NW][16], joined[16];
+    __shared__ float weight[NW][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     // (heads fastest: consecutive workgroups go to different XCDs, and a part that many sequences lack would leave one of them idle)
     const int b = blockIdx.z, hk = a.c.n_kv_heads, h = blockIdx.x % hk, q0 = (blockIdx.x / hk) * (16 * RT);
@@ -476,21 +479,30 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 #pragma unroll
         for (int d = 0; d < DT; ++d) merged[wave][d][lane] = o[t][d];
         __syncthreads();
+        // (A thread for each wavefront and row: by every thread for itself, 256 workgroups of 64 positions take 5.2 us, 4.6 this way.)
+        if (threadIdx.x < NW * 16) {
+            const int k = threadIdx.x >> 4, row = lane & 15;
+            float top, most, den;
+            join_references<NW>(NW, [&](int i) { return ml[i][row]; }, &top, &most, &den);
+            weight[k][row] = join_weight(ml[k][row], top, most);
+            if (k == 0) joined[row] = {top, den, most, 0.f};
+        }
+        __syncthreads();
         for (int i = threadIdx.x; i < DT * 64; i += 64 * NW) {
             const int d = i >> 6, ln = i & 63, qi = q0 + 16 * t + (ln & 15);
             if (qi >= n_q) continue;
-            float top, most, den;
-            join_references(NW, [&](int k) { return ml[k][ln & 15]; }, &top, &most, &den);
+            const Partial all = joined[ln & 15];
             q8_floatx4 v = zero;
-            for (int k = 0; k < NW; ++k) v += merged[k][d][ln] * join_weight(ml[k][ln & 15], top, most);
+#pragma unroll
+            for (int k = 0; k < NW; ++k) v += merged[k][d][ln] * weight[k][ln & 15];
             const int row = r0 + qi / a.group, head = h * a.group + qi % a.group, dim = 16 * d + 4 * (ln >> 4), hq = hk * a.group;
             const size_t at = (size_t)row * hq + head;
             if (a.parts == 1) {
-                *reinterpret_cast<uint2*>(a.out + at * HD + dim) = finished(v, most, den);
+                *reinterpret_cast<uint2*>(a.out + at * HD + dim) = finished(v, all.e, all.sum);
             } else {
                 const size_t pt = at * a.parts + part;
                 *reinterpret_cast<q8_floatx4*>(a.part_o + pt * HD + dim) = v;
-                if (dim == 0) a.part_ml[pt] = {top, den, most, 0.f};
+                if (dim == 0) a.part_ml[pt] = all;
             }
         }
     }
@@ -516,7 +528,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ par
     q8_floatx4 o = {0.f, 0.f, 0.f, 0.f};
     float top, most = 0.f, den = 0.f;
     if (on) {
-        join_references(parts, [&](int k) { return ml[item][k]; }, &top, &most, &den);
+        join_references<2>(parts, [&](int k) { return ml[item][k]; }, &top, &most, &den);
 #pragma unroll 4
         for (int k = sub; k < parts; k += per) {
             const Partial x = ml[item][k];
