@@ -35,8 +35,8 @@ extern "C" {
 #define SPEC_KV8_PAGE 32             /* positions of a cache page */
 #define SPEC_FILTER_MAX_VOCAB 262144
 
-/* Types are SPEC_DTYPE_FP32 or SPEC_DTYPE_BF16.  q 16-byte aligned; everything else as its element type asks.
- * rows = 0 does nothing. */
+/* Types are SPEC_DTYPE_FP32 or SPEC_DTYPE_BF16.  q, packed matrices and the product's y 16-byte aligned; everything else as its element
+ * type asks.  Columns, n_out and n_in: at most 2^30 (SPEC_ERR_SHAPE beyond).  rows = 0 does nothing. */
 
 /* q, scales = the rows of x [rows][cols], ld elements apart (ld >= cols). */
 int spec_q8_quantize(const void* x, int32_t x_dtype, int64_t ld, int32_t rows, int32_t cols, void* q, float* scales,
@@ -51,7 +51,7 @@ int spec_q8_add_rmsnorm(const void* x, int32_t x_dtype, const void* delta, int32
 /* q, scales = silu(gate) * up of gate_up [rows][2 d_ffn]: d_ffn gate columns, then d_ffn up columns. */
 int spec_q8_swiglu(const void* gate_up, int32_t dtype, int32_t rows, int32_t d_ffn, void* q, float* scales, void* stream);
 
-/* Bytes of a packed [n_out][n_in] matrix of 8-bit numbers: n_out rounded up to 16, n_in to 128. */
+/* Bytes of a packed [n_out][n_in] matrix of 8-bit numbers: n_out rounded up to 16, n_in to 128 (0: no such matrix). */
 size_t spec_q8_packed_weight_bytes(int32_t n_out, int32_t n_in);
 
 /* Row-major e4m3 [n_out][n_in] -> the order the product reads.  Tile (kb, j) holds out features 16j..16j+15 and in
@@ -61,7 +61,7 @@ size_t spec_q8_packed_weight_bytes(int32_t n_out, int32_t n_in);
 int spec_q8_pack_weight(const void* src, void* dst_packed, int32_t n_out, int32_t n_in, void* stream);
 
 /* y [M][N] (contiguous) = sum over blocks kb of scales[kb][m] * w_scales[n/128][kb] * (q's block . w's block):
- * the sums over blocks in fp32, y rounded once to y_dtype.  q: [M][Kp]; K is the row length before padding.
+ * the sums over blocks in fp32, y rounded once to y_dtype.  q: [M][Kp], M <= 1048560; K is the row length before padding.
  * Within a block: for fp32 y products are exact and their sum is fp32.  For bf16 y it is one fp8 matrix instruction, at twice the rate, which cuts
  * off each of eight neighbouring products at 2^-13 of the largest of them; all in all that is less than 2^-10 of the sum of the magnitudes
  * of the products (the numbers that are multiplied were rounded by up to 2^-4).  Callers whose sums cancel and who want what is left ask for fp32. */

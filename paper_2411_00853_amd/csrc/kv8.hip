@@ -620,7 +620,7 @@ extern "C" int spec_kv8_append(const spec_kv8_cache* cache, const void* qkv, int
     if (!rows || !max_window) return SPEC_OK;
     if (!qkv || (cos_sin && !q_out)) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_append: null pointer");
     if (cos_sin && max_pos <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_kv8_append: a rotation of %d positions", max_pos);
-    const int group = n_q_heads / cache->n_kv_heads, pages = (max_window + PAGE - 2) / PAGE + 1;
+    const int group = n_q_heads / cache->n_kv_heads, pages = (int)(((int64_t)max_window + PAGE - 2) / PAGE) + 1;
     const int at_once = APPEND_TPB / (cache->head_dim / 16);
     const int64_t queries = q_out ? ((int64_t)max_window * group + at_once - 1) / at_once : 0;
     if (queries + pages > 0x7fffffff) return fail(SPEC_ERR_SHAPE, "spec_kv8_append: a window of %d rows", max_window);

@@ -19,6 +19,8 @@ typedef unsigned q8_uintx2 __attribute__((ext_vector_type(2)));
 constexpr float Q8_MAX = 448.f;         // largest e4m3 number
 constexpr float Q8_TINY = 0x1p-126f;    // smallest scale
 
+constexpr int Q8_MAX_SIZE = 1 << 30;    // of a row or a matrix: places in it, rounded up to whole blocks, are ints
+
 inline int q8_blocks(int cols) { return (cols + SPEC_Q8_BLOCK - 1) / SPEC_Q8_BLOCK; }
 inline bool q8_dtype(int t) { return t == SPEC_DTYPE_FP32 || t == SPEC_DTYPE_BF16; }
 

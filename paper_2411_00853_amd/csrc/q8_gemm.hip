@@ -520,7 +520,7 @@ using namespace specv;
 
 extern "C" size_t spec_q8_packed_weight_bytes(int32_t n_out, int32_t n_in)
 {
-    if (n_out <= 0 || n_in <= 0) return 0;
+    if (n_out <= 0 || n_in <= 0 || n_out > Q8_MAX_SIZE || n_in > Q8_MAX_SIZE) return 0;
     return (size_t)((n_out + 15) / 16) * (size_t)q8_blocks(n_in) * TILE;
 }
 
@@ -530,7 +530,7 @@ extern "C" int spec_q8_pack_weight(const void* src, void* dst_packed, int32_t n_
     if (n_out <= 0 || n_in <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_pack_weight: %d x %d", n_out, n_in);
     if ((uintptr_t)dst_packed & 15) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_pack_weight: dst_packed is not 16-byte aligned");
     const size_t total = spec_q8_packed_weight_bytes(n_out, n_in) / 16;
-    if (total > ((size_t)1 << 38)) return fail(SPEC_ERR_SHAPE, "spec_q8_pack_weight: %d x %d is too large", n_out, n_in);
+    if (!total || total > ((size_t)1 << 38)) return fail(SPEC_ERR_SHAPE, "spec_q8_pack_weight: %d x %d is too large", n_out, n_in);
     hipLaunchKernelGGL(pack_kernel, dim3((unsigned)((total + 255) / 256)), dim3(256), 0, (hipStream_t)stream, (const uint8_t*)src,
                        (uint8_t*)dst_packed, n_out, n_in, (n_out + 15) / 16, total);
     SPECV_LAUNCH_CHECK("pack_kernel");
@@ -541,6 +541,7 @@ extern "C" int spec_q8_gemm(const void* q, const float* scales, const void* w_pa
                             int32_t M, int32_t N, int32_t K, void* stream)
 {
     if (M < 0 || N <= 0 || K <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: M = %d, N = %d, K = %d", M, N, K);
+    if (N > Q8_MAX_SIZE || K > Q8_MAX_SIZE) return fail(SPEC_ERR_SHAPE, "spec_q8_gemm: N = %d, K = %d, at most %d", N, K, Q8_MAX_SIZE);
     if (!q8_dtype(y_dtype)) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: unknown type %d", y_dtype);
     if (!M) return SPEC_OK;
     if (!q || !scales || !w_packed || !w_scales || !y) return fail(SPEC_ERR_INVALID_ARG, "spec_q8_gemm: null pointer");

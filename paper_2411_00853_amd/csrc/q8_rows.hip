@@ -200,6 +200,7 @@ using namespace specv;
 static int check_rows(const char* name, const void* x, int dtype, int rows, int cols, const void* q, const void* scales)
 {
     if (rows < 0 || cols <= 0) return fail(SPEC_ERR_INVALID_ARG, "%s: %d rows of %d columns", name, rows, cols);
+    if (cols > Q8_MAX_SIZE) return fail(SPEC_ERR_SHAPE, "%s: %d columns, at most %d", name, cols, Q8_MAX_SIZE);
     if (!q8_dtype(dtype)) return fail(SPEC_ERR_INVALID_ARG, "%s: unknown type %d", name, dtype);
     if (rows && (!x || !q || !scales)) return fail(SPEC_ERR_INVALID_ARG, "%s: null pointer", name);
     if ((uintptr_t)q & 15) return fail(SPEC_ERR_INVALID_ARG, "%s: q is not 16-byte aligned", name);
