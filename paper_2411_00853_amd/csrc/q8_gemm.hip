@@ -462,7 +462,9 @@ void launch_few(const void* x, const void* w, const float* sx, const float* sw, 
     }
 }
 
-// A tile shape's time for one block of K, in us with a workgroup on every compute unit (bf16 results, K = 4096)
+// A tile shape's time for one block of K, in us with a workgroup on every compute unit (bf16 results, K = 4096).  fp32 results take 1.6 times
+// as long in each of the three shapes that they have (0.57, 0.76, 1.21), so that the same prices rank them: over 50 sizes of 64 to 2048 rows, 512
+// to 23000 columns and K of 256 to 8192 the choice was 0.5 % slower than the best of the three on average, 9 % at most.
 struct TileShape {
     int rows, cols;
     float us;
