@@ -121,7 +121,7 @@ int spec_kv8_attention(const spec_kv8_cache* cache, const void* q, int64_t ld_q,
  *     top_p:  the mass ranked before it is below top_p[r] times the mass that top_k leaves   (top_p[r] >= 1: all)
  *     min_p:  its mass is at least min_p[r] times the largest                                (min_p[r] <= 0: all)
  * (the first token always is).  temperature[r] <= 0 (or NaN) keeps the first token alone, one between 0 and 2^-126 counts as 2^-126, an
- * infinite one as fp32's largest number; a NaN in top_p or min_p keeps all.  The token drawn is the first id whose
+ * infinite one as fp32's largest number, a difference of logits that fp32 does not hold as infinite; a NaN in top_p or min_p keeps all.  The token drawn is the first id whose
  * inclusive prefix sum of kept masses exceeds floor(uniforms[r] * kept mass).  Excluded logits may be -inf; a row
  * with a NaN, a +inf or no finite logit gives token -1, n_kept 0, logprob NaN and a filtered row of -inf. */
 typedef struct {

@@ -193,8 +193,8 @@ __global__ void __launch_bounds__(APPEND_TPB) append_kernel(const uint16_t* __re
 //     sum of weights = sum * 2^(ref - log2(base)),   O = o * 2^(ref + lift),   out = o / sum * 2^(lift + log2(base)),
 // and results are joined by S = ref - log2(base) and E = lift + log2(base), small numbers that no large score swallows.
 //
-// Bound by the stream of the cache: 8 sequences of 2048 with 32 kv heads of 128, 136 MB in 24 us (5.6 TB/s); 32 of 512 to 16384 with 8, 549 MB
-// in 104 us (5.3 TB/s).  So every byte is read once for all query heads and window rows that share it; a page's registers are
+// Bound by the stream of the cache: 8 sequences of 2048 with 32 kv heads of 128, 136 MB in 23.5 us (5.8 TB/s); 32 of 512 to 16384 with 8, 549 MB
+// in 103 us (5.3 TB/s).  So every byte is read once for all query heads and window rows that share it; a page's registers are
 // filled again as soon as they are free, the keys' while the values are worked on and the other way round (all of a page asked
 // for behind its last use: 37.7 us for the first of the two, with the append, against 29); and what runs meanwhile is little: two conversions
 // and four products of 16 rows for each 1 KiB.
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(64 * NW) attn8_kernel(const AttnArgs a)
 constexpr int MAX_PARTS = 64;
 
 // `per` (a power of two) groups of HD/4 threads join the parts of one (row, head): a thread has four dimensions of every per-th part.
-// Latency: two rounds of loads, 4.3 us for 286 rows of 32 heads in two parts.
+// Latency: two rounds of loads, 5 us for 143 rows of 32 heads in two parts.
 template <int HD>
 __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ part_o, const Partial* __restrict__ part_ml, int parts, int per,
                                                    size_t items, const int32_t* __restrict__ row0, int batch, int hq, uint16_t* __restrict__ out)
