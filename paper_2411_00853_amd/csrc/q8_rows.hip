@@ -139,13 +139,42 @@ __global__ void __launch_bounds__(1024) norm_kernel(const TX* x, const TD* __res
 #pragma unroll
         for (int i = 0; i < 8; ++i) ss += h[k][i] * h[k][i];
     }
+    auto all = [&](float v, auto join) {   // of the workgroup, the same for all threads
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) ss += __shfl_xor(ss, d);
-    if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = ss;
-    __syncthreads();
-    ss = 0.f;
-    for (int w = 0; w < n_waves; ++w) ss += wave_sum[w];
-    const float r = 1.f / sqrtf(ss / (float)cols + eps);
+        for (int d = 1; d < 64; d <<= 1) v = join(v, __shfl_xor(v, d));
+        if ((threadIdx.x & 63) == 0) wave_sum[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.f;
+        for (int w = 0; w < n_waves; ++w) v = join(v, wave_sum[w]);
+        return v;
+    };
+    auto add = [](float a, float b) { return a + b; };
+    ss = all(ss, add);
+    float r = 1.f / sqrtf(ss / (float)cols + eps);
+    const float known = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(ss)));   // (the branch is the workgroup's)
+    if (!(known <= 0x1.fffffep127f) || (eps == 0.f && known < 0x1p-80f)) {
+        // Squares that leave fp32's range: they are those of the row over a power of two near its largest number, if that is one
+        float top = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(h[k][i]));
+        __syncthreads();
+        top = all(top, [](float a, float b) { return fmaxf(a, b); });
+        const int e = min(max((int)(__float_as_uint(top) >> 23), 2), 252);   // (an infinity or a NaN leaves its mark in the sum below)
+        const float down = __uint_as_float((unsigned)(254 - e) << 23);
+        ss = 0.f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[k][i] *= down;
+                ss = fmaf(h[k][i], h[k][i], ss);
+            }
+        __syncthreads();
+        ss = all(ss, add);
+        r = 1.f / sqrtf(ss / (float)cols + eps * down * down);
+    }
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
         const int col = (k * blockDim.x + threadIdx.x) * 8;
