@@ -61,7 +61,8 @@ size_t spec_q8_packed_weight_bytes(int32_t n_out, int32_t n_in);
 int spec_q8_pack_weight(const void* src, void* dst_packed, int32_t n_out, int32_t n_in, void* stream);
 
 /* y [M][N] (contiguous) = sum over blocks kb of scales[kb][m] * w_scales[n/128][kb] * (q's block . w's block):
- * the sums over blocks in fp32, y rounded once to y_dtype.  q: [M][Kp], M <= 1048560; K is the row length before padding.
+ * the sums over blocks in fp32, y rounded once to y_dtype.  q: [M][Kp], M <= 1048560; K is the row length before padding.  The
+ * two scales of a block are multiplied first: their product is meant to be a normal fp32 number.
  * Within a block: for fp32 y products are exact and their sum is fp32.  For bf16 y it is one fp8 matrix instruction, at twice the rate, which cuts
  * off each of eight neighbouring products at 2^-13 of the largest of them; all in all that is less than 2^-10 of the sum of the magnitudes
  * of the products (the numbers that are multiplied were rounded by up to 2^-4).  Callers whose sums cancel and who want what is left ask for fp32. */
