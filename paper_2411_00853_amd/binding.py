@@ -1,5 +1,5 @@
 """ctypes binding of libspecverify.so: the same entry points as include/spec_verify.h, include/spec_decode.h,
-include/spec_q8.h and include/spec_kernels.h, taking torch tensors where the C side takes device pointers.  Argument
+include/spec_q8.h, include/spec_prompt.h and include/spec_kernels.h, taking torch tensors where the C side takes device pointers.  Argument
 marshalling only -- no arithmetic of the method happens here, and there is no fallback: if the
 HIP library is missing or fails to load, every call raises."""
 from __future__ import annotations
@@ -94,6 +94,18 @@ class spec_filter_args(C.Structure):
 
 class spec_filter_out(C.Structure):
     _fields_ = [("tokens", C.c_void_p), ("logprob", C.c_void_p), ("n_kept", C.c_void_p), ("logits_out", C.c_void_p)]
+
+
+class spec_prompt_epilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("residual_dtype", C.c_int32),
+                ("activation", C.c_int32)]
+
+
+class spec_prompt_attn_args(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in "qkv"] + [(n, C.c_int64) for n in ("ld_q", "ld_k", "ld_v", "ld_out")] + \
+               [("q_row0", C.c_void_p), ("k_row0", C.c_void_p)] + \
+               [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "batch", "q_rows", "k_rows", "max_q_len", "max_k_len")] + \
+               [("scale", C.c_float), ("out", C.c_void_p)]
 
 
 PLAN_MAX_PASSES, PLAN_PROJECTIONS = 32, 5
@@ -205,6 +217,14 @@ def lib():
         L.spec_filter_workspace_bytes.restype = C.c_size_t
         L.spec_filter_workspace_bytes.argtypes = [i32, i32]
         L.spec_filter_sample.argtypes = [C.POINTER(spec_filter_args), C.POINTER(spec_filter_out), ptr, C.c_size_t, ptr]
+        L.spec_prompt_rmsnorm.argtypes = [ptr, i32, i64, ptr, f32, i32, i32, ptr, ptr]
+        L.spec_prompt_gemm_workspace_bytes.restype = C.c_size_t
+        L.spec_prompt_gemm_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.spec_prompt_gemm.argtypes = [ptr, i64, ptr, C.POINTER(spec_prompt_epilogue), ptr, i32, i64, i32, i32, i32, ptr, C.c_size_t, ptr]
+        L.spec_prompt_append.argtypes = [ptr, i32, ptr, i64, ptr, i64, ptr, ptr, ptr, i32, i32, ptr]
+        L.spec_prompt_attention_workspace_bytes.restype = C.c_size_t
+        L.spec_prompt_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        L.spec_prompt_attention.argtypes = [C.POINTER(spec_prompt_attn_args), ptr, C.c_size_t, ptr]
         _lib = L
     return _lib
 
@@ -463,7 +483,8 @@ def _native():
             _build.build_native()
         from . import _native as m
         m.bind(*(C.cast(f, C.c_void_p).value for f in (L.spec_q8_quantize, L.spec_q8_add_rmsnorm, L.spec_q8_swiglu, L.spec_q8_gemm,
-                                                       L.spec_kv8_append, L.spec_kv8_attention, L.spec_filter_sample)))
+                                                       L.spec_kv8_append, L.spec_kv8_attention, L.spec_filter_sample, L.spec_prompt_rmsnorm,
+                                                       L.spec_prompt_gemm, L.spec_prompt_append, L.spec_prompt_attention)))
         _native_module = m
     return _native_module
 
@@ -573,6 +594,68 @@ def spec_filter_sample(logits: torch.Tensor, uniforms: torch.Tensor, temperature
     _check(_native().sample(logits, uniforms, temperature, tokens, top_k, top_p, min_p, logprob, n_kept, logits_out, workspace,
                             _raw_stream(stream)))
     return tokens
+
+
+# ---- whole prompts (include/spec_prompt.h) -------------------------------------------------------------
+# Checked and marshalled as the 8-bit calls are.
+
+def _place(stream):
+    """The raw stream, and the device whose tensors a call on it takes: the current one."""
+    device = torch._C._cuda_getDevice()
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device) or None, device
+    if stream.device_index != device:
+        raise ValueError(f"stream: of device {stream.device_index}, the current one is {device}")
+    return stream.cuda_stream or None, device
+
+
+PROMPT_ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "swiglu": 4}
+
+
+def spec_prompt_rmsnorm(x: torch.Tensor, gain: torch.Tensor, eps: float, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rows of x [rows][cols] (float32 or bfloat16, any row stride), normalised, times gain -> y bf16."""
+    if y is None:
+        y = _new(x.shape, torch.bfloat16, x.device, stream)
+    _check(_native().prompt_rmsnorm(x, gain, eps, y, *_place(stream)))
+    return y
+
+
+def spec_prompt_gemm_workspace_bytes(M: int, N: int, K: int, activation: str = "none") -> int:
+    return int(lib().spec_prompt_gemm_workspace_bytes(M, N, K, PROMPT_ACTIVATIONS[activation]))
+
+
+def spec_prompt_gemm(x: torch.Tensor, w_packed: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none",
+                     residual: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """y [M][N] (float32 or bfloat16) = residual + activation(x [M][K] bf16 times the packed matrix + bias); any row strides.  residual may be
+    y.  "swiglu": the matrix is gate and up, packed with interleave_halves, and has 2 N rows."""
+    code = PROMPT_ACTIVATIONS.get(activation)
+    if code is None:
+        raise ValueError(f"activation: expected one of {', '.join(PROMPT_ACTIVATIONS)}, got {activation!r}")
+    _check(_native().prompt_gemm(x, w_packed, y, bias, code, residual, workspace, *_place(stream)))
+    return y
+
+
+def spec_prompt_append(h: Handle, layer: int, qkv: torch.Tensor, rotated: torch.Tensor, row0: torch.Tensor, seq_slot: torch.Tensor,
+                       pos0: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """Rotary embedding of qkv's queries and keys -> rotated (may be qkv's own first columns); keys and values -> the handle's cache, row j
+    of sequence b at position pos0[b] + j (None: j) of slot seq_slot[b]."""
+    c = h.cfg
+    _check(_native().prompt_append(h.ptr, layer, qkv, rotated, row0, seq_slot, pos0, (c.n_q_heads + c.n_kv_heads) * c.head_dim,
+                                   (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, *_place(stream)))
+    return rotated
+
+
+def spec_prompt_attention_workspace_bytes(q_rows: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().spec_prompt_attention_workspace_bytes(q_rows, batch, n_q_heads, n_kv_heads, head_dim))
+
+
+def spec_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_q_heads: int, n_kv_heads: int, q_row0: torch.Tensor,
+                          out: torch.Tensor, scale: float, k_row0: Optional[torch.Tensor] = None, max_q_len: int = 0, max_k_len: int = 0,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """out bf16 [q_rows][n_q_heads * head_dim]: causal attention of packed sequences; q, k, v, out: any row strides that are multiples of 8."""
+    _check(_native().prompt_attention(q, k, v, n_q_heads, n_kv_heads, q_row0, k_row0, out, scale, max_q_len, max_k_len, workspace,
+                                      *_place(stream)))
+    return out
 
 
 class Lookahead:

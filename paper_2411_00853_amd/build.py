@@ -13,7 +13,7 @@ LIB = os.path.join(HERE, "libspecverify.so")
 NATIVE = os.path.join(HERE, "_native.so")
 SOURCES = ["attention.hip", "attention_reuse.hip", "spec_verify.hip", "forward.hip", "sampler.hip", "gemm.hip",
            "elementwise.hip", "probe.hip", "decode.hip", "lookahead.hip", "q8_rows.hip", "q8_gemm.hip", "kv8.hip",
-           "filter_sample.hip"]
+           "filter_sample.hip", "prompt_rows.hip", "prompt_gemm.hip", "prompt_attention.hip"]
 # packed-fp32 instructions are disabled for all device code.  The first kernel arguments (up to 14 dwords, whole structs
 # excepted) come in scalar registers with the wavefront instead of by a load that every wavefront waits for before its
 # first address: a step is a chain of small launches (1B shape, batch 1, 120 of them: 812 -> 787 us).  Kernels list

@@ -1,4 +1,4 @@
-// Marshalling of tensors for the calls of spec_q8.h, as an extension module: these calls last a few microseconds on the GPU, and
+// Marshalling of tensors for the calls of spec_q8.h and spec_prompt.h, as an extension module: these calls last a few microseconds on the GPU, and
 // reading a tensor's type, shape and address from Python took as long again for every call.  Checks of arguments only -- no arithmetic,
 // no allocation, and the functions called are the library's, whose addresses bind() receives.
 #include <Python.h>
@@ -7,6 +7,7 @@
 #include <stdexcept>
 #include <string>
 
+#include "../../include/spec_prompt.h"
 #include "../../include/spec_q8.h"
 
 namespace {
@@ -25,6 +26,10 @@ struct Library {
     decltype(&spec_kv8_append) append;
     decltype(&spec_kv8_attention) attention;
     decltype(&spec_filter_sample) sample;
+    decltype(&spec_prompt_rmsnorm) prompt_rmsnorm;
+    decltype(&spec_prompt_gemm) prompt_gemm;
+    decltype(&spec_prompt_append) prompt_append;
+    decltype(&spec_prompt_attention) prompt_attention;
 } lib{};
 
 std::string text(at::IntArrayRef s)
@@ -251,6 +256,113 @@ int sample(PyObject* const* a)   // logits, uniforms, temperature, tokens, top_k
     return lib.sample(&args, &out, ws, bytes, stream_of(a[11]));
 }
 
+// The calls on prompts take tensors of the device that is current (their last argument)
+const at::Tensor& here(PyObject* o, const char* name, PyObject* device)
+{
+    const at::Tensor& t = tensor(o, name);
+    if (t.get_device() != integer(device, "device"))
+        throw Bad(std::string(name) + ": of device " + std::to_string(t.get_device()) + ", the current one is " + std::to_string(integer(device, "device")));
+    return t;
+}
+void* optional_here(PyObject* o, at::IntArrayRef shape, at::ScalarType type, const char* name, PyObject* device)
+{
+    return o == Py_None ? nullptr : shaped(here(o, name, device), shape, type, name);
+}
+
+struct Scratch {
+    void* p;
+    size_t bytes;
+};
+Scratch scratch(PyObject* o, PyObject* device)
+{
+    if (o == Py_None) return {nullptr, 0};
+    const at::Tensor& t = here(o, "workspace", device);
+    return {whole(t, "workspace"), t.nbytes()};
+}
+
+// Rows of bf16 numbers, `cols` of them (less than 0: any number)
+Rows bf16_rows(const at::Tensor& t, int64_t cols, const char* name)
+{
+    const Rows r = rows_of(t, name);
+    if (t.scalar_type() != BF16 || (cols >= 0 && r.cols != cols))
+        throw Bad(std::string(name) + ": expected BFloat16 rows" + (cols < 0 ? "" : " of " + std::to_string(cols)) + ", got " +
+                  at::toString(t.scalar_type()) + " " + text(t.sizes()));
+    return r;
+}
+
+int prompt_rmsnorm(PyObject* const* a)   // x, gain, eps, y, stream, device
+{
+    const at::Tensor& x = here(a[0], "x", a[5]);
+    const Rows r = rows_of(x, "x");
+    return lib.prompt_rmsnorm(r.p, code(x, "x"), r.ld, (float*)shaped(here(a[1], "gain", a[5]), {r.cols}, F32, "gain"), real(a[2], "eps"), r.rows, r.cols,
+                              shaped(here(a[3], "y", a[5]), x.sizes(), BF16, "y"), stream_of(a[4]));
+}
+
+int prompt_gemm(PyObject* const* a)   // x, w_packed, y, bias, activation, residual, workspace, stream, device
+{
+    const at::Tensor &w = here(a[1], "w_packed", a[8]), &y = here(a[2], "y", a[8]);
+    const Rows x = bf16_rows(here(a[0], "x", a[8]), -1, "x"), o = rows_of(y, "y");
+    spec_prompt_epilogue e{};
+    e.activation = integer(a[4], "activation");
+    const int64_t n_out = (int64_t)o.cols * (e.activation == SPEC_ACT_SWIGLU ? 2 : 1), kp = ((int64_t)x.cols + 127) / 128 * 128;
+    if (o.rows != x.rows) throw Bad("y: expected " + std::to_string(x.rows) + " rows, got " + std::to_string(o.rows));
+    if (w.scalar_type() != BF16 || w.numel() != (n_out + 15) / 16 * 16 * kp)
+        throw Bad("w_packed: expected a packed BFloat16 matrix of " + std::to_string(n_out) + " x " + std::to_string(x.cols));
+    e.bias = (const float*)optional_here(a[3], {n_out}, F32, "bias", a[8]);
+    if (a[5] != Py_None) {
+        const at::Tensor& t = here(a[5], "residual", a[8]);
+        const Rows r = rows_of(t, "residual");
+        if (t.sizes() != y.sizes()) throw Bad("residual: expected shape " + text(y.sizes()) + ", got " + text(t.sizes()));
+        e.residual = r.p;
+        e.ld_residual = r.ld;
+        e.residual_dtype = code(t, "residual");
+    }
+    const Scratch s = scratch(a[6], a[8]);
+    return lib.prompt_gemm(x.p, x.ld, whole(w, "w_packed"), &e, o.p, code(y, "y"), o.ld, x.rows, o.cols, x.cols, s.p, s.bytes, stream_of(a[7]));
+}
+
+int prompt_append(PyObject* const* a)   // handle, layer, qkv, rotated, row0, seq_slot, pos0, rotated columns, qkv columns, stream, device
+{
+    const at::Tensor& row0 = here(a[4], "row0", a[10]);
+    const Rows x = bf16_rows(here(a[2], "qkv", a[10]), integer(a[8], "columns"), "qkv"), o = bf16_rows(here(a[3], "rotated", a[10]), integer(a[7], "columns"), "rotated");
+    if (o.rows != x.rows) throw Bad("rotated: expected " + std::to_string(x.rows) + " rows, got " + std::to_string(o.rows));
+    if (row0.dim() != 1 || !row0.size(0)) throw Bad("row0: expected the sequences' first rows and one number more");
+    const int64_t batch = row0.size(0) - 1;
+    return lib.prompt_append((spec_handle*)PyLong_AsVoidPtr(a[0]), integer(a[1], "layer"), x.p, x.ld, o.p, o.ld,
+                             (const int32_t*)shaped(row0, {batch + 1}, I32, "row0"), (const int32_t*)shaped(here(a[5], "seq_slot", a[10]), {batch}, I32, "seq_slot"),
+                             (const int32_t*)optional_here(a[6], {batch}, I32, "pos0", a[10]), narrow(batch, "row0"), x.rows, stream_of(a[9]));
+}
+
+int prompt_attention(PyObject* const* a)   // q, k, v, n_q_heads, n_kv_heads, q_row0, k_row0, out, scale, max_q_len, max_k_len, workspace, stream, device
+{
+    const at::Tensor& row0 = here(a[5], "q_row0", a[13]);
+    spec_prompt_attn_args p{};
+    p.n_q_heads = integer(a[3], "n_q_heads");
+    p.n_kv_heads = integer(a[4], "n_kv_heads");
+    if (p.n_q_heads <= 0 || p.n_kv_heads <= 0) throw Bad("n_q_heads, n_kv_heads: expected positive numbers");
+    const Rows q = bf16_rows(here(a[0], "q", a[13]), -1, "q");
+    if (q.cols % p.n_q_heads) throw Bad("q: " + std::to_string(q.cols) + " columns are not those of " + std::to_string(p.n_q_heads) + " heads");
+    p.head_dim = q.cols / p.n_q_heads;
+    const Rows k = bf16_rows(here(a[1], "k", a[13]), (int64_t)p.n_kv_heads * p.head_dim, "k"), v = bf16_rows(here(a[2], "v", a[13]), k.cols, "v"),
+               out = bf16_rows(here(a[7], "out", a[13]), q.cols, "out");
+    if (v.rows != k.rows) throw Bad("v: expected " + std::to_string(k.rows) + " rows, got " + std::to_string(v.rows));
+    if (out.rows != q.rows) throw Bad("out: expected " + std::to_string(q.rows) + " rows, got " + std::to_string(out.rows));
+    if (row0.dim() != 1 || !row0.size(0)) throw Bad("q_row0: expected the sequences' first rows and one number more");
+    if (a[6] == Py_None && k.rows != q.rows) throw Bad("k_row0: sequences of " + std::to_string(k.rows) + " key rows need their own");
+    p.q = q.p, p.k = k.p, p.v = v.p, p.out = out.p;
+    p.ld_q = q.ld, p.ld_k = k.ld, p.ld_v = v.ld, p.ld_out = out.ld;
+    p.q_row0 = (const int32_t*)shaped(row0, {row0.size(0)}, I32, "q_row0");
+    p.k_row0 = (const int32_t*)optional_here(a[6], {row0.size(0)}, I32, "k_row0", a[13]);
+    p.batch = narrow(row0.size(0) - 1, "q_row0");
+    p.q_rows = q.rows;
+    p.k_rows = k.rows;
+    p.scale = real(a[8], "scale");
+    p.max_q_len = integer(a[9], "max_q_len");
+    p.max_k_len = integer(a[10], "max_k_len");
+    const Scratch s = scratch(a[11], a[13]);
+    return lib.prompt_attention(&p, s.p, s.bytes, stream_of(a[12]));
+}
+
 template <int (*F)(PyObject* const*), Py_ssize_t COUNT>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -266,12 +378,13 @@ PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n)
 
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-    if (n != 7) {
-        PyErr_SetString(PyExc_ValueError, "expected the addresses of seven functions");
+    constexpr Py_ssize_t COUNT = sizeof(Library) / sizeof(void*);
+    if (n != COUNT) {
+        PyErr_SetString(PyExc_ValueError, "expected the addresses of as many functions as there are calls");
         return nullptr;
     }
-    void* p[7];
-    for (int i = 0; i < 7; ++i) {
+    void* p[COUNT];
+    for (int i = 0; i < COUNT; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a function's address is null");
@@ -279,7 +392,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
         }
     }
     lib = {(decltype(lib.quantize))p[0], (decltype(lib.add_rmsnorm))p[1], (decltype(lib.swiglu))p[2], (decltype(lib.gemm))p[3],
-           (decltype(lib.append))p[4], (decltype(lib.attention))p[5], (decltype(lib.sample))p[6]};
+           (decltype(lib.append))p[4], (decltype(lib.attention))p[5], (decltype(lib.sample))p[6], (decltype(lib.prompt_rmsnorm))p[7],
+           (decltype(lib.prompt_gemm))p[8], (decltype(lib.prompt_append))p[9], (decltype(lib.prompt_attention))p[10]};
     Py_RETURN_NONE;
 }
 
@@ -292,6 +406,10 @@ PyMethodDef methods[] = {ENTRY("bind", bind),
                          ENTRY("append", (call<append, 12>)),
                          ENTRY("attention", (call<attention, 14>)),
                          ENTRY("sample", (call<sample, 12>)),
+                         ENTRY("prompt_rmsnorm", (call<prompt_rmsnorm, 6>)),
+                         ENTRY("prompt_gemm", (call<prompt_gemm, 9>)),
+                         ENTRY("prompt_append", (call<prompt_append, 11>)),
+                         ENTRY("prompt_attention", (call<prompt_attention, 14>)),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -14,6 +14,7 @@ from typing import Optional
 import torch
 
 from . import binding as sv
+from .prompt import Prompt, pack_weights
 
 _F8 = torch.float8_e4m3fn
 
@@ -128,15 +129,13 @@ class Draft8:
 class Rounds:
     """A bf16 target and the Draft8 that proposes to it: `feed` a context, then `round` after round.  Sequence b is slot b of both."""
 
-    def __init__(self, target_shape, weights: dict, draft: Draft8, lookahead: int):
-        """weights: as workload.make_weights gives them, on the device."""
+    def __init__(self, target_shape, weights: dict, draft: Draft8, lookahead: int, prompt_rows: int = 0):
+        """weights: as workload.make_weights gives them, on the device.  prompt_rows > 0: `feed` takes contexts of up to so many tokens in all through
+        the target as whole prompts; else window by window."""
         B, V, K, dev = draft.batch, target_shape.vocab, lookahead, draft.embed.device
         self.draft, self.K, self.B = draft, K, B
         cfg = sv.make_cfg(target_shape, B, draft.max_kv_len, K)
-        packed = {"tok_embed": weights["tok_embed"], "final_norm": weights["final_norm"], "lm_head": sv.spec_pack_weight(weights["lm_head"]),
-                  "layers": [{"attn_norm": lw["attn_norm"], "ffn_norm": lw["ffn_norm"], "w_qkv": sv.spec_pack_weight(lw["w_qkv"]),
-                              "w_o": sv.spec_pack_weight(lw["w_o"]), "w_gate_up": sv.spec_pack_weight(lw["w_gate_up"], True),
-                              "w_down": sv.spec_pack_weight(lw["w_down"])} for lw in weights["layers"]]}
+        packed = pack_weights(weights)
         cache = torch.zeros(sv.spec_kv_cache_bytes(cfg), dtype=torch.uint8, device=dev)
         self.kv_len = torch.zeros(B, dtype=torch.int32, device=dev)   # of the target; the position of `last` on both sides
         self.handle = sv.spec_verify_init(cfg, packed, cache, self.kv_len)
@@ -144,6 +143,7 @@ class Rounds:
         self.prev, self.last, self.slots = ints(B), ints(B), torch.arange(B, dtype=torch.int32, device=dev)
         self.tokens, self.n_accepted, self.out = ints(B, K), ints(B), ints(B, K + 1)
         self.logits = torch.zeros((B, K, V), device=dev)
+        self.prompt = Prompt(self.handle, packed, prompt_rows) if prompt_rows else None
 
     def feed(self, context: torch.Tensor):
         """context int32 [batch][n], n >= 2: into both caches, in windows; its last token is the first one to be decoded."""
@@ -152,6 +152,13 @@ class Rounds:
         for t in range(0, n - 1, d.max_window):
             window = context[:, t:min(t + d.max_window, n - 1)].contiguous()
             d.feed(window, at + t, logits=False)
+        self.prev.copy_(context[:, n - 2])
+        self.last.copy_(context[:, n - 1])
+        if self.prompt is not None:
+            row0 = torch.arange(self.B + 1, dtype=torch.int32, device=context.device) * (n - 1)
+            self.prompt.run(context[:, :n - 1].reshape(-1), row0, self.slots, n - 1, logits=False)
+            self.kv_len.fill_(n - 1)
+            return
         # the target scores a window as it does proposals, and keeps all of it
         half = torch.full((self.B, self.K + 1), 0.5, device=context.device)
         for t in range(0, n - 1, self.K + 1):
@@ -160,8 +167,6 @@ class Rounds:
             sv.spec_verify_step(self.handle, [window.shape[1] - 1] * self.B, half, 1.0, self.n_accepted, self.out, seq_slot=self.slots,
                                 last_token=window[:, 0].contiguous(), draft_tokens=self.tokens, draft_logits=self.logits,
                                 auto_rollback=False)
-        self.prev.copy_(context[:, n - 2])
-        self.last.copy_(context[:, n - 1])
 
     def propose(self, uniforms: torch.Tensor, max_len: int = 0):
         self.draft.propose(self.prev, self.last, self.kv_len, uniforms, self.tokens, self.logits, max_len)
@@ -191,6 +196,7 @@ def main():
     ap.add_argument("--top-k", type=int)
     ap.add_argument("--top-p", type=float)
     ap.add_argument("--min-p", type=float)
+    ap.add_argument("--prompt", action="store_true", help="the context goes through the target as whole prompts, not window by window")
     a = ap.parse_args()
     B, K, T = a.batch, a.lookahead, a.temperature
     W = 3   # rounds before the clock starts
@@ -199,7 +205,7 @@ def main():
     shape = wl.SEVEN_B if a.model == "target" else wl.SEVEN_B_DRAFT
     own = weights if a.model == "target" else wl.make_weights(shape, wl.SEED_BASE + 3, "cuda")
     draft = Draft8(shape, own, B, max_kv, 64, T, a.top_k, a.top_p, a.min_p)
-    rounds = Rounds(wl.SEVEN_B, weights, draft, K)
+    rounds = Rounds(wl.SEVEN_B, weights, draft, K, B * a.context if a.prompt else 0)
     del weights, own
     rng = wl.Rng(wl.SEED_BASE + 4, "cuda")
     rounds.feed(rng.randint(wl.S_TOKENS, (B, a.context), shape.vocab))

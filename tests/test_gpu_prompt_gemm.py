@@ -1,0 +1,140 @@
+"""The product of packed prompts against the plain product in 64 bits: exactly where whole numbers leave nothing to round, within the
+roundings elsewhere."""
+import pytest
+import torch
+
+import prompt_ref as ref
+from paper_2411_00853_amd import binding as sv
+
+pytestmark = pytest.mark.gpu
+BF16, F32 = torch.bfloat16, torch.float32
+
+SIZES = [(1, 16, 32), (1, 1000, 4096), (2, 17, 96), (15, 333, 128), (16, 256, 160), (17, 48, 224), (31, 100, 1056), (33, 500, 2080), (48, 4096, 512),
+         (63, 31, 320), (64, 64, 64), (65, 16, 32), (100, 130, 288), (127, 513, 96), (128, 1024, 1024), (129, 257, 160), (200, 900, 416),
+         (255, 256, 256), (256, 512, 128), (257, 272, 352), (352, 2048, 512), (500, 333, 1504), (777, 1030, 736), (1030, 4104, 2080), (2048, 256, 64)]
+
+
+def work(M, N, K, act="none"):
+    return torch.empty(max(16, sv.spec_prompt_gemm_workspace_bytes(M, N, K, act)), dtype=torch.uint8, device="cuda")
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("with_work", (False, True))
+def test_whole_numbers_are_exact(M, N, K, with_work):
+    """Products of numbers up to 8, at most 4096 of them: every partial sum is a whole number below 2^19."""
+    x, w = ref.small_ints(M + 1, M, K), ref.small_ints(N + 2, N, K)
+    y = torch.full((M, N), 7.0, device="cuda")
+    sv.spec_prompt_gemm(x, ref.pack(w), y, workspace=work(M, N, K) if with_work else None)
+    assert torch.equal(y.double(), ref.product(x, w))
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 48, 64), (40, 80, 96), (90, 1008, 160), (333, 528, 224)])
+@pytest.mark.parametrize("act", ("none", "relu", "gelu", "silu", "swiglu"))
+@pytest.mark.parametrize("y_type", (F32, BF16))
+def test_epilogue(M, N, K, act, y_type):
+    """v = x w + b is a sum of K products and a bias in fp32: off by at most (K + 1) 2^-23 of the sum of their magnitudes, S.  No activation's
+    slope exceeds 1.13 (gelu, silu), which swiglu's product carries over to the other half; the function itself adds some 2^-20 of its result."""
+    n_out = 2 * N if act == "swiglu" else N
+    x, w = ref.normal(1, M, K, dtype=BF16), ref.normal(2, n_out, K, std=K ** -0.5, dtype=BF16)
+    bias = ref.normal(3, n_out)
+    S = (x.double().abs() @ w.double().abs().t().contiguous() + bias.double().abs()) * ((K + 1) * 2.0 ** -23) * 1.13
+    v = ref.product(x, w, bias)
+    if act == "swiglu":
+        g, u = v.chunk(2, -1)
+        S = S[:, :N] * u.abs() + S[:, N:] * g.abs() + S[:, :N] * S[:, N:]
+    for residual in (None, ref.normal(4, M, N), ref.normal(5, M, N, dtype=BF16)):
+        if act == "swiglu" and residual is not None:
+            residual = residual * 3
+        want = ref.product(x, w, bias, act, residual)
+        y = torch.full((M, N), 7.0, dtype=y_type, device="cuda")
+        sv.spec_prompt_gemm(x, ref.pack(w, act == "swiglu"), y, bias=bias, activation=act, residual=residual, workspace=work(M, N, K, act))
+        size = want.abs() + (0 if residual is None else residual.double().abs())
+        tol = S + size * 2.0 ** -20 + want.abs() * (ref.HALF_BF16 if y_type == BF16 else ref.HALF_F32) * 1.01 + 1e-30
+        assert torch.all((y.double() - want).abs() <= tol)
+
+
+@pytest.mark.parametrize("M", (3, 50, 100, 300))
+def test_strides_odd_columns_and_what_lies_around(M):
+    N, K = 333, 96
+    xs = torch.full((M, K + 40), float("nan"), dtype=BF16, device="cuda")
+    xs[:, 8:8 + K] = ref.small_ints(1, M, K)
+    w = ref.small_ints(2, N, K)
+    bias = ref.small_ints(3, N).float()
+    for y_type in (F32, BF16):
+        for ld, at in ((N + 3, 1), (N + 5, 4), (N, 0)):
+            ys = torch.full((M, ld), 7.0, dtype=y_type, device="cuda")
+            rs = ref.small_ints(4, M, ld + 2).to(y_type)
+            y, r = ys[:, at % (ld - N + 1):][:, :N], rs[:, 1:1 + N]
+            sv.spec_prompt_gemm(xs[:, 8:8 + K], ref.pack(w), y, bias=bias, residual=r)
+            want = ref.product(xs[:, 8:8 + K], w, bias, residual=r)
+            assert torch.equal(y, want.to(y_type))
+            ys[:, at % (ld - N + 1):][:, :N] = 7.0
+            assert torch.all(ys == 7.0)
+
+
+@pytest.mark.parametrize("M", (1, 37, 128, 600))
+def test_residual_in_place(M):
+    N, K = 512, 320
+    x, w = ref.small_ints(1, M, K), ref.small_ints(2, N, K)
+    y = ref.small_ints(3, M, N).float()
+    want = ref.product(x, w, residual=y)
+    sv.spec_prompt_gemm(x, ref.pack(w), y, residual=y, workspace=work(M, N, K))
+    assert torch.equal(y.double(), want)
+
+
+@pytest.mark.parametrize("M", (2, 40, 100, 400))
+@pytest.mark.parametrize("K", (32, 96, 160, 224))
+def test_infinities_and_nan_stay_in_their_rows(M, K):
+    """Also where K ends inside a stage: the row after a row's end is not multiplied by the zeros that fill the packed matrix up."""
+    N = 80
+    x, w = ref.small_ints(1, M, K), ref.small_ints(2, N, K).abs() + 1
+    want = ref.product(x, w)
+    x[M // 2, 0], want[M // 2] = float("inf"), float("inf")
+    if M > 3:
+        x[0, K - 1], want[0] = float("nan"), float("nan")
+        x[M - 1, 3], want[M - 1] = float("-inf"), float("-inf")
+    y = torch.empty((M, N), device="cuda")
+    sv.spec_prompt_gemm(x, ref.pack(w), y, workspace=work(M, N, K))
+    assert torch.equal(torch.nan_to_num(y.double(), 1e9, 2e9, -2e9), torch.nan_to_num(want, 1e9, 2e9, -2e9))
+
+
+@pytest.mark.parametrize("act", ("relu", "silu", "gelu", "swiglu"))
+def test_activations_far_out(act):
+    """silu and gelu of very negative numbers are 0 and of very positive ones the numbers; relu keeps NaN."""
+    vals = torch.tensor([-1e30, -200.0, -90.0, -0.0, 0.0, 90.0, 200.0, 1e30, float("nan")], device="cuda")
+    K, N = 32, 16
+    x = torch.zeros((len(vals), K), dtype=BF16, device="cuda")
+    w = torch.zeros((2 * N if act == "swiglu" else N, K), dtype=BF16, device="cuda")
+    bias = torch.ones(w.shape[0], device="cuda")
+    for i, v in enumerate(vals.tolist()):
+        bias[:N] = v
+        y = torch.empty((len(vals), N), device="cuda")
+        sv.spec_prompt_gemm(x, ref.pack(w, act == "swiglu"), y, bias=bias, activation=act)
+        want = ref.activate(bias.double()[None], act).float()[:, :N]
+        assert torch.allclose(y[:1], want, rtol=1e-6, atol=1e-30, equal_nan=True), v
+
+
+def test_no_rows():
+    y = torch.empty((0, 48), device="cuda")
+    sv.spec_prompt_gemm(torch.empty((0, 64), dtype=BF16, device="cuda"), ref.pack(ref.small_ints(1, 48, 64)), y)
+
+
+def test_replayed_and_on_another_stream():
+    M, N, K = 21, 700, 512
+    x, w = ref.small_ints(1, M, K), ref.small_ints(2, N, K)
+    packed, ws = ref.pack(w), work(M, N, K)
+    y = torch.zeros((M, N), device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    sv.spec_prompt_gemm(x, packed, y, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(y.double(), ref.product(x, w))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sv.spec_prompt_gemm(x, packed, y, workspace=ws)
+    for seed in range(3):
+        x.copy_(ref.small_ints(10 + seed, M, K))
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y.double(), ref.product(x, w))
