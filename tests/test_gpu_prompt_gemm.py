@@ -11,7 +11,8 @@ BF16, F32 = torch.bfloat16, torch.float32
 
 SIZES = [(1, 16, 32), (1, 1000, 4096), (2, 17, 96), (15, 333, 128), (16, 256, 160), (17, 48, 224), (31, 100, 1056), (33, 500, 2080), (48, 4096, 512),
          (63, 31, 320), (64, 64, 64), (65, 16, 32), (100, 130, 288), (127, 513, 96), (128, 1024, 1024), (129, 257, 160), (200, 900, 416),
-         (255, 256, 256), (256, 512, 128), (257, 272, 352), (352, 2048, 512), (500, 333, 1504), (777, 1030, 736), (1030, 4104, 2080), (2048, 256, 64)]
+         (255, 256, 256), (256, 512, 128), (257, 272, 352), (352, 2048, 512), (500, 333, 1504), (777, 1030, 736), (1030, 4104, 2080), (2048, 256, 64),
+         (1300, 2304, 416), (2100, 4000, 352), (2304, 2560, 1120), (300, 1100, 3104), (20, 4096, 4096), (150, 400, 8192), (4700, 300, 288), (1500, 16, 512)]
 
 
 def work(M, N, K, act="none"):
@@ -28,7 +29,7 @@ def test_whole_numbers_are_exact(M, N, K, with_work):
     assert torch.equal(y.double(), ref.product(x, w))
 
 
-@pytest.mark.parametrize("M,N,K", [(5, 48, 64), (40, 80, 96), (90, 1008, 160), (333, 528, 224)])
+@pytest.mark.parametrize("M,N,K", [(5, 48, 64), (40, 80, 96), (90, 1008, 160), (333, 528, 224), (70, 272, 2080), (600, 400, 1056), (1500, 2064, 352), (24, 2000, 1024)])
 @pytest.mark.parametrize("act", ("none", "relu", "gelu", "silu", "swiglu"))
 @pytest.mark.parametrize("y_type", (F32, BF16))
 def test_epilogue(M, N, K, act, y_type):
