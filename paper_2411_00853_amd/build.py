@@ -26,7 +26,8 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-mllvm", "-amdg
 # The GEMM kernels keep the default: several of their variants measured slower with this option.
 SOURCE_FLAGS = {"attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                 "attention_reuse.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-                "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+                "kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+                "prompt_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 OBJ_DIR = os.path.join(HERE, "_build")
 
 

@@ -30,30 +30,53 @@ __device__ __forceinline__ PromptSpan prompt_span(const int32_t* row0, int b, in
     return {lo, max(lo, hi)};
 }
 
+// n / d for 0 <= n < 2^31, by a product (the compiler's division by a number it does not know is some forty instructions)
+struct FastDiv {
+    uint32_t d, mul, shift;
+    FastDiv() = default;
+    explicit FastDiv(uint32_t by) : d(by)
+    {
+        uint32_t l = 0;
+        while (((uint64_t)1 << l) < by) ++l;
+        shift = 31 + l;
+        mul = (uint32_t)(((uint64_t)1 << shift) / by + 1);   // n (mul / 2^shift - 1 / d) < 2^31 2^-shift <= 1 / d: what is cut off is below a d-th
+    }
+    __device__ __forceinline__ int div(int n) const { return (int)(((uint64_t)(uint32_t)n * mul) >> shift); }
+};
+
+// The sum over the lanes up to and with each one (by DPP: a chain of six permutations through LDS takes 700 cycles)
+__device__ __forceinline__ int wave_scan(int v)
+{
+#define PR_STEP(CTRL, ROWS) v += __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false)
+    PR_STEP(0x111, 0xf);    // from 1, 2, 4, 8 lanes below within sixteen, then from the last lane of the sixteen, of the half below
+    PR_STEP(0x112, 0xf);
+    PR_STEP(0x114, 0xf);
+    PR_STEP(0x118, 0xf);
+    PR_STEP(0x142, 0xa);
+    PR_STEP(0x143, 0xc);
+#undef PR_STEP
+    return v;
+}
+
 // Which unit of work a workgroup has, if sequence b has count(b) units and they are numbered sequence by sequence: the sequence (-1: none,
 // there are fewer) and the number within it.  By all lanes of every wavefront alike, 64 sequences at a time.
 struct PromptUnit {
-    int seq, index;
+    int seq, index, lane;   // lane: which one has counted the sequence
 };
 template <typename COUNT>
 __device__ __forceinline__ PromptUnit prompt_unit(int unit, int batch, COUNT count)
 {
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < batch; b0 += 64) {
-        const int n = b0 + lane < batch ? count(b0 + lane) : 0;
-        int sum = n;   // up to and with this lane
-        for (int d = 1; d < 64; d <<= 1) {
-            const int below = __shfl_up(sum, d);
-            if (lane >= d) sum += below;
-        }
+        const int n = b0 + lane < batch ? count(b0 + lane) : 0, sum = wave_scan(n);
         const int total = __builtin_amdgcn_readlane(sum, 63);
         if (unit < total) {
             const int at = __builtin_ctzll(__ballot(unit < sum));
-            return {b0 + at, unit - __builtin_amdgcn_readlane(sum - n, at)};
+            return {b0 + at, unit - __builtin_amdgcn_readlane(sum - n, at), at};
         }
         unit -= total;
     }
-    return {-1, 0};
+    return {-1, 0, 0};
 }
 
 }  // namespace specv

@@ -10,6 +10,7 @@
 namespace specv {
 namespace {
 
+#define INLINE __attribute__((always_inline))   // (the kernel's lambdas: called, they would get scalars in vector registers)
 constexpr int BLK = 64;   // positions of a block
 
 struct Args {
@@ -17,10 +18,38 @@ struct Args {
     uint16_t* out;
     int64_t ld_q, ld_k, ld_v, ld_out;
     const int32_t *q_row0, *k_row0;
-    int n_kv_heads, group, batch, q_rows, k_rows;
+    FastDiv heads, group;   // kv heads; query heads of one
+    int batch, q_rows, k_rows;
     float factor;       // |scale| * log2(e), not zero: what is masked is -inf times it
     unsigned sign;      // 0x80008000 where the scale is negative: the queries are negated
+    FastDiv parts;      // a tile's keys are shared out among so many workgroups; with more than one, what they leave to the join:
+    float *part_o, *part_ml;   // [unit][kv head][part][row of the tile][head_dim] sums of weighted values, [..][2] maximum and sum of weights
 };
+
+// The tile of a unit (its number and kv head): of one sequence, some rows
+struct Tile {
+    int seq, q_begin, n_q, k_begin, n_k, n_rows, row0;
+};
+template <int TILE>
+__device__ __forceinline__ Tile find_tile(const Args& A, int number)
+{
+    const int group = A.group.d;
+    PromptSpan q_span{0, 0}, k_span{0, 0};   // of the sequence that this lane looks at
+    const PromptUnit unit = prompt_unit(number, A.batch, [&](int b) {
+        q_span = k_span = prompt_span(A.q_row0, b, A.q_rows);
+        if (A.k_row0) k_span = prompt_span(A.k_row0, b, A.k_rows);
+        return ((q_span.end - q_span.begin) * group + TILE - 1) / TILE;
+    });
+    Tile t;
+    t.seq = unit.seq;
+    t.q_begin = __builtin_amdgcn_readlane(q_span.begin, unit.lane);
+    t.n_q = __builtin_amdgcn_readlane(q_span.end, unit.lane) - t.q_begin;
+    t.k_begin = __builtin_amdgcn_readlane(k_span.begin, unit.lane);
+    t.n_k = __builtin_amdgcn_readlane(k_span.end, unit.lane) - t.k_begin;
+    t.n_rows = t.n_q * group;
+    t.row0 = ((t.n_rows + TILE - 1) / TILE - 1 - unit.index) * TILE;   // the tiles with the longest way first
+    return t;
+}
 
 // The largest of lane and lane ^ 32; their sum
 __device__ __forceinline__ float both_max(float v)
@@ -35,212 +64,272 @@ __device__ __forceinline__ float both_sum(float v)
 }
 
 typedef short pr_shortx4 __attribute__((ext_vector_type(4)));
+typedef __bf16 pr_bf16x2 __attribute__((ext_vector_type(2)));
 
 template <int HD, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, 2) attention_kernel(Args A)
+__global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) attention_kernel(Args A)
 {
     constexpr int ROW = 2 * HD, PART = BLK * ROW, KIB = PART / 1024;       // bytes of a row, of a block's keys; requests for them
     constexpr int PIECES = ROW / 16, ROWS = 1024 / ROW;                    // 16-byte pieces of a row, rows of a request
-    constexpr int U = KIB / WAVES > 0 ? KIB / WAVES : 1;
+    constexpr int U = KIB / WAVES, TILE = 32 * WAVES;
     static_assert(KIB % WAVES == 0, "every wavefront has as many requests");
     __shared__ __attribute__((aligned(16))) char lds[4 * PART];            // keys, keys, values, values
+    __shared__ int first[2][HD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r32 = lane & 31, half = lane >> 5;
-    const int head = blockIdx.x % A.n_kv_heads;
-    const int32_t* k_row0 = A.k_row0 ? A.k_row0 : A.q_row0;
-    const PromptUnit unit = prompt_unit(blockIdx.x / A.n_kv_heads, A.batch, [&](int b) {
-        const PromptSpan s = prompt_span(A.q_row0, b, A.q_rows);
-        return ((s.end - s.begin) * A.group + 32 * WAVES - 1) / (32 * WAVES);
-    });
-    if (unit.seq < 0) return;
-    const PromptSpan qs = prompt_span(A.q_row0, unit.seq, A.q_rows), ks = prompt_span(k_row0, unit.seq, A.k_rows);
-    const int n_q = qs.end - qs.begin, n_k = ks.end - ks.begin;
-    const int n_rows = n_q * A.group, n_tiles = (n_rows + 32 * WAVES - 1) / (32 * WAVES);
-    const int tile0 = (n_tiles - 1 - unit.index) * (32 * WAVES);           // the tiles with the longest way first
-    const int row = tile0 + wave * 32 + r32;
-    const bool live = row < n_rows;
-    const int at = min(row, n_rows - 1) / A.group, sub = min(row, n_rows - 1) - at * A.group;
-    const int last = n_k - n_q + at;                                        // the last position that this lane's row sees
-    const int last_first = n_k - n_q + tile0 / A.group, last_last = n_k - n_q + (min(tile0 + 32 * WAVES, n_rows) - 1) / A.group;
-    const int n_blocks = last_last < 0 ? 0 : last_last / BLK + 1;
-    const int n_clear = last_first < 0 ? 0 : (last_first + 1) / BLK;       // blocks that all rows see whole
+    const int job = A.parts.div(blockIdx.x), part = (int)blockIdx.x - job * (int)A.parts.d;
+    const int number = A.heads.div(job), head = job - number * (int)A.heads.d, group = A.group.d;
+    const Tile T = find_tile<TILE>(A, number);
+    if (T.seq < 0) return;
+    const int tile0 = T.row0, n_rows = T.n_rows, q_begin = T.q_begin;
+    const int last_first = T.n_k - T.n_q + A.group.div(tile0), last_last = T.n_k - T.n_q + A.group.div(min(tile0 + TILE, n_rows) - 1);
+    const int all_blocks = last_last < 0 ? 0 : last_last / BLK + 1;
+    // This part's blocks; all positions below are counted from their first one
+    const int block0 = A.parts.div(all_blocks * part), n_blocks = A.parts.div(all_blocks * (part + 1)) - block0, p_first = block0 * BLK;
+    const int n_k = T.n_k - p_first, k_begin = T.k_begin + p_first;
+    const int n_clear = last_first < p_first ? 0 : (last_first - p_first + 1) / BLK;       // blocks that all rows see whole
 
+    // A row of LDS holds the pieces of a row of keys in the order piece ^ key_turn(row), of values piece ^ value_turn(row): the lanes that a read
+    // serves at once (sixteen of keys, 32 of values) then find different groups of banks
+    auto key_turn = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
+    auto value_turn = [](int r) { return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const char* const kb = (const char*)(A.k + (size_t)k_begin * A.ld_k + (size_t)head * HD);
+    const char* const vb = (const char*)(A.v + (size_t)k_begin * A.ld_v + (size_t)head * HD);
+    uint32_t k_off[U], v_off[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int r = (wave * U + u) * ROWS + lane / PIECES;
+        k_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_k) + (lane % PIECES ^ key_turn(r)) * 16;
+        v_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn(r)) * 16;
+    }
+    auto fetch_part = [&](const char* base, int64_t ld, const uint32_t (&off)[U], int block, uint32_t to, auto turn) INLINE {
+        const int p0 = block * BLK;
+        const char* from = base + (size_t)p0 * ld * 2;
+        if (p0 + BLK <= n_k) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) q8_fetch_lds(from, off[u], to + (wave * U + u) * 1024);
+        } else {        // (beyond the end: the last row again)
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int r = (wave * U + u) * ROWS + lane / PIECES;
+                q8_fetch_lds(from, (uint32_t)min(r, n_k - 1 - p0) * (uint32_t)(2 * ld) + (lane % PIECES ^ turn(r)) * 16, to + (wave * U + u) * 1024);
+            }
+        }
+    };
+    auto fetch_keys = [&](int block) INLINE { fetch_part(kb, A.ld_k, k_off, block, lds0 + (block & 1) * PART, key_turn); };
+    auto fetch_values = [&](int block) INLINE { fetch_part(vb, A.ld_v, v_off, block, lds0 + (2 + (block & 1)) * PART, value_turn); };
+
+    if (n_blocks) {
+        fetch_keys(0);
+        fetch_values(0);
+        if (n_blocks > 1) fetch_keys(1);
+    }
+    // (the fetches are under way) the lane's query row, and the last position that it sees
+    auto place = [&](int row) {   // position in the sequence and query head of a tile's row
+        row = min(tile0 + row, n_rows - 1);
+        const int at = A.group.div(row);
+        return make_int2(at, row - at * group);
+    };
+    int last;
     pr_bf16x8 qf[HD / 16];
     {
-        const uint16_t* src = A.q + (size_t)(qs.begin + at) * A.ld_q + (size_t)(head * A.group + sub) * HD + 8 * half;
+        const int2 to = place(wave * 32 + r32);
+        last = n_k - T.n_q + to.x;
+        const uint16_t* src = A.q + (size_t)(q_begin + to.x) * A.ld_q + (size_t)(head * group + to.y) * HD + 8 * half;
 #pragma unroll
-        for (int s = 0; s < HD / 16; ++s) {
-            pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(src + 16 * s);
+        for (int c = 0; c < HD / 16; ++c) {
+            pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(src + 16 * c);
             v ^= A.sign;
-            qf[s] = __builtin_bit_cast(pr_bf16x8, v);
+            qf[c] = __builtin_bit_cast(pr_bf16x8, v);
         }
     }
 
-    // A row of LDS holds the pieces of a row of keys in the order piece ^ key_turn(row), of values piece ^ value_turn(row): neighbouring lanes of a
-    // read then find different groups of banks
-    auto key_turn = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
-    auto value_turn = [](int r) { return HD == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); };
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
-    const char* const kb = (const char*)(A.k + (size_t)ks.begin * A.ld_k + (size_t)head * HD);
-    const char* const vb = (const char*)(A.v + (size_t)ks.begin * A.ld_v + (size_t)head * HD);
-    auto fetch = [&](int block) {
-        const int p0 = block * BLK;
-        const char* kp = kb + (size_t)p0 * A.ld_k * 2;
-        const char* vp = vb + (size_t)p0 * A.ld_v * 2;
-        const uint32_t to = lds0 + (block & 1) * PART;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = wave * U + u, r = i * ROWS + lane / PIECES, piece = lane % PIECES;
-            const uint32_t from = (uint32_t)min(r, n_k - 1 - p0);     // (beyond the end: the last row again)
-            q8_fetch_lds(kp, from * (uint32_t)(2 * A.ld_k) + (piece ^ key_turn(r)) * 16, to + i * 1024);
-            q8_fetch_lds(vp, from * (uint32_t)(2 * A.ld_v) + (piece ^ value_turn(r)) * 16, to + 2 * PART + i * 1024);
-        }
+    struct Scores {
+        pr_floatx16 v[2];
     };
-
     pr_floatx16 o[HD / 32];
+    Scores s0, s1;
+    float m = -INFINITY, l[2] = {0.f, 0.f};   // (two sums, of even and of odd sixteens: one would be a chain of additions)
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
 
     // where this lane reads keys (rows r32, r32 + 32) and values (rows 4 half + (lane & 15) / 4 + 8 j)
     const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn(v_row);
-    auto step = [&](int block, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        const char* kl = lds + (block & 1) * PART + r32 * ROW;
-        const char* vl = lds + (2 + (block & 1)) * PART + v_row * ROW + (lane & 1) * 8;
-        pr_floatx16 s[2];
+    auto key = [&](int par, int p, int c) INLINE {   // par: of the block's number, odd or even
+        return *reinterpret_cast<const pr_bf16x8*>(lds + par * PART + (r32 + 32 * p) * ROW + ((2 * c + half) ^ key_turn(r32)) * 16);
+    };
+    auto value = [&](int par, int d, int k) INLINE {   // the operand of dims 32 d .. and positions 16 k ..
+        const char* vl = lds + (2 + par) * PART + v_row * ROW + (lane & 1) * 8;
+        const int piece = ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_turn) * 16;
+        union {
+            pr_shortx4 h[2];
+            pr_bf16x8 f;
+        } vf;
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
+        for (int j = 0; j < 2; ++j)
+            vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) pr_shortx4*)(vl + (16 * k + 8 * j) * ROW + piece));
+        return vf.f;
+    };
+    auto scores = [&](Scores& t, int par, int p) INLINE {   // of positions 32 p .. 32 p + 31
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[p][i] = 0.f;
+        for (int i = 0; i < 16; ++i) t.v[p][i] = 0.f;
 #pragma unroll
-            for (int c = 0; c < HD / 16; ++c) {
-                const pr_bf16x8 kf = *reinterpret_cast<const pr_bf16x8*>(kl + p * 32 * ROW + ((2 * c + half) ^ key_turn(r32)) * 16);
-                s[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s[p], 0, 0, 0);
-            }
-        }
-        if (MASKED) {
+        for (int c = 0; c < HD / 16; ++c) t.v[p] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key(par, p, c), qf[c], t.v[p], 0, 0, 0);
+    };
+    // The row's maximum over what it has seen, or what is left of one that is smaller by a factor of at most 2^8: the sums hold weights up to that as
+    // well, and rescaling them at every new maximum took a seventh of the time
+    auto raise = [&](const Scores& s) INLINE {
+        float top = fmaxf(s.v[0][0], s.v[0][1]);
 #pragma unroll
-            for (int p = 0; p < 2; ++p)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (block * BLK + 32 * p + 8 * (i / 4) + 4 * half + i % 4 > last) s[p][i] = -INFINITY;
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, s[i / 16][i % 16]);
-        top = fmaxf(both_max(top), m);
-        if (__any(top > m)) {
-            const float f = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * A.factor);
-            l *= f;
+        for (int i = 2; i < 32; i += 2) top = fmaxf(fmaxf(s.v[i / 16][i % 16], s.v[i / 16][i % 16 + 1]), top);
+        top = both_max(top);
+        if (__any((top - m) * A.factor > 8.f)) {
+            const float up = fmaxf(top, m);
+            const float f = m == up ? 1.f : __builtin_amdgcn_exp2f((m - up) * A.factor);
+            l[0] *= f;
+            l[1] *= f;
 #pragma unroll
             for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o[d][i] *= f;
-            m = top;
+            m = up;
         }
-        const float shift = (MASKED && m == -INFINITY) ? 0.f : m * A.factor;   // (a row that has seen nothing yet)
-        pr_bf16x8 pf[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            pr_uintx4 v;
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const float a = __builtin_amdgcn_exp2f(fmaf(s[k / 2][8 * (k % 2) + e], A.factor, -shift));
-                const float b = __builtin_amdgcn_exp2f(fmaf(s[k / 2][8 * (k % 2) + e + 1], A.factor, -shift));
-                l += a + b;
-                v[e / 2] = pr_pack2(a, b);
-            }
-            pf[k] = __builtin_bit_cast(pr_bf16x8, v);
-        }
-        bool odd = false;
-        if (MASKED) {   // does the block hold a value that a weight of zero does not take away?
-            unsigned any = 0;
-            const char* part = lds + (2 + (block & 1)) * PART + lane * 16;
-#pragma unroll 2
-            for (int i = 0; i < KIB; ++i) {
-                const pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(part + i * 1024);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7f807f80u) + 0x00800080u;
-            }
-            odd = __any((any & 0x80008000u) != 0);
-        }
-        auto values = [&](int d, int k) {   // the operand of dims 32 d .. and positions 16 k ..
-            const int piece = ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_turn) * 16;
-            union {
-                pr_shortx4 h[2];
-                pr_uintx4 u;
-            } vf;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) pr_shortx4*)(vl + (16 * k + 8 * j) * ROW + piece));
-            return vf.u;
-        };
-        if (MASKED && odd) {
-            // Infinities and NaN apart: what meets a weight that is not zero ends in the sum, by products with ones in their places
-            auto pick = [](pr_uintx4 v, unsigned sign) {    // ones where v is NaN or the infinity of that sign
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const unsigned bad = ((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u, nan = ((v[e] & 0x007f007fu) + 0x7fff7fffu) & 0x80008000u;
-                    const unsigned at = bad & (nan | ~(v[e] ^ sign));
-                    v[e] = (at >> 15) * 0x3f80u;
-                }
-                return v;
-            };
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d) {
-#pragma unroll 1
-                for (unsigned sign = 0; sign < 2; ++sign) {
-                    pr_floatx16 t;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) t[i] = 0.f;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        asm volatile("" ::: "memory");   // (one operand after the other: this is the rare way, and registers are few)
-                        t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pr_bf16x8, pick(values(d, k), sign * 0x80008000u)), pf[k], t, 0, 0, 0);
-                    }
-                    const float f = sign ? -INFINITY : INFINITY;
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] += t[i] > 0.f ? f : 0.f;
-                }
-            }
-            // (every wavefront has seen the same block, so all come here)
-            q8_wait_lds();
-            q8_barrier();
-            char* own = lds + (2 + (block & 1)) * PART + threadIdx.x * 16;
-#pragma unroll 1
-            for (int i = 0; i < PART; i += WAVES * 1024) {
-                pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(own + i);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] &= ~(((((v[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu);
-                *reinterpret_cast<pr_uintx4*>(own + i) = v;
-            }
-            q8_wait_lds();
-            q8_barrier();
-        }
-#pragma unroll
-        for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(pr_bf16x8, values(d, k)), pf[k], o[d], 0, 0, 0);
     };
-    if (n_blocks) fetch(0);
-    int block = 0;
-    auto turn = [&](auto masked) {
+    auto shift_of = [&]() { return m == -INFINITY ? 0.f : m * A.factor; };   // (a row that has seen nothing yet)
+    auto weights = [&](const Scores& s, int k, float shift) INLINE {   // of positions 16 k .. 16 k + 15, rounded; their sum is that of the rounded ones
+        pr_uintx4 v;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(s.v[k / 2][8 * (k % 2) + e], A.factor, -shift));
+            const float y = __builtin_amdgcn_exp2f(fmaf(s.v[k / 2][8 * (k % 2) + e + 1], A.factor, -shift));
+            unsigned both = pr_pack2(x, y);
+            asm("" : "+v"(both));   // (a register of its own: as an element of v this compiler takes the first element's every time)
+            l[k & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pr_bf16x2, both), (pr_bf16x2){(__bf16)1.f, (__bf16)1.f}, l[k & 1], false);
+            v[e / 2] = both;
+        }
+        return __builtin_bit_cast(pr_bf16x8, v);
+    };
+    auto sum_values = [&](int par, int k, pr_bf16x8 pf) INLINE {
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(par, d, k), pf, o[d], 0, 0, 0);
+    };
+    // Keys are fetched two blocks ahead and values one, in front of a block whose scores are there
+    auto meet = [&](int block) INLINE {
         q8_wait_fetches<0>();
         q8_wait_lds();
         q8_barrier();
-        if (block + 1 < n_blocks) fetch(block + 1);
-        step(block, masked);
+        if (block + 2 < n_blocks) fetch_keys(block + 2);
+        if (block + 1 < n_blocks) fetch_values(block + 1);
     };
-    for (; block < n_clear; ++block) turn(std::false_type());
-    for (; block < n_blocks; ++block) turn(std::true_type());
-    if (!live) return;
-    l = both_sum(l);
-    const float inv = last < 0 ? 0.f : 1.f / l;
-    uint16_t* dst = A.out + (size_t)(qs.begin + at) * A.ld_out + (size_t)(head * A.group + sub) * HD + 4 * half;
+    // A block that all rows see whole, not the last one: the next block's scores, t, run beside this one's weights
+    auto clear = [&](int block, auto par, const Scores& s, Scores& t) INLINE {
+        constexpr int PAR = decltype(par)::value;
+        meet(block);
+        raise(s);
+        const float shift = shift_of();
+        const pr_bf16x8 p0 = weights(s, 0, shift);
+        scores(t, 1 - PAR, 0);
+        const pr_bf16x8 p1 = weights(s, 1, shift);
+        scores(t, 1 - PAR, 1);
+        const pr_bf16x8 p2 = weights(s, 2, shift);
+        sum_values(PAR, 0, p0);
+        const pr_bf16x8 p3 = weights(s, 3, shift);
+        sum_values(PAR, 1, p1);
+        sum_values(PAR, 2, p2);
+        sum_values(PAR, 3, p3);
+    };
+    auto masked = [&](int block, Scores& s) INLINE {
+        meet(block);
+        const int seen = last - block * BLK - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (8 * (i / 4) + i % 4 > seen) s.v[i / 16][i % 16] = -INFINITY;
+        raise(s);
+        // does the block hold a value that a weight of zero does not take away?
+        unsigned any = 0;
+        char* const part = lds + (2 + (block & 1)) * PART;
+#pragma unroll 2
+        for (int i = 0; i < KIB; ++i) {
+            const pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(part + lane * 16 + i * 1024);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7f807f80u) + 0x00800080u;
+        }
+        if (__any((any & 0x80008000u) != 0)) {
+            // Then they leave the block, and every row that sees the first one of a column has it in its sum.  (Every wavefront has looked at the same
+            // block, so all come here.)
+            q8_wait_lds();
+            q8_barrier();
+#pragma unroll 1
+            for (int d = threadIdx.x; d < HD; d += 64 * WAVES) {
+                int up = INT_MAX, down = INT_MAX;   // positions of the first +infinity (NaN), -infinity (NaN)
+#pragma unroll 1
+                for (int r = BLK - 1; r >= 0; --r) {
+                    uint16_t* const at = reinterpret_cast<uint16_t*>(part + r * ROW + ((d >> 3) ^ value_turn(r)) * 16) + (d & 7);
+                    const unsigned x = *at;
+                    if ((x & 0x7f80u) != 0x7f80u) continue;
+                    *at = 0;
+                    if ((x & 0x7fu) || !(x & 0x8000u)) up = block * BLK + r;
+                    if ((x & 0x7fu) || (x & 0x8000u)) down = block * BLK + r;
+                }
+                first[0][d] = up;
+                first[1][d] = down;
+            }
+            q8_wait_lds();
+            q8_barrier();
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int dim = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+                    o[d][i] += (first[0][dim] <= last ? INFINITY : 0.f) - (first[1][dim] <= last ? INFINITY : 0.f);
+                }
+        }
+        const float shift = shift_of();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum_values(block & 1, k, weights(s, k, shift));
+        if (block + 1 < n_blocks) {
+            scores(s, 1 - (block & 1), 0);
+            scores(s, 1 - (block & 1), 1);
+        }
+    };
+    if (n_blocks) {
+        q8_wait_fetches<0>();
+        q8_barrier();
+        scores(s0, 0, 0);
+        scores(s0, 0, 1);
+    }
+    const int n_beside = min(n_clear, n_blocks - 1);
+    int block = 0;
+    for (; block + 1 < n_beside; block += 2) {
+        clear(block, std::integral_constant<int, 0>(), s0, s1);
+        clear(block + 1, std::integral_constant<int, 1>(), s1, s0);
+    }
+    if (block < n_beside) {
+        clear(block++, std::integral_constant<int, 0>(), s0, s1);
+        s0 = s1;
+    }
+    for (; block < n_blocks; ++block) masked(block, s0);
+    const float sum = both_sum(l[0] + l[1]);
+    int row = threadIdx.x;
+    asm volatile("" : "+v"(row));   // (found anew: kept from above it would take registers all the way)
+    const int own_half = (row >> 5) & 1;
+    row = (row >> 6) * 32 + (row & 31);
+    if (tile0 + row >= n_rows) return;
+    if (A.parts.d > 1) {
+        const size_t at = (size_t)blockIdx.x * TILE + row;      // (blockIdx.x counts parts, heads, units, in this order)
+        float* po = A.part_o + at * HD + 4 * own_half;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<pr_floatx4*>(po + 32 * d + 2 * i) = (pr_floatx4){o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+        if (own_half == 0) *reinterpret_cast<float2*>(A.part_ml + 2 * at) = make_float2(m, sum);
+        return;
+    }
+    const float inv = last < 0 ? 0.f : 1.f / sum;
+    const int2 to = place(row);
+    uint16_t* dst = A.out + (size_t)(q_begin + to.x) * A.ld_out + (size_t)(head * group + to.y) * HD + 4 * own_half;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
@@ -250,11 +339,71 @@ __global__ void __launch_bounds__(64 * WAVES, 2) attention_kernel(Args A)
         }
 }
 
-template <int HD, int WAVES>
-void launch(const Args& a, hipStream_t s)
+// The parts of a tile's rows, in their order: eight dims of a row a thread
+template <int HD, int TILE>
+__global__ void __launch_bounds__(256) join_kernel(Args A)
 {
-    const int64_t tiles = (int64_t)a.q_rows * a.group / (32 * WAVES) + a.batch;
-    hipLaunchKernelGGL((attention_kernel<HD, WAVES>), dim3((unsigned)(tiles * a.n_kv_heads)), dim3(64 * WAVES), 0, s, a);
+    constexpr int LANES = HD / 8, ROWS = 256 / LANES;   // rows of a workgroup
+    constexpr int GROUPS = (TILE + ROWS - 1) / ROWS;
+    const int job = blockIdx.x / GROUPS, r = (blockIdx.x % GROUPS) * ROWS + threadIdx.x / LANES, dim = threadIdx.x % LANES * 8;
+    const int number = A.heads.div(job), head = job - number * (int)A.heads.d, group = A.group.d;
+    const Tile T = find_tile<TILE>(A, number);
+    if (T.seq < 0 || r >= TILE || T.row0 + r >= T.n_rows) return;
+    const int parts = A.parts.d;
+    const float* ml = A.part_ml + ((size_t)job * parts * TILE + r) * 2;
+    const float* po = A.part_o + ((size_t)job * parts * TILE + r) * HD + dim;
+    float m = -INFINITY, l = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[(size_t)p * TILE * 2]);
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) {
+        const float2 q = *reinterpret_cast<const float2*>(ml + (size_t)p * TILE * 2);
+        const float f = q.x == m ? 1.f : __builtin_amdgcn_exp2f((q.x - m) * A.factor);
+        l = fmaf(q.y, f, l);
+        const pr_floatx4 a = *reinterpret_cast<const pr_floatx4*>(po + (size_t)p * TILE * HD), b = *reinterpret_cast<const pr_floatx4*>(po + (size_t)p * TILE * HD + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = fmaf(a[i], f, v[i]);
+            v[4 + i] = fmaf(b[i], f, v[4 + i]);
+        }
+    }
+    const int row = T.row0 + r, at = A.group.div(row), sub = row - at * group;
+    const float inv = T.n_k - T.n_q + at < 0 ? 0.f : 1.f / l;
+    pr_uintx4 w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pr_pack2(v[2 * i] * inv, v[2 * i + 1] * inv);
+    *reinterpret_cast<pr_uintx4*>(A.out + (size_t)(T.q_begin + at) * A.ld_out + (size_t)(head * group + sub) * HD + dim) = w;
+}
+
+// How many wavefronts a workgroup has, and among how many workgroups a tile's keys are shared out: as many rows as the sequences have, and
+// workgroups for all places that the compute units have for them, as long as a part has four blocks.
+constexpr int MOST_PARTS = 32;
+struct Plan {
+    int waves, parts;
+    int64_t tiles;          // units of a launch, at most
+    size_t part_bytes;      // of the workspace, for one part of every tile
+};
+Plan plan(int q_rows, int batch, int n_kv_heads, int group, int head_dim, int64_t q_len, int64_t k_len, int waves = 0)
+{
+    Plan p;
+    p.waves = waves ? waves : q_len * group <= 32 ? 1 : q_len * group <= 64 ? 2 : 4;
+    const int rows = 32 * p.waves;
+    p.tiles = (int64_t)q_rows * group / rows + batch;
+    // sequences of about one length each
+    const int64_t wgs = std::min(p.tiles, std::max((int64_t)1, ((int64_t)q_rows * group + rows - 1) / rows)) * n_kv_heads;
+    const int64_t places = 256 * (head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
+    p.parts = (int)std::max((int64_t)1, std::min({places / wgs, (k_len / BLK + 3) / 4, (int64_t)MOST_PARTS}));
+    p.part_bytes = (size_t)p.tiles * n_kv_heads * rows * (head_dim + 2) * 4;
+    return p;
+}
+
+template <int HD, int WAVES>
+void launch(const Args& a, const Plan& p, hipStream_t s)
+{
+    hipLaunchKernelGGL((attention_kernel<HD, WAVES>), dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(64 * WAVES), 0, s, a);
+    if (p.parts > 1) {
+        constexpr int ROWS = 2048 / HD, GROUPS = (32 * WAVES + ROWS - 1) / ROWS;
+        hipLaunchKernelGGL((join_kernel<HD, 32 * WAVES>), dim3((unsigned)(p.tiles * a.heads.d * GROUPS)), dim3(256), 0, s, a);
+    }
 }
 
 }  // namespace
@@ -264,7 +413,13 @@ using namespace specv;
 
 extern "C" size_t spec_prompt_attention_workspace_bytes(int32_t q_rows, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
 {
-    return 0;
+    if (q_rows <= 0 || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128)) return 0;
+    size_t most = 0;
+    for (int waves = 1; waves <= 4; waves *= 2) {
+        const Plan p = plan(q_rows, batch, n_kv_heads, n_q_heads / n_kv_heads, head_dim, 0, INT_MAX, waves);
+        if (p.parts > 1) most = std::max(most, p.parts * p.part_bytes);
+    }
+    return most;
 }
 
 extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* workspace, size_t workspace_bytes, void* stream)
@@ -292,13 +447,28 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     if (!a.batch || !a.q_rows) return SPEC_OK;
     if (!a.q || !a.out || !a.q_row0 || (a.k_rows && (!a.k || !a.v))) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_attention: null pointer");
     const int group = a.n_q_heads / a.n_kv_heads;
-    if ((int64_t)a.q_rows * group > 0x3fffffff || ((int64_t)a.q_rows * group / 32 + a.batch) * a.n_kv_heads > 0x7fffffff)
+    if ((int64_t)a.q_rows * group > 0x3fffffff || ((int64_t)a.q_rows * group / 32 + a.batch) * a.n_kv_heads * 16 > 0x7fffffff)
         return fail(SPEC_ERR_SHAPE, "spec_prompt_attention: %d query rows are too many", a.q_rows);
+    // lengths that are not known: all rows are of one sequence, or of as many as there are, whichever gives more workgroups
+    const int64_t q_len = a.max_q_len ? a.max_q_len : a.q_rows, k_len = a.max_k_len ? a.max_k_len : a.k_rows;
+    Plan p = plan(a.q_rows, a.batch, a.n_kv_heads, group, a.head_dim, q_len, k_len);
+    if (p.parts > 1) p.parts = workspace ? (int)std::min((size_t)p.parts, workspace_bytes / p.part_bytes) : 1;
+    if (p.parts < 1) p.parts = 1;
+    float* const ws = (float*)workspace;
+    const size_t rows = p.part_bytes / (a.head_dim + 2) / 4 * p.parts;
     const Args g{(const uint16_t*)a.q, (const uint16_t*)a.k, (const uint16_t*)a.v, (uint16_t*)a.out, a.ld_q, a.ld_k, a.ld_v, a.ld_out, a.q_row0,
-                 a.k_row0, a.n_kv_heads, group, a.batch, a.q_rows, a.k_rows, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 0x1p-149f), a.scale < 0.f ? 0x80008000u : 0u};
+                 a.k_row0, FastDiv(a.n_kv_heads), FastDiv(group), a.batch, a.q_rows, a.k_rows, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 0x1p-149f),
+                 a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr};
     hipStream_t s = (hipStream_t)stream;
-    if (a.head_dim == 128) launch<128, 4>(g, s);
-    else launch<64, 4>(g, s);
+    if (a.head_dim == 128) {
+        if (p.waves == 1) launch<128, 1>(g, p, s);
+        else if (p.waves == 2) launch<128, 2>(g, p, s);
+        else launch<128, 4>(g, p, s);
+    } else {
+        if (p.waves == 1) launch<64, 1>(g, p, s);
+        else if (p.waves == 2) launch<64, 2>(g, p, s);
+        else launch<64, 4>(g, p, s);
+    }
     SPECV_LAUNCH_CHECK("attention_kernel");
     return SPEC_OK;
 }
