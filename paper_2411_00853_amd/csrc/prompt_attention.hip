@@ -22,8 +22,9 @@ struct Args {
     int batch, q_rows, k_rows;
     float factor;       // |scale| * log2(e), not zero: what is masked is -inf times it
     unsigned sign;      // 0x80008000 where the scale is negative: the queries are negated
-    FastDiv parts;      // a tile's keys are shared out among so many workgroups; with more than one, what they leave to the join:
-    float *part_o, *part_ml;   // [unit][kv head][part][row of the tile][head_dim] sums of weighted values, [..][2] maximum and sum of weights
+    FastDiv parts;      // a tile's keys are shared out among at most so many workgroups,
+    int chunk;          // each of which takes so many blocks (more where parts would not do); with more than one part, what they leave to the join:
+    float *part_o, *part_ml;   // [unit][part][kv head][row of the tile][head_dim] sums of weighted values, [..][2] maximum and sum of weights
 };
 
 // The tile of a unit (its number and kv head): of one sequence, some rows
@@ -66,6 +67,135 @@ __device__ __forceinline__ float both_sum(float v)
 typedef short pr_shortx4 __attribute__((ext_vector_type(4)));
 typedef __bf16 pr_bf16x2 __attribute__((ext_vector_type(2)));
 
+// Blocks of a part, if the tile has that many in all
+__device__ __forceinline__ int chunk_of(const Args& A, int all_blocks)
+{
+    return max(A.chunk, A.parts.div(all_blocks + (int)A.parts.d - 1));
+}
+// Blocks that some row of a tile sees
+template <int TILE>
+__device__ __forceinline__ int blocks_of(const Args& A, const Tile& T)
+{
+    const int last = T.n_k - T.n_q + A.group.div(min(T.row0 + TILE, T.n_rows) - 1);
+    return last < 0 ? 0 : last / BLK + 1;
+}
+
+// A row of LDS holds the pieces (16 bytes) of a row of keys in the order piece ^ key_turn(row), of values piece ^ value_turn(row): the lanes that a
+// read serves at once (sixteen of keys, 32 of values) then find different groups of banks
+template <int HD>
+__device__ __forceinline__ int key_turn(int r)
+{
+    return HD == 128 ? r & 15 : (r >> 1) & 7;
+}
+template <int HD>
+__device__ __forceinline__ int value_turn(int r)
+{
+    return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1);
+}
+
+// Position in the sequence and query head (of the kv head's) of a tile's row; rows beyond the last are the last again
+__device__ __forceinline__ int2 place(const Args& A, const Tile& T, int row)
+{
+    row = min(T.row0 + row, T.n_rows - 1);
+    const int at = A.group.div(row);
+    return make_int2(at, row - at * (int)A.group.d);
+}
+
+// What a lane holds of the row `row` of its tile: to the output, or to the join
+template <int HD, int TILE>
+__device__ __forceinline__ void leave(const Args& A, const Tile& T, int head, int row, int half, const pr_floatx16 (&o)[HD / 32], float m, float sum, bool seen)
+{
+    if (T.row0 + row >= T.n_rows) return;
+    if (A.parts.d > 1) {
+        const size_t at = (size_t)blockIdx.x * TILE + row;      // (blockIdx.x counts kv heads, parts, units, in this order)
+        float* po = A.part_o + at * HD + 4 * half;
+#pragma unroll
+        for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) *reinterpret_cast<pr_floatx4*>(po + 32 * d + 2 * i) = (pr_floatx4){o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+        if (half == 0) *reinterpret_cast<float2*>(A.part_ml + 2 * at) = make_float2(m, sum);
+        return;
+    }
+    const float inv = seen ? 1.f / sum : 0.f;
+    const int2 to = place(A, T, row);
+    uint16_t* dst = A.out + (size_t)(T.q_begin + to.x) * A.ld_out + (size_t)(head * (int)A.group.d + to.y) * HD + 4 * half;
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<pr_uintx2*>(dst + 32 * d + 2 * i) = (pr_uintx2){pr_pack2(o[d][i] * inv, o[d][i + 1] * inv), pr_pack2(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+}
+
+// The lane's query row as operands of the score product
+template <int HD>
+__device__ __forceinline__ void load_query(const Args& A, const Tile& T, int head, int2 to, int half, pr_bf16x8 (&qf)[HD / 16])
+{
+    const uint16_t* src = A.q + (size_t)(T.q_begin + to.x) * A.ld_q + (size_t)(head * (int)A.group.d + to.y) * HD + 8 * half;
+#pragma unroll
+    for (int c = 0; c < HD / 16; ++c) qf[c] = __builtin_bit_cast(pr_bf16x8, *reinterpret_cast<const pr_uintx4*>(src + 16 * c) ^ A.sign);
+}
+
+// Sixteen weights' worth of a lane: eight numbers exp2(s * factor - shift), rounded to bf16, and their sum (that of the rounded ones) added to l
+__device__ __forceinline__ pr_bf16x8 eight_weights(const pr_floatx16& s, int at, float factor, float shift, float& l)
+{
+    pr_uintx4 v;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float x = __builtin_amdgcn_exp2f(fmaf(s[at + e], factor, -shift)), y = __builtin_amdgcn_exp2f(fmaf(s[at + e + 1], factor, -shift));
+        unsigned both = pr_pack2(x, y);
+        asm("" : "+v"(both));   // (a register of its own: as an element of v this compiler takes the first element's every time)
+        l = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pr_bf16x2, both), (pr_bf16x2){(__bf16)1.f, (__bf16)1.f}, l, false);
+        v[e / 2] = both;
+    }
+    return __builtin_bit_cast(pr_bf16x8, v);
+}
+
+// Are there infinities or NaN among the KIB KiB of values at `part`?  (by one wavefront)
+template <int KIB>
+__device__ __forceinline__ bool has_odd(const char* part)
+{
+    unsigned any = 0;
+#pragma unroll 2
+    for (int i = 0; i < KIB; ++i) {
+        const pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(part + (threadIdx.x & 63) * 16 + i * 1024);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7f807f80u) + 0x00800080u;
+    }
+    return __any((any & 0x80008000u) != 0);
+}
+// They leave the block's values (rows positions p0 ..); first: the positions of each column's first +infinity (NaN) and -infinity (NaN)
+template <int HD, int ROWS>
+__device__ __forceinline__ void clear_odd(char* part, int p0, int (*first)[HD], int tid, int threads)
+{
+#pragma unroll 1
+    for (int d = tid; d < HD; d += threads) {
+        int up = INT_MAX, down = INT_MAX;
+#pragma unroll 1
+        for (int r = ROWS - 1; r >= 0; --r) {
+            uint16_t* const at = reinterpret_cast<uint16_t*>(part + r * (2 * HD) + ((d >> 3) ^ value_turn<HD>(r)) * 16) + (d & 7);
+            const unsigned x = *at;
+            if ((x & 0x7f80u) != 0x7f80u) continue;
+            *at = 0;
+            if ((x & 0x7fu) || !(x & 0x8000u)) up = p0 + r;
+            if ((x & 0x7fu) || (x & 0x8000u)) down = p0 + r;
+        }
+        first[0][d] = up;
+        first[1][d] = down;
+    }
+}
+// Every row that sees the first one of a column has it in its sum
+template <int HD>
+__device__ __forceinline__ void add_odd(const int (*first)[HD], int half, int last, pr_floatx16 (&o)[HD / 32])
+{
+#pragma unroll
+    for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int dim = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
+            o[d][i] += (first[0][dim] <= last ? INFINITY : 0.f) - (first[1][dim] <= last ? INFINITY : 0.f);
+        }
+}
+
 template <int HD, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) attention_kernel(Args A)
 {
@@ -76,22 +206,18 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
     __shared__ __attribute__((aligned(16))) char lds[4 * PART];            // keys, keys, values, values
     __shared__ int first[2][HD];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r32 = lane & 31, half = lane >> 5;
-    const int job = A.parts.div(blockIdx.x), part = (int)blockIdx.x - job * (int)A.parts.d;
-    const int number = A.heads.div(job), head = job - number * (int)A.heads.d, group = A.group.d;
+    // Workgroups in a row take the kv heads: what they read lies together
+    const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
     const Tile T = find_tile<TILE>(A, number);
     if (T.seq < 0) return;
-    const int tile0 = T.row0, n_rows = T.n_rows, q_begin = T.q_begin;
-    const int last_first = T.n_k - T.n_q + A.group.div(tile0), last_last = T.n_k - T.n_q + A.group.div(min(tile0 + TILE, n_rows) - 1);
-    const int all_blocks = last_last < 0 ? 0 : last_last / BLK + 1;
+    const int last_first = T.n_k - T.n_q + A.group.div(T.row0), all_blocks = blocks_of<TILE>(A, T);
     // This part's blocks; all positions below are counted from their first one
-    const int block0 = A.parts.div(all_blocks * part), n_blocks = A.parts.div(all_blocks * (part + 1)) - block0, p_first = block0 * BLK;
+    const int chunk = chunk_of(A, all_blocks), block0 = part * chunk, p_first = block0 * BLK;
+    if (part && block0 >= all_blocks) return;
+    const int n_blocks = min(all_blocks - block0, chunk);
     const int n_k = T.n_k - p_first, k_begin = T.k_begin + p_first;
     const int n_clear = last_first < p_first ? 0 : (last_first - p_first + 1) / BLK;       // blocks that all rows see whole
 
-    // A row of LDS holds the pieces of a row of keys in the order piece ^ key_turn(row), of values piece ^ value_turn(row): the lanes that a read
-    // serves at once (sixteen of keys, 32 of values) then find different groups of banks
-    auto key_turn = [](int r) { return HD == 128 ? r & 15 : (r >> 1) & 7; };
-    auto value_turn = [](int r) { return HD == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
     const char* const kb = (const char*)(A.k + (size_t)k_begin * A.ld_k + (size_t)head * HD);
     const char* const vb = (const char*)(A.v + (size_t)k_begin * A.ld_v + (size_t)head * HD);
@@ -99,8 +225,8 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int r = (wave * U + u) * ROWS + lane / PIECES;
-        k_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_k) + (lane % PIECES ^ key_turn(r)) * 16;
-        v_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn(r)) * 16;
+        k_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_k) + (lane % PIECES ^ key_turn<HD>(r)) * 16;
+        v_off[u] = (uint32_t)r * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn<HD>(r)) * 16;
     }
     auto fetch_part = [&](const char* base, int64_t ld, const uint32_t (&off)[U], int block, uint32_t to, auto turn) INLINE {
         const int p0 = block * BLK;
@@ -116,8 +242,8 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
             }
         }
     };
-    auto fetch_keys = [&](int block) INLINE { fetch_part(kb, A.ld_k, k_off, block, lds0 + (block & 1) * PART, key_turn); };
-    auto fetch_values = [&](int block) INLINE { fetch_part(vb, A.ld_v, v_off, block, lds0 + (2 + (block & 1)) * PART, value_turn); };
+    auto fetch_keys = [&](int block) INLINE { fetch_part(kb, A.ld_k, k_off, block, lds0 + (block & 1) * PART, key_turn<HD>); };
+    auto fetch_values = [&](int block) INLINE { fetch_part(vb, A.ld_v, v_off, block, lds0 + (2 + (block & 1)) * PART, value_turn<HD>); };
 
     if (n_blocks) {
         fetch_keys(0);
@@ -125,24 +251,10 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
         if (n_blocks > 1) fetch_keys(1);
     }
     // (the fetches are under way) the lane's query row, and the last position that it sees
-    auto place = [&](int row) {   // position in the sequence and query head of a tile's row
-        row = min(tile0 + row, n_rows - 1);
-        const int at = A.group.div(row);
-        return make_int2(at, row - at * group);
-    };
-    int last;
+    const int2 to = place(A, T, wave * 32 + r32);
+    const int last = n_k - T.n_q + to.x;
     pr_bf16x8 qf[HD / 16];
-    {
-        const int2 to = place(wave * 32 + r32);
-        last = n_k - T.n_q + to.x;
-        const uint16_t* src = A.q + (size_t)(q_begin + to.x) * A.ld_q + (size_t)(head * group + to.y) * HD + 8 * half;
-#pragma unroll
-        for (int c = 0; c < HD / 16; ++c) {
-            pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(src + 16 * c);
-            v ^= A.sign;
-            qf[c] = __builtin_bit_cast(pr_bf16x8, v);
-        }
-    }
+    load_query<HD>(A, T, head, to, half, qf);
 
     struct Scores {
         pr_floatx16 v[2];
@@ -156,9 +268,9 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
     // where this lane reads keys (rows r32, r32 + 32) and values (rows 4 half + (lane & 15) / 4 + 8 j)
-    const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn(v_row);
+    const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn<HD>(v_row);
     auto key = [&](int par, int p, int c) INLINE {   // par: of the block's number, odd or even
-        return *reinterpret_cast<const pr_bf16x8*>(lds + par * PART + (r32 + 32 * p) * ROW + ((2 * c + half) ^ key_turn(r32)) * 16);
+        return *reinterpret_cast<const pr_bf16x8*>(lds + par * PART + (r32 + 32 * p) * ROW + ((2 * c + half) ^ key_turn<HD>(r32)) * 16);
     };
     auto value = [&](int par, int d, int k) INLINE {   // the operand of dims 32 d .. and positions 16 k ..
         const char* vl = lds + (2 + par) * PART + v_row * ROW + (lane & 1) * 8;
@@ -198,19 +310,7 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
         }
     };
     auto shift_of = [&]() { return m == -INFINITY ? 0.f : m * A.factor; };   // (a row that has seen nothing yet)
-    auto weights = [&](const Scores& s, int k, float shift) INLINE {   // of positions 16 k .. 16 k + 15, rounded; their sum is that of the rounded ones
-        pr_uintx4 v;
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(s.v[k / 2][8 * (k % 2) + e], A.factor, -shift));
-            const float y = __builtin_amdgcn_exp2f(fmaf(s.v[k / 2][8 * (k % 2) + e + 1], A.factor, -shift));
-            unsigned both = pr_pack2(x, y);
-            asm("" : "+v"(both));   // (a register of its own: as an element of v this compiler takes the first element's every time)
-            l[k & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pr_bf16x2, both), (pr_bf16x2){(__bf16)1.f, (__bf16)1.f}, l[k & 1], false);
-            v[e / 2] = both;
-        }
-        return __builtin_bit_cast(pr_bf16x8, v);
-    };
+    auto weights = [&](const Scores& s, int k, float shift) INLINE { return eight_weights(s.v[k / 2], 8 * (k % 2), A.factor, shift, l[k & 1]); };   // of positions 16 k .. 16 k + 15
     auto sum_values = [&](int par, int k, pr_bf16x8 pf) INLINE {
 #pragma unroll
         for (int d = 0; d < HD / 32; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value(par, d, k), pf, o[d], 0, 0, 0);
@@ -247,44 +347,15 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
         for (int i = 0; i < 32; ++i)
             if (8 * (i / 4) + i % 4 > seen) s.v[i / 16][i % 16] = -INFINITY;
         raise(s);
-        // does the block hold a value that a weight of zero does not take away?
-        unsigned any = 0;
+        // A weight of zero does not take an infinity or a NaN away
         char* const part = lds + (2 + (block & 1)) * PART;
-#pragma unroll 2
-        for (int i = 0; i < KIB; ++i) {
-            const pr_uintx4 v = *reinterpret_cast<const pr_uintx4*>(part + lane * 16 + i * 1024);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) any |= (v[e] & 0x7f807f80u) + 0x00800080u;
-        }
-        if (__any((any & 0x80008000u) != 0)) {
-            // Then they leave the block, and every row that sees the first one of a column has it in its sum.  (Every wavefront has looked at the same
-            // block, so all come here.)
+        if (has_odd<KIB>(part)) {   // (every wavefront has looked at the same block, so all come here)
             q8_wait_lds();
             q8_barrier();
-#pragma unroll 1
-            for (int d = threadIdx.x; d < HD; d += 64 * WAVES) {
-                int up = INT_MAX, down = INT_MAX;   // positions of the first +infinity (NaN), -infinity (NaN)
-#pragma unroll 1
-                for (int r = BLK - 1; r >= 0; --r) {
-                    uint16_t* const at = reinterpret_cast<uint16_t*>(part + r * ROW + ((d >> 3) ^ value_turn(r)) * 16) + (d & 7);
-                    const unsigned x = *at;
-                    if ((x & 0x7f80u) != 0x7f80u) continue;
-                    *at = 0;
-                    if ((x & 0x7fu) || !(x & 0x8000u)) up = block * BLK + r;
-                    if ((x & 0x7fu) || (x & 0x8000u)) down = block * BLK + r;
-                }
-                first[0][d] = up;
-                first[1][d] = down;
-            }
+            clear_odd<HD, BLK>(part, block * BLK, first, threadIdx.x, 64 * WAVES);
             q8_wait_lds();
             q8_barrier();
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int dim = 32 * d + 8 * (i / 4) + 4 * half + i % 4;
-                    o[d][i] += (first[0][dim] <= last ? INFINITY : 0.f) - (first[1][dim] <= last ? INFINITY : 0.f);
-                }
+            add_odd<HD>(first, half, last, o);
         }
         const float shift = shift_of();
 #pragma unroll
@@ -316,56 +387,179 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
     asm volatile("" : "+v"(row));   // (found anew: kept from above it would take registers all the way)
     const int own_half = (row >> 5) & 1;
     row = (row >> 6) * 32 + (row & 31);
-    if (tile0 + row >= n_rows) return;
-    if (A.parts.d > 1) {
-        const size_t at = (size_t)blockIdx.x * TILE + row;      // (blockIdx.x counts parts, heads, units, in this order)
-        float* po = A.part_o + at * HD + 4 * own_half;
+    leave<HD, TILE>(A, T, head, row, own_half, o, m, sum, last >= 0);
+}
+
+// ---- few rows: the stream of keys and values -----------------------------------------------------------------------------
+//
+// One wavefront takes 32 query rows (those of a kv head's query heads at one position, say).  What bounds it is how much a compute unit has asked
+// for at a time, so blocks are small, 32 positions, and go round in RING places of LDS of which all but one are under way.
+constexpr int FEW = 32, RING = 5;
+template <int HD>
+__global__ void __launch_bounds__(64, 1) few_kernel(Args A)
+{
+    constexpr int ROW = 2 * HD, PART = FEW * ROW, U = PART / 1024, PIECES = ROW / 16, ROWS = 1024 / ROW, TILE = 32;
+    __shared__ __attribute__((aligned(16))) char lds[RING * 2 * PART];     // [place][keys, values]
+    const int lane = threadIdx.x, r32 = lane & 31, half = lane >> 5;
+    const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
+    const Tile T = find_tile<TILE>(A, number);
+    if (T.seq < 0) return;
+    const int all_blocks = blocks_of<TILE>(A, T), chunk = chunk_of(A, all_blocks), p_first = part * chunk * BLK;
+    if (part && part * chunk >= all_blocks) return;
+    // All positions are counted from the part's first one
+    const int n_k = T.n_k - p_first, to_see = n_k - T.n_q;
+    const int end = min(to_see + A.group.div(min(T.row0 + TILE, T.n_rows) - 1) + 1, min(all_blocks, chunk) * BLK);   // positions that some row sees
+    const int n_blocks = end <= 0 ? 0 : (end + FEW - 1) / FEW, n_clear = to_see + A.group.div(T.row0) + 1;         // positions that all see
+
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
+    const char* const kb = (const char*)(A.k + (size_t)(T.k_begin + p_first) * A.ld_k + (size_t)head * HD);
+    const char* const vb = (const char*)(A.v + (size_t)(T.k_begin + p_first) * A.ld_v + (size_t)head * HD);
+    auto fetch = [&](int block, int slot) INLINE {
+        const int p0 = block * FEW;
+        const char *kp = kb + (size_t)p0 * A.ld_k * 2, *vp = vb + (size_t)p0 * A.ld_v * 2;
 #pragma unroll
-        for (int d = 0; d < HD / 32; ++d)
+        for (int u = 0; u < U; ++u) {
+            const int r = u * ROWS + lane / PIECES, from = min(r, n_k - 1 - p0);    // (beyond the end: the last row again)
+            q8_fetch_lds(kp, (uint32_t)from * (uint32_t)(2 * A.ld_k) + (lane % PIECES ^ key_turn<HD>(r)) * 16, lds0 + slot * (2 * PART) + u * 1024);
+        }
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) *reinterpret_cast<pr_floatx4*>(po + 32 * d + 2 * i) = (pr_floatx4){o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-        if (own_half == 0) *reinterpret_cast<float2*>(A.part_ml + 2 * at) = make_float2(m, sum);
-        return;
-    }
-    const float inv = last < 0 ? 0.f : 1.f / sum;
-    const int2 to = place(row);
-    uint16_t* dst = A.out + (size_t)(q_begin + to.x) * A.ld_out + (size_t)(head * group + to.y) * HD + 4 * own_half;
+        for (int u = 0; u < U; ++u) {
+            const int r = u * ROWS + lane / PIECES, from = min(r, n_k - 1 - p0);
+            q8_fetch_lds(vp, (uint32_t)from * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn<HD>(r)) * 16, lds0 + slot * (2 * PART) + PART + u * 1024);
+        }
+    };
+    for (int b = 0; b < min(n_blocks, RING - 1); ++b) fetch(b, b);
+    const int2 to = place(A, T, r32);
+    const int last = to_see + to.x;
+    pr_bf16x8 qf[HD / 16];
+    load_query<HD>(A, T, head, to, half, qf);
+
+    pr_floatx16 o[HD / 32];
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const pr_uintx2 v = {pr_pack2(o[d][i] * inv, o[d][i + 1] * inv), pr_pack2(o[d][i + 2] * inv, o[d][i + 3] * inv)};
-            *reinterpret_cast<pr_uintx2*>(dst + 32 * d + 2 * i) = v;
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    float m = -INFINITY, l[2] = {0.f, 0.f};
+    const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn<HD>(v_row);
+    int slot = 0;
+    for (int block = 0; block < n_blocks; ++block) {
+        if (block + RING - 2 < n_blocks) q8_wait_fetches<(RING - 2) * 2 * U>();
+        else q8_wait_fetches<0>();
+        q8_wait_lds();
+        if (block + RING - 1 < n_blocks) fetch(block + RING - 1, slot == 0 ? RING - 1 : slot - 1);
+        char* const keys = lds + slot * (2 * PART);
+        char* const values = keys + PART;
+        pr_floatx16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c) {
+            const pr_bf16x8 kf = *reinterpret_cast<const pr_bf16x8*>(keys + r32 * ROW + ((2 * c + half) ^ key_turn<HD>(r32)) * 16);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[c], s, 0, 0, 0);
         }
+        const bool masked = (block + 1) * FEW > n_clear;
+        if (masked) {
+            const int seen = last - block * FEW - 4 * half;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i / 4) + i % 4 > seen) s[i] = -INFINITY;
+        }
+        float top = fmaxf(s[0], s[1]);
+#pragma unroll
+        for (int i = 2; i < 16; i += 2) top = fmaxf(fmaxf(s[i], s[i + 1]), top);
+        top = fmaxf(both_max(top), m);
+        if (__any(top > m)) {
+            const float f = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * A.factor);
+            l[0] *= f;
+            l[1] *= f;
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= f;
+            m = top;
+        }
+        if (masked && has_odd<U>(values)) {
+            int(*const first)[HD] = reinterpret_cast<int(*)[HD]>(keys);   // (the block's keys have been read)
+            q8_wait_lds();
+            clear_odd<HD, FEW>(values, block * FEW, first, lane, 64);
+            q8_wait_lds();
+            add_odd<HD>(first, half, last, o);
+            q8_wait_lds();
+        }
+        const float shift = m == -INFINITY ? 0.f : m * A.factor;   // (a row that has seen nothing yet)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const pr_bf16x8 pf = eight_weights(s, 8 * k, A.factor, shift, l[k]);
+#pragma unroll
+            for (int d = 0; d < HD / 32; ++d) {
+                const int piece = ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_turn) * 16;
+                union {
+                    pr_shortx4 h[2];
+                    pr_bf16x8 f;
+                } vf;
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) pr_shortx4*)(values + (v_row + 16 * k + 8 * j) * ROW + (lane & 1) * 8 + piece));
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf, o[d], 0, 0, 0);
+            }
+        }
+        slot = slot == RING - 1 ? 0 : slot + 1;
+    }
+    leave<HD, TILE>(A, T, head, r32, half, o, m, both_sum(l[0] + l[1]), last >= 0);
 }
 
-// The parts of a tile's rows, in their order: eight dims of a row a thread
+// The parts of a tile's rows: eight dims of a row a thread, every fourth part a wavefront, whose sums meet in LDS (always in the same order)
 template <int HD, int TILE>
 __global__ void __launch_bounds__(256) join_kernel(Args A)
 {
-    constexpr int LANES = HD / 8, ROWS = 256 / LANES;   // rows of a workgroup
-    constexpr int GROUPS = (TILE + ROWS - 1) / ROWS;
-    const int job = blockIdx.x / GROUPS, r = (blockIdx.x % GROUPS) * ROWS + threadIdx.x / LANES, dim = threadIdx.x % LANES * 8;
+    constexpr int LANES = HD / 8, ROWS = 64 / LANES, GROUPS = TILE / ROWS;   // rows of a workgroup, workgroups of a tile
+    const int job = blockIdx.x / GROUPS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int r = (blockIdx.x % GROUPS) * ROWS + lane / LANES, dim = lane % LANES * 8;
     const int number = A.heads.div(job), head = job - number * (int)A.heads.d, group = A.group.d;
     const Tile T = find_tile<TILE>(A, number);
-    if (T.seq < 0 || r >= TILE || T.row0 + r >= T.n_rows) return;
-    const int parts = A.parts.d;
-    const float* ml = A.part_ml + ((size_t)job * parts * TILE + r) * 2;
-    const float* po = A.part_o + ((size_t)job * parts * TILE + r) * HD + dim;
+    if (T.seq < 0 || T.row0 + (int)(blockIdx.x % GROUPS) * ROWS >= T.n_rows) return;
+    const int blocks = blocks_of<TILE>(A, T), parts = max(1, (blocks + chunk_of(A, blocks) - 1) / chunk_of(A, blocks));
+    const size_t step = (size_t)A.heads.d * TILE, first = ((size_t)number * A.parts.d * A.heads.d + head) * TILE + r;   // rows
+    const float* ml = A.part_ml + first * 2;
+    const float* po = A.part_o + first * HD + dim;
     float m = -INFINITY, l = 0.f, v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int p = 0; p < parts; ++p) m = fmaxf(m, ml[(size_t)p * TILE * 2]);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-        const float2 q = *reinterpret_cast<const float2*>(ml + (size_t)p * TILE * 2);
-        const float f = q.x == m ? 1.f : __builtin_amdgcn_exp2f((q.x - m) * A.factor);
-        l = fmaf(q.y, f, l);
-        const pr_floatx4 a = *reinterpret_cast<const pr_floatx4*>(po + (size_t)p * TILE * HD), b = *reinterpret_cast<const pr_floatx4*>(po + (size_t)p * TILE * HD + 4);
+    auto add = [&](float2 q, const pr_floatx4& a, const pr_floatx4& b) {
+        const float top = fmaxf(m, q.x);
+        const float old = m == top ? 1.f : __builtin_amdgcn_exp2f((m - top) * A.factor), f = q.x == top ? 1.f : __builtin_amdgcn_exp2f((q.x - top) * A.factor);
+        l = fmaf(q.y, f, l * old);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[i] = fmaf(a[i], f, v[i]);
-            v[4 + i] = fmaf(b[i], f, v[4 + i]);
+        for (int e = 0; e < 4; ++e) {
+            v[e] = fmaf(a[e], f, v[e] * old);
+            v[4 + e] = fmaf(b[e], f, v[4 + e] * old);
         }
+        m = top;
+    };
+    // eight parts at a time (beyond the last one: it again, not added): one by one each would wait for memory
+    constexpr int N = 8;
+    for (int p0 = wave; p0 < parts; p0 += 4 * N) {
+        float2 q[N];
+        pr_floatx4 a[N], b[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const size_t p = min(p0 + 4 * i, parts - 1);
+            q[i] = *reinterpret_cast<const float2*>(ml + p * step * 2);
+            a[i] = *reinterpret_cast<const pr_floatx4*>(po + p * step * HD);
+            b[i] = *reinterpret_cast<const pr_floatx4*>(po + p * step * HD + 4);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (p0 + 4 * i < parts) add(q[i], a[i], b[i]);
     }
+    __shared__ pr_floatx4 sums[4][2][64];
+    __shared__ float2 tops[4][64];
+    tops[wave][lane] = make_float2(m, l);
+    sums[wave][0][lane] = (pr_floatx4){v[0], v[1], v[2], v[3]};
+    sums[wave][1][lane] = (pr_floatx4){v[4], v[5], v[6], v[7]};
+    __syncthreads();
+    if (wave || T.row0 + r >= T.n_rows) return;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) add(tops[w][lane], sums[w][0][lane], sums[w][1][lane]);
     const int row = T.row0 + r, at = A.group.div(row), sub = row - at * group;
     const float inv = T.n_k - T.n_q + at < 0 ? 0.f : 1.f / l;
     pr_uintx4 w;
@@ -374,34 +568,47 @@ __global__ void __launch_bounds__(256) join_kernel(Args A)
     *reinterpret_cast<pr_uintx4*>(A.out + (size_t)(T.q_begin + at) * A.ld_out + (size_t)(head * group + sub) * HD + dim) = w;
 }
 
-// How many wavefronts a workgroup has, and among how many workgroups a tile's keys are shared out: as many rows as the sequences have, and
-// workgroups for all places that the compute units have for them, as long as a part has four blocks.
-constexpr int MOST_PARTS = 32;
+// How many wavefronts a workgroup has -- as many rows as the sequences have -- and how many blocks of keys: such that all of them together fill the
+// places that the compute units have for workgroups once, at least four, and only if that saves more blocks (some microsecond each) than the
+// join costs.  Sequences differ in length: a tile may have several times as many parts as places allow on average.
+constexpr int MOST_PARTS = 64, LEAST_CHUNK = 4, JOIN_BLOCKS = 8;
 struct Plan {
-    int waves, parts;
+    int waves, parts, chunk;
     int64_t tiles;          // units of a launch, at most
     size_t part_bytes;      // of the workspace, for one part of every tile
 };
-Plan plan(int q_rows, int batch, int n_kv_heads, int group, int head_dim, int64_t q_len, int64_t k_len, int waves = 0)
+Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head_dim, int64_t q_len, int64_t k_len, int waves = 0)
 {
     Plan p;
     p.waves = waves ? waves : q_len * group <= 32 ? 1 : q_len * group <= 64 ? 2 : 4;
     const int rows = 32 * p.waves;
     p.tiles = (int64_t)q_rows * group / rows + batch;
-    // sequences of about one length each
-    const int64_t wgs = std::min(p.tiles, std::max((int64_t)1, ((int64_t)q_rows * group + rows - 1) / rows)) * n_kv_heads;
-    const int64_t places = 256 * (head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
-    p.parts = (int)std::max((int64_t)1, std::min({places / wgs, (k_len / BLK + 3) / 4, (int64_t)MOST_PARTS}));
     p.part_bytes = (size_t)p.tiles * n_kv_heads * rows * (head_dim + 2) * 4;
+    const int64_t wgs = std::min(p.tiles, std::max((int64_t)batch, ((int64_t)q_rows * group + rows - 1) / rows)) * n_kv_heads;
+    const int64_t places = 256 * (head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
+    const int64_t longest = (k_len + BLK - 1) / BLK, mean = std::min(longest, (int64_t)k_rows / batch / BLK + 1);
+    const int64_t most = std::min((int64_t)MOST_PARTS, 4 / p.waves * places / wgs);
+    // One sequence: as many parts of each tile as there are places.  Several, of different lengths: the last part of a tile is rarely a whole one, and
+    // a few workgroups more than there are places take as long as twice as many.
+    const int64_t each = std::max((int64_t)1, places / wgs), spare = std::max(places - wgs, places / 2);
+    int64_t chunk = std::max((int64_t)LEAST_CHUNK, batch == 1 ? (longest + each - 1) / each : (wgs * mean + spare - 1) / spare);
+    p.parts = 1;
+    if (most > 1) {
+        chunk = std::max(chunk, (longest + most - 1) / most);
+        if (longest - chunk > JOIN_BLOCKS) p.parts = (int)((longest + chunk - 1) / chunk);
+    }
+    p.chunk = (int)std::min(chunk, (int64_t)1 << 26);
     return p;
 }
 
 template <int HD, int WAVES>
 void launch(const Args& a, const Plan& p, hipStream_t s)
 {
-    hipLaunchKernelGGL((attention_kernel<HD, WAVES>), dim3((unsigned)(p.tiles * a.heads.d * p.parts)), dim3(64 * WAVES), 0, s, a);
+    const dim3 grid((unsigned)(p.tiles * a.heads.d * p.parts));
+    if constexpr (WAVES == 1) hipLaunchKernelGGL((few_kernel<HD>), grid, dim3(64), 0, s, a);
+    else hipLaunchKernelGGL((attention_kernel<HD, WAVES>), grid, dim3(64 * WAVES), 0, s, a);
     if (p.parts > 1) {
-        constexpr int ROWS = 2048 / HD, GROUPS = (32 * WAVES + ROWS - 1) / ROWS;
+        constexpr int GROUPS = 32 * WAVES * HD / 512;
         hipLaunchKernelGGL((join_kernel<HD, 32 * WAVES>), dim3((unsigned)(p.tiles * a.heads.d * GROUPS)), dim3(256), 0, s, a);
     }
 }
@@ -416,8 +623,8 @@ extern "C" size_t spec_prompt_attention_workspace_bytes(int32_t q_rows, int32_t 
     if (q_rows <= 0 || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128)) return 0;
     size_t most = 0;
     for (int waves = 1; waves <= 4; waves *= 2) {
-        const Plan p = plan(q_rows, batch, n_kv_heads, n_q_heads / n_kv_heads, head_dim, 0, INT_MAX, waves);
-        if (p.parts > 1) most = std::max(most, p.parts * p.part_bytes);
+        const Plan p = plan(q_rows, INT_MAX, batch, n_kv_heads, n_q_heads / n_kv_heads, head_dim, 0, INT_MAX, waves);
+        most = std::max(most, p.parts > 1 ? p.parts * p.part_bytes : 0);
     }
     return most;
 }
@@ -451,14 +658,14 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
         return fail(SPEC_ERR_SHAPE, "spec_prompt_attention: %d query rows are too many", a.q_rows);
     // lengths that are not known: all rows are of one sequence, or of as many as there are, whichever gives more workgroups
     const int64_t q_len = a.max_q_len ? a.max_q_len : a.q_rows, k_len = a.max_k_len ? a.max_k_len : a.k_rows;
-    Plan p = plan(a.q_rows, a.batch, a.n_kv_heads, group, a.head_dim, q_len, k_len);
+    Plan p = plan(a.q_rows, a.k_rows, a.batch, a.n_kv_heads, group, a.head_dim, q_len, k_len);
     if (p.parts > 1) p.parts = workspace ? (int)std::min((size_t)p.parts, workspace_bytes / p.part_bytes) : 1;
     if (p.parts < 1) p.parts = 1;
     float* const ws = (float*)workspace;
     const size_t rows = p.part_bytes / (a.head_dim + 2) / 4 * p.parts;
     const Args g{(const uint16_t*)a.q, (const uint16_t*)a.k, (const uint16_t*)a.v, (uint16_t*)a.out, a.ld_q, a.ld_k, a.ld_v, a.ld_out, a.q_row0,
                  a.k_row0, FastDiv(a.n_kv_heads), FastDiv(group), a.batch, a.q_rows, a.k_rows, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 0x1p-149f),
-                 a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr};
+                 a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? p.chunk : 1 << 26, p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr};
     hipStream_t s = (hipStream_t)stream;
     if (a.head_dim == 128) {
         if (p.waves == 1) launch<128, 1>(g, p, s);
