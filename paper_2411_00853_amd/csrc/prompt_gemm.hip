@@ -23,7 +23,7 @@ __device__ __forceinline__ float activate(float v)
     if (ACT == SPEC_ACT_RELU) return v < 0.f ? 0.f : v;
     if (ACT == SPEC_ACT_GELU) {
         // erfc(z) = (a1 t + .. + a5 t^5) exp(-z^2), t = 1 / (1 + 0.3275911 z), off by 1.5e-7 at most (Abramowitz and Stegun, 7.1.26).
-        // 1333 x 4104 x 2080 with the library's erf: 40.1 us
+        // 1333 x 4104 x 2080 with gelu alone 31 us; with the library's erf, before other steps, 40.1 where this took 35.5
         const float z = fabsf(v) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
         const float p = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f) * t;
         const float half = 0.5f * p * __builtin_amdgcn_exp2f(z * z * -1.44269504f);
@@ -37,35 +37,46 @@ __device__ __forceinline__ float activate(float v)
 struct Four {
     pr_floatx4 v, up;
 };
+template <bool WHOLE>
 __device__ __forceinline__ pr_floatx4 load_bias(const Out& o, int n)
 {
     pr_floatx4 b = {0.f, 0.f, 0.f, 0.f};
-    if (o.whole) return *reinterpret_cast<const pr_floatx4*>(o.bias + n);
+    if (WHOLE) return *reinterpret_cast<const pr_floatx4*>(o.bias + n);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
         if (n % o.N + i < o.N) b[i] = o.bias[n + i];
     return b;
 }
-__device__ __forceinline__ pr_floatx4 load_residual(const Out& o, int64_t m, int n)
+// The residual's four numbers as they lie in memory: made floats where they are added, as that has to wait for them
+template <bool WHOLE>
+__device__ __forceinline__ pr_uintx4 load_residual(const Out& o, int64_t m, int n)
 {
-    pr_floatx4 r = {0.f, 0.f, 0.f, 0.f};
+    pr_uintx4 r = {0, 0, 0, 0};
     const int64_t at = m * o.ld_r + n;
-    if (o.whole) {
-        if (o.r_dtype == SPEC_DTYPE_FP32) return *reinterpret_cast<const pr_floatx4*>((const float*)o.residual + at);
+    if (WHOLE) {
+        if (o.r_dtype == SPEC_DTYPE_FP32) return *reinterpret_cast<const pr_uintx4*>((const float*)o.residual + at);
         const pr_uintx2 u = *reinterpret_cast<const pr_uintx2*>((const uint16_t*)o.residual + at);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = __uint_as_float(i & 1 ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16);
+        r[0] = u[0];
+        r[1] = u[1];
         return r;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (n + i < o.N) r[i] = o.r_dtype == SPEC_DTYPE_FP32 ? ((const float*)o.residual)[at + i] : q8_widen(((const uint16_t*)o.residual)[at + i]);
+        if (n + i < o.N) r[i] = o.r_dtype == SPEC_DTYPE_FP32 ? ((const unsigned*)o.residual)[at + i] : (unsigned)((const uint16_t*)o.residual)[at + i] << 16;
     return r;
 }
+template <bool WHOLE>
+__device__ __forceinline__ pr_floatx4 residual_of(const Out& o, const pr_uintx4& r)
+{
+    const bool pairs = WHOLE && o.r_dtype != SPEC_DTYPE_FP32;
+    return (pr_floatx4){__uint_as_float(pairs ? r[0] << 16 : r[0]), __uint_as_float(pairs ? r[0] & 0xffff0000u : r[1]), __uint_as_float(pairs ? r[1] << 16 : r[2]),
+                        __uint_as_float(pairs ? r[1] & 0xffff0000u : r[3])};
+}
+template <bool WHOLE>
 __device__ __forceinline__ void store(const Out& o, int64_t m, int n, const pr_floatx4& v)
 {
     const int64_t at = m * o.ld_y + n;
-    if (o.whole) {
+    if (WHOLE) {
         if (o.y_dtype == SPEC_DTYPE_FP32) *reinterpret_cast<pr_floatx4*>((float*)o.y + at) = v;
         else *reinterpret_cast<pr_uintx2*>((uint16_t*)o.y + at) = (pr_uintx2){pr_pack2(v[0], v[1]), pr_pack2(v[2], v[3])};
         return;
@@ -78,23 +89,26 @@ __device__ __forceinline__ void store(const Out& o, int64_t m, int n, const pr_f
     }
 }
 
-// R rows (stride apart in rows) by C groups of four columns, `step` columns apart from n on.  What is read is asked for three rows ahead of its sums.
-template <int ACT, int R, int C, typename GET>
+// R rows (stride apart in rows) by C groups of four columns, `step` columns apart from n on.  What is read is asked for three rows ahead of its sums
+// (1333 x 4104 x 2080 with bias and residual 29.8 us, plain 28.9; lanes that exchange their columns for stores of 16 bytes take 0.5 us off that).
+// Whether groups are whole is asked once, here: asked at each access, with gelu, bias and residual 43.1 us where this took 38.4.
+template <int ACT, bool WHOLE, int R, int C, typename GET>
 __device__ __forceinline__ void finish_as(const Out& o, int m0, int stride, int M, int n0, int step, GET get)
 {
     const pr_floatx4 zero = {0.f, 0.f, 0.f, 0.f};
-    pr_floatx4 bias[C], bias_up[C], res[4][C];
+    pr_floatx4 bias[C], bias_up[C];
+    pr_uintx4 res[4][C];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int n = n0 + step * c;
-        bias[c] = o.bias && n < o.N ? load_bias(o, n) : zero;
-        bias_up[c] = ACT == SPEC_ACT_SWIGLU && o.bias && n < o.N ? load_bias(o, o.N + n) : zero;
+        bias[c] = o.bias && n < o.N ? load_bias<WHOLE>(o, n) : zero;
+        bias_up[c] = ACT == SPEC_ACT_SWIGLU && o.bias && n < o.N ? load_bias<WHOLE>(o, o.N + n) : zero;
     }
     auto ask = [&](int r) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int m = m0 + stride * r, n = n0 + step * c;
-            res[r & 3][c] = o.residual && m < M && n < o.N ? load_residual(o, m, n) : zero;
+            res[r & 3][c] = o.residual && m < M && n < o.N ? load_residual<WHOLE>(o, m, n) : (pr_uintx4){0, 0, 0, 0};
         }
     };
 #pragma unroll
@@ -111,21 +125,27 @@ __device__ __forceinline__ void finish_as(const Out& o, int m0, int stride, int 
             const pr_floatx4 up = f.up + bias_up[c];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = activate<ACT>(v[i]) * (ACT == SPEC_ACT_SWIGLU ? up[i] : 1.f);
-            if (o.residual) v += res[r & 3][c];     // (-0 + 0 would be 0)
-            if (m < M && n < o.N) store(o, m, n, v);
+            if (o.residual) v += residual_of<WHOLE>(o, res[r & 3][c]);     // (-0 + 0 would be 0)
+            if (m < M && n < o.N) store<WHOLE>(o, m, n, v);
         }
+    }
+}
+template <bool WHOLE, bool GATED, int R, int C, typename GET>
+__device__ __forceinline__ void finish_for(const Out& o, int m0, int stride, int M, int n0, int step, GET get)
+{
+    if (GATED) return finish_as<SPEC_ACT_SWIGLU, WHOLE, R, C>(o, m0, stride, M, n0, step, get);
+    switch (o.act) {   // (the launch's)
+    case SPEC_ACT_RELU: return finish_as<SPEC_ACT_RELU, WHOLE, R, C>(o, m0, stride, M, n0, step, get);
+    case SPEC_ACT_GELU: return finish_as<SPEC_ACT_GELU, WHOLE, R, C>(o, m0, stride, M, n0, step, get);
+    case SPEC_ACT_SILU: return finish_as<SPEC_ACT_SILU, WHOLE, R, C>(o, m0, stride, M, n0, step, get);
+    default: return finish_as<SPEC_ACT_NONE, WHOLE, R, C>(o, m0, stride, M, n0, step, get);
     }
 }
 template <bool GATED, int R, int C, typename GET>
 __device__ __forceinline__ void finish(const Out& o, int m0, int stride, int M, int n0, int step, GET get)
 {
-    if (GATED) return finish_as<SPEC_ACT_SWIGLU, R, C>(o, m0, stride, M, n0, step, get);
-    switch (o.act) {   // (the launch's)
-    case SPEC_ACT_RELU: return finish_as<SPEC_ACT_RELU, R, C>(o, m0, stride, M, n0, step, get);
-    case SPEC_ACT_GELU: return finish_as<SPEC_ACT_GELU, R, C>(o, m0, stride, M, n0, step, get);
-    case SPEC_ACT_SILU: return finish_as<SPEC_ACT_SILU, R, C>(o, m0, stride, M, n0, step, get);
-    default: return finish_as<SPEC_ACT_NONE, R, C>(o, m0, stride, M, n0, step, get);
-    }
+    if (o.whole) finish_for<true, GATED, R, C>(o, m0, stride, M, n0, step, get);
+    else finish_for<false, GATED, R, C>(o, m0, stride, M, n0, step, get);
 }
 
 // The 16 RT x 16 CT block of products that a wavefront holds, from row m0 and column tile j0 of W on
@@ -152,8 +172,12 @@ constexpr size_t MOST_PARTS = (size_t)1 << 25;   // floats of a workspace that i
 //
 // A stage is 2 RT steps of CT products (32 columns of K by RT row tiles, twice).  Nothing is waited for in a row: X's operand is read from LDS
 // AHEAD steps before its products, W's half a stage before, and the requests for later stages go out one by one between the products -- all at
-// once they keep the wavefront from its products for as long as the fetch of a stage takes.  The wavefronts meet AHEAD steps before a stage's
-// end: there the stage is in registers, its place is free, and the next one has to be there.
+// once they keep the wavefront from its products for as long as the fetch of a stage takes (2048 x 22016 x 4096, gate and up: 343 us, between the
+// products 280).  The wavefronts meet AHEAD steps before a stage's end: there the stage is in registers, its place is free, and the next one has
+// to be there.
+//
+// What bounds it: large products the power of the card -- 4096 x 4096 x 8192 runs at 1.47 PFLOP/s, with zeros for operands at 1.92 -- others the
+// tiles that do not fill the compute units' last turn, and some 8 us of launch, first fetch and epilogue: 1333 x 4104 x 2080 in 231 tiles 28.9 us.
 template <bool GATED, int WR, int WC, int RT, int CT, int SX, int SW, int AHEAD>
 __global__ void __launch_bounds__(64 * WR * WC, 2) tiled_kernel(const uint16_t* __restrict__ x, const uint8_t* __restrict__ w, int64_t ld_x, int M, int K, int n_tiles, int row_blocks,
                                                       int col_blocks, int splits, int per_split, Out out, float* __restrict__ partial)
@@ -168,7 +192,7 @@ __global__ void __launch_bounds__(64 * WR * WC, 2) tiled_kernel(const uint16_t* 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, g = lane >> 4;
     const int wr = wave / WC, wc = wave % WC;
     // An XCD takes neighbouring tiles: panels of PANEL row blocks, column block by column block, so that the 32 compute units of an XCD work on some
-    // 8 by 4 tiles and its L2 has each operand once (all row blocks of one column block: 8192 x 8192 x 8192 901 us, now 815)
+    // 8 by 4 tiles and its L2 has each operand once (8192 x 8192 x 8192: 832 us; all row blocks of one column block at a time: 901)
     const int tiles = row_blocks * col_blocks, total = tiles * splits, xcd = blockIdx.x & 7, each = total >> 3, more = total & 7;
     const int id = xcd * each + min(xcd, more) + (blockIdx.x >> 3), split = id / tiles, tile = id - split * tiles;
     const int panel = tile / (PANEL * col_blocks), in_panel = tile - panel * PANEL * col_blocks, high = min(PANEL, row_blocks - panel * PANEL);
@@ -320,7 +344,8 @@ __global__ void __launch_bounds__(256) join_kernel(const float* __restrict__ par
 // ---- few rows: the stream of W ------------------------------------------------------------------------------------------
 //
 // A workgroup takes 16 RT rows by 16 NT columns; its wavefronts share out K by 128 columns and add their sums up in LDS.  Both operands go
-// straight into registers, the next 128 columns' while this one's products run.
+// straight into registers, the next 128 columns' while this one's products run.  Memory bounds it: 8 x 32000 x 4096 38.5 us, 6.8 TB/s of weights (some
+// of which stay in the card's last cache from one call to the next).
 template <bool GATED, int RT, int NT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES) skinny_kernel(const uint16_t* __restrict__ x, const uint8_t* __restrict__ w, int64_t ld_x, int M, int K, int n_tiles, Out out)
 {
@@ -442,8 +467,8 @@ struct Shape {
     int rows, cols, slots;      // slots: SW, which a part's stages have to exceed
     float us1, us2;             // us2 = 0: one workgroup on a compute unit
 };
-constexpr Shape SHAPES[] = {{256, 256, 3, 1.4f, 0.f}, {256, 128, 3, 0.8f, 0.f}, {128, 256, 3, 0.8f, 0.f}, {128, 128, 3, 0.56f, 0.88f},
-                            {64, 128, 3, 0.30f, 0.52f}, {64, 64, 4, 0.23f, 0.36f}, {32, 64, 5, 0.19f, 0.30f}};
+constexpr Shape SHAPES[] = {{256, 256, 3, 1.4f, 0.f}, {256, 128, 3, 0.8f, 0.f}, {192, 128, 3, 0.66f, 0.f}, {128, 256, 3, 0.8f, 0.f},
+                            {128, 128, 3, 0.56f, 0.88f}, {96, 128, 3, 0.48f, 0.70f}, {64, 128, 3, 0.30f, 0.52f}, {64, 64, 4, 0.23f, 0.36f}, {32, 64, 5, 0.19f, 0.30f}};
 struct Plan {
     int shape, splits, per_split;   // shape < 0: K is shared out within workgroups
     size_t floats;                  // of the workspace
@@ -459,11 +484,13 @@ Plan plan(int M, int n_tiles, int K, size_t floats)
     for (int i = 0; i < (int)(sizeof(SHAPES) / sizeof(SHAPES[0])); ++i) {
         const Shape& t = SHAPES[i];
         const int64_t tiles = (int64_t)((M + t.rows - 1) / t.rows) * ((16 * (int64_t)n_tiles + t.cols - 1) / t.cols);
+        if (tiles > 0x7fffffff / 8) continue;
         for (int splits = 1; splits <= 8; ++splits) {
             const int per = (stages + splits - 1) / splits;
             const size_t need = splits > 1 ? (size_t)splits * M * n_tiles * 16 : 0;
-            if (stages - (splits - 1) * per <= t.slots || need > floats || tiles * splits > 0x7fffffff) continue;
-            const int64_t wgs = tiles * splits, whole = t.us2 ? wgs / 512 : wgs / 256, rest = wgs - whole * (t.us2 ? 512 : 256);
+            if (need > floats || (splits > 1 && tiles * splits > 1024)) break;   // (nor would more of them do)
+            if (stages - (splits - 1) * per <= t.slots) continue;
+            const int wgs = (int)tiles * splits, at_once = t.us2 ? 512 : 256, whole = wgs / at_once, rest = wgs % at_once;
             const float round = (float)whole * (t.us2 ? t.us2 : t.us1) + (rest == 0 ? 0.f : rest <= 256 ? t.us1 : t.us2);
             const float work = round * per, join = splits > 1 ? 2.5f + (float)need * 8e-6f / 5.f : 0.f;
             const float us = std::max(work, stream) + 0.1f * work + join;
@@ -483,11 +510,13 @@ void launch(const Call& c)
     switch (p.shape) {
     case 0: return launch_tiled<GATED, 2, 4, 8, 4, 2, 3, 1>(c, p.splits, p.per_split);
     case 1: return launch_tiled<GATED, 4, 2, 4, 4, 3, 3, 3>(c, p.splits, p.per_split);
-    case 2: return launch_tiled<GATED, 2, 4, 4, 4, 3, 3, 1>(c, p.splits, p.per_split);
-    case 3: return launch_tiled<GATED, 2, 2, 4, 4, 2, 3, 1>(c, p.splits, p.per_split);
-    case 4: return launch_tiled<GATED, 2, 2, 2, 4, 3, 3, 1>(c, p.splits, p.per_split);
-    case 5: return launch_tiled<GATED, 2, 2, 2, 2, 3, 4, 1>(c, p.splits, p.per_split);
-    case 6: if constexpr (!GATED) return launch_tiled<GATED, 1, 4, 2, 1, 4, 5, 1>(c, p.splits, p.per_split);
+    case 2: return launch_tiled<GATED, 4, 2, 3, 4, 3, 3, 2>(c, p.splits, p.per_split);
+    case 3: return launch_tiled<GATED, 2, 4, 4, 4, 3, 3, 1>(c, p.splits, p.per_split);
+    case 4: return launch_tiled<GATED, 2, 2, 4, 4, 2, 3, 1>(c, p.splits, p.per_split);
+    case 5: return launch_tiled<GATED, 2, 2, 3, 4, 2, 3, 2>(c, p.splits, p.per_split);
+    case 6: return launch_tiled<GATED, 2, 2, 2, 4, 3, 3, 1>(c, p.splits, p.per_split);
+    case 7: return launch_tiled<GATED, 2, 2, 2, 2, 3, 4, 1>(c, p.splits, p.per_split);
+    case 8: if constexpr (!GATED) return launch_tiled<GATED, 1, 4, 2, 1, 4, 5, 1>(c, p.splits, p.per_split);
             else return launch_tiled<GATED, 1, 2, 2, 2, 4, 5, 1>(c, p.splits, p.per_split);
     }
     // (one row of 4096 x 4096: 6.8 us, 8.2 with two column tiles and eight wavefronts; 8 rows of 32000 x 4096 42.6 with one tile and four, 39.3 with two)
