@@ -58,23 +58,43 @@ __device__ __forceinline__ int wave_scan(int v)
     return v;
 }
 
-// Which unit of work a workgroup has, if sequence b has count(b) units and they are numbered sequence by sequence: the sequence (-1: none,
-// there are fewer) and the number within it.  By all lanes of every wavefront alike, 64 sequences at a time.
+// Which unit of work a workgroup has, if sequence b has count(b) units: the sequence (-1: none, there are fewer units) and the unit's number within
+// it.  Units are numbered sequence by sequence, the last one of each first; by_place: 64 sequences at a time, those with the highest number within
+// their sequence first.  By all lanes of every wavefront alike.
 struct PromptUnit {
     int seq, index, lane;   // lane: which one has counted the sequence
 };
 template <typename COUNT>
-__device__ __forceinline__ PromptUnit prompt_unit(int unit, int batch, COUNT count)
+__device__ __forceinline__ PromptUnit prompt_unit(int unit, int batch, bool by_place, COUNT count)
 {
     const int lane = threadIdx.x & 63;
     for (int b0 = 0; b0 < batch; b0 += 64) {
         const int n = b0 + lane < batch ? count(b0 + lane) : 0, sum = wave_scan(n);
         const int total = __builtin_amdgcn_readlane(sum, 63);
-        if (unit < total) {
-            const int at = __builtin_ctzll(__ballot(unit < sum));
-            return {b0 + at, unit - __builtin_amdgcn_readlane(sum - n, at), at};
+        if (unit >= total) {
+            unit -= total;
+            continue;
         }
-        unit -= total;
+        if (!by_place) {
+            const int at = __builtin_ctzll(__ballot(unit < sum));
+            return {b0 + at, __builtin_amdgcn_readlane(sum, at) - 1 - unit, at};
+        }
+        auto from = [&](int index) { return __builtin_amdgcn_readlane(wave_scan(max(n - index, 0)), 63); };   // units with this number or a higher one
+        int lo = 0, hi = 1;     // from(lo) > unit >= from(hi)
+        while (from(hi) > unit) {
+            lo = hi;
+            hi *= 2;
+        }
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (from(mid) > unit) lo = mid;
+            else hi = mid;
+        }
+        const int nth = unit - from(hi);            // (by all lanes)
+        const uint64_t with = __ballot(n > lo);     // those sequences have a unit of this number, and this many of them come before the lane's
+        const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(with >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)with, 0u));
+        const int at = __builtin_ctzll(__ballot(n > lo && before == nth));
+        return {b0 + at, lo, at};
     }
     return {-1, 0, 0};
 }

@@ -25,18 +25,21 @@ struct Args {
     FastDiv parts;      // a tile's keys are shared out among at most so many workgroups,
     int chunk;          // each of which takes so many blocks (more where parts would not do); with more than one part, what they leave to the join:
     float *part_o, *part_ml;   // [unit][part][kv head][row of the tile][head_dim] sums of weighted values, [..][2] maximum and sum of weights
+    bool by_place;      // the order of the tiles: by their place in their sequences, the last ones first; otherwise sequence by sequence
 };
 
-// The tile of a unit (its number and kv head): of one sequence, some rows
+// The tile of a unit (its number and kv head): of one sequence, some rows.  Longer tiles come first, so that short ones fill what is left of the
+// compute units' time: within a sequence, and with by_place over 64 sequences (8 x 1024 positions of 32 heads of 64: 57 -> 51 us; the search takes
+// a microsecond more).
 struct Tile {
     int seq, q_begin, n_q, k_begin, n_k, n_rows, row0;
 };
 template <int TILE>
-__device__ __forceinline__ Tile find_tile(const Args& A, int number)
+__device__ __forceinline__ Tile find_tile(const Args& A, int number, bool by_place)
 {
     const int group = A.group.d;
     PromptSpan q_span{0, 0}, k_span{0, 0};   // of the sequence that this lane looks at
-    const PromptUnit unit = prompt_unit(number, A.batch, [&](int b) {
+    const PromptUnit unit = prompt_unit(number, A.batch, by_place, [&](int b) {
         q_span = k_span = prompt_span(A.q_row0, b, A.q_rows);
         if (A.k_row0) k_span = prompt_span(A.k_row0, b, A.k_rows);
         return ((q_span.end - q_span.begin) * group + TILE - 1) / TILE;
@@ -48,7 +51,7 @@ __device__ __forceinline__ Tile find_tile(const Args& A, int number)
     t.k_begin = __builtin_amdgcn_readlane(k_span.begin, unit.lane);
     t.n_k = __builtin_amdgcn_readlane(k_span.end, unit.lane) - t.k_begin;
     t.n_rows = t.n_q * group;
-    t.row0 = ((t.n_rows + TILE - 1) / TILE - 1 - unit.index) * TILE;   // the tiles with the longest way first
+    t.row0 = unit.index * TILE;
     return t;
 }
 
@@ -118,12 +121,19 @@ __device__ __forceinline__ void leave(const Args& A, const Tile& T, int head, in
     }
     const float inv = seen ? 1.f / sum : 0.f;
     const int2 to = place(A, T, row);
-    uint16_t* dst = A.out + (size_t)(T.q_begin + to.x) * A.ld_out + (size_t)(head * (int)A.group.d + to.y) * HD + 4 * half;
+    // lane and lane ^ 32 exchange every other four dims: then each stores eight in a row
+    uint16_t* dst = A.out + (size_t)(T.q_begin + to.x) * A.ld_out + (size_t)(head * (int)A.group.d + to.y) * HD + 8 * half;
 #pragma unroll
     for (int d = 0; d < HD / 32; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<pr_uintx2*>(dst + 32 * d + 2 * i) = (pr_uintx2){pr_pack2(o[d][i] * inv, o[d][i + 1] * inv), pr_pack2(o[d][i + 2] * inv, o[d][i + 3] * inv)};
+        for (int i = 0; i < 16; i += 8) {
+            pr_uintx2 w[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                w[j] = __builtin_amdgcn_permlane32_swap(pr_pack2(o[d][i + 2 * j] * inv, o[d][i + 2 * j + 1] * inv), pr_pack2(o[d][i + 4 + 2 * j] * inv, o[d][i + 5 + 2 * j] * inv),
+                                                        false, false);
+            *reinterpret_cast<pr_uintx4*>(dst + 32 * d + 2 * i) = (pr_uintx4){w[0][0], w[1][0], w[0][1], w[1][1]};
+        }
 }
 
 // The lane's query row as operands of the score product
@@ -208,7 +218,7 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r32 = lane & 31, half = lane >> 5;
     // Workgroups in a row take the kv heads: what they read lies together
     const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
-    const Tile T = find_tile<TILE>(A, number);
+    const Tile T = find_tile<TILE>(A, number, A.by_place);
     if (T.seq < 0) return;
     const int last_first = T.n_k - T.n_q + A.group.div(T.row0), all_blocks = blocks_of<TILE>(A, T);
     // This part's blocks; all positions below are counted from their first one
@@ -402,7 +412,7 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
     __shared__ __attribute__((aligned(16))) char lds[RING * 2 * PART];     // [place][keys, values]
     const int lane = threadIdx.x, r32 = lane & 31, half = lane >> 5;
     const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
-    const Tile T = find_tile<TILE>(A, number);
+    const Tile T = find_tile<TILE>(A, number, false);
     if (T.seq < 0) return;
     const int all_blocks = blocks_of<TILE>(A, T), chunk = chunk_of(A, all_blocks), p_first = part * chunk * BLK;
     if (part && part * chunk >= all_blocks) return;
@@ -517,7 +527,7 @@ __global__ void __launch_bounds__(256) join_kernel(Args A)
     const int job = blockIdx.x / GROUPS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int r = (blockIdx.x % GROUPS) * ROWS + lane / LANES, dim = lane % LANES * 8;
     const int number = A.heads.div(job), head = job - number * (int)A.heads.d, group = A.group.d;
-    const Tile T = find_tile<TILE>(A, number);
+    const Tile T = find_tile<TILE>(A, number, false);
     if (T.seq < 0 || T.row0 + (int)(blockIdx.x % GROUPS) * ROWS >= T.n_rows) return;
     const int blocks = blocks_of<TILE>(A, T), parts = max(1, (blocks + chunk_of(A, blocks) - 1) / chunk_of(A, blocks));
     const size_t step = (size_t)A.heads.d * TILE, first = ((size_t)number * A.parts.d * A.heads.d + head) * TILE + r;   // rows
@@ -576,6 +586,7 @@ struct Plan {
     int waves, parts, chunk;
     int64_t tiles;          // units of a launch, at most
     size_t part_bytes;      // of the workspace, for one part of every tile
+    bool by_place;          // more workgroups than places
 };
 Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head_dim, int64_t q_len, int64_t k_len, int waves = 0)
 {
@@ -598,6 +609,7 @@ Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head
         if (longest - chunk > JOIN_BLOCKS) p.parts = (int)((longest + chunk - 1) / chunk);
     }
     p.chunk = (int)std::min(chunk, (int64_t)1 << 26);
+    p.by_place = p.waves > 1 && batch > 1 && wgs > places;
     return p;
 }
 
@@ -665,7 +677,7 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     const size_t rows = p.part_bytes / (a.head_dim + 2) / 4 * p.parts;
     const Args g{(const uint16_t*)a.q, (const uint16_t*)a.k, (const uint16_t*)a.v, (uint16_t*)a.out, a.ld_q, a.ld_k, a.ld_v, a.ld_out, a.q_row0,
                  a.k_row0, FastDiv(a.n_kv_heads), FastDiv(group), a.batch, a.q_rows, a.k_rows, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 0x1p-149f),
-                 a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? p.chunk : 1 << 26, p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr};
+                 a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? p.chunk : 1 << 26, p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr, p.by_place && p.parts == 1};
     hipStream_t s = (hipStream_t)stream;
     if (a.head_dim == 128) {
         if (p.waves == 1) launch<128, 1>(g, p, s);

@@ -149,6 +149,7 @@ struct AppendArgs {
     const float* cos_sin;
     int32_t* flag;
     int n_q_heads, layer, batch, rows, max_batch, max_kv_len, kv_blocks;
+    FastDiv per_row, kv_heads;   // pairs of sixteen bytes of a row's queries; n_kv_heads
 };
 
 struct AppendSeq {
@@ -208,8 +209,8 @@ __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
     const int tid = threadIdx.x;
     if ((int)blockIdx.x < A.kv_blocks * n_kv) {
         __shared__ __align__(16) uint16_t values[32 * LD];
-        const int head = blockIdx.x % n_kv;
-        const PromptUnit u = prompt_unit((int)blockIdx.x / n_kv, A.batch, [&](int b) {
+        const int block = A.kv_heads.div((int)blockIdx.x), head = (int)blockIdx.x - block * n_kv;
+        const PromptUnit u = prompt_unit(block, A.batch, false, [&](int b) {
             const AppendSeq s = append_seq(A.row0, A.seq_slot, A.pos0, b, A.rows, A.max_batch, A.max_kv_len);
             if (!s.len) return 0;
             return s.ok ? ((s.pos + s.len - 1) >> 5) - (s.pos >> 5) + 1 : (s.len + 31) >> 5;
@@ -292,9 +293,9 @@ __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
         place[tid] = at;
     }
     __syncthreads();
-    const int per_row = A.n_q_heads * PAIRS;
+    const int per_row = A.per_row.d;
     for (int i = tid; i < 16 * per_row; i += TPB) {
-        const int t = i / per_row, p = i % per_row, head = p / PAIRS, c = p % PAIRS * 8;
+        const int t = A.per_row.div(i), p = i - t * per_row, head = p / PAIRS, c = p % PAIRS * 8;
         const int at = place[t];
         if (at == -2) continue;
         const size_t row = (size_t)r0 + t;
@@ -358,7 +359,8 @@ extern "C" int spec_prompt_append(spec_handle* h, int32_t layer, const void* qkv
         SPECV_LAUNCH_CHECK("append_cover_kernel");
     }
     const AppendArgs a{h->geom, (const uint16_t*)qkv, (uint16_t*)rotated, (uint16_t*)h->kv_cache, ld_qkv, ld_rotated, row0, seq_slot, pos0,
-                       h->cos_sin, h->flag, c.n_q_heads, layer, batch, rows, c.max_batch, c.max_kv_len, (int)kv_blocks};
+                       h->cos_sin, h->flag, c.n_q_heads, layer, batch, rows, c.max_batch, c.max_kv_len, (int)kv_blocks,
+                       FastDiv(c.n_q_heads * c.head_dim / 16), FastDiv(c.n_kv_heads)};
     if (c.head_dim == 128) hipLaunchKernelGGL((append_kernel<128>), dim3((unsigned)grid), dim3(TPB), 0, s, a);
     else hipLaunchKernelGGL((append_kernel<64>), dim3((unsigned)grid), dim3(TPB), 0, s, a);
     SPECV_LAUNCH_CHECK("append_kernel");
