@@ -40,7 +40,7 @@ int spec_prompt_rmsnorm(const void* x, int32_t x_dtype, int64_t ld, const float*
  * y = silu(gate) * up. */
 #define SPEC_ACT_NONE 0
 #define SPEC_ACT_RELU 1     /* max(v, 0) */
-#define SPEC_ACT_GELU 2     /* v * (1 + erf(v / sqrt(2))) / 2 */
+#define SPEC_ACT_GELU 2     /* v * (1 + erf(v / sqrt(2))) / 2, off by 5e-7 |v| at most */
 #define SPEC_ACT_SILU 3     /* v / (1 + exp(-v)) */
 #define SPEC_ACT_SWIGLU 4
 typedef struct {
@@ -51,7 +51,8 @@ typedef struct {
     int32_t activation;        /* SPEC_ACT_* */
 } spec_prompt_epilogue;
 /* epilogue NULL: none of it.  workspace: device scratch, 16-byte aligned, through which few rows share K out among workgroups; with less
- * than spec_prompt_gemm_workspace_bytes (0 where that would not pay) they do not (NULL: none).  Calls that overlap in time need their own. */
+ * than spec_prompt_gemm_workspace_bytes (0 where that would not pay) they do so less, or not (NULL: none).  Calls that overlap in time need
+ * their own. */
 size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t activation);
 int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packed, const spec_prompt_epilogue* epilogue, void* y, int32_t y_dtype,
                      int64_t ld_y, int32_t M, int32_t N, int32_t K, void* workspace, size_t workspace_bytes, void* stream);

@@ -289,8 +289,9 @@ def spec_kv_cache_bytes(cfg: spec_model_cfg) -> int:
 class Handle:
     """Owns a spec_handle* and keeps the caller-owned tensors it points into alive."""
 
-    def __init__(self, ptr, cfg, keep):
+    def __init__(self, ptr, cfg, keep, device=None):
         self.ptr, self.cfg, self._keep = ptr, cfg, keep
+        self.device = device    # number of the one that has the cache (None: there is no cache)
 
     def __del__(self):
         try:
@@ -340,7 +341,7 @@ def spec_verify_init(cfg: spec_model_cfg, weights: Optional[dict], kv_cache: Opt
     nbytes = kv_cache.numel() * kv_cache.element_size() if kv_cache is not None else 0
     init = lib().spec_verify_init_paged if paged else lib().spec_verify_init
     _check(init(C.byref(cfg), wp, _ptr(kv_cache), nbytes, _ptr(kv_len, torch.int32), C.byref(out)))
-    return Handle(out.value, cfg, keep)
+    return Handle(out.value, cfg, keep, None if kv_cache is None else kv_cache.get_device())
 
 
 def spec_verify_destroy(h: Handle):
@@ -640,8 +641,11 @@ def spec_prompt_append(h: Handle, layer: int, qkv: torch.Tensor, rotated: torch.
     """Rotary embedding of qkv's queries and keys -> rotated (may be qkv's own first columns); keys and values -> the handle's cache, row j
     of sequence b at position pos0[b] + j (None: j) of slot seq_slot[b]."""
     c = h.cfg
+    raw, device = _place(stream)
+    if h.device is not None and h.device != device:
+        raise ValueError(f"handle: of device {h.device}, the current one is {device}")
     _check(_native().prompt_append(h.ptr, layer, qkv, rotated, row0, seq_slot, pos0, (c.n_q_heads + c.n_kv_heads) * c.head_dim,
-                                   (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, *_place(stream)))
+                                   (c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim, raw, device))
     return rotated
 
 

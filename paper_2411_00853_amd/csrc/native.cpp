@@ -328,7 +328,7 @@ int prompt_append(PyObject* const* a)   // handle, layer, qkv, rotated, row0, se
     if (o.rows != x.rows) throw Bad("rotated: expected " + std::to_string(x.rows) + " rows, got " + std::to_string(o.rows));
     if (row0.dim() != 1 || !row0.size(0)) throw Bad("row0: expected the sequences' first rows and one number more");
     const int64_t batch = row0.size(0) - 1;
-    return lib.prompt_append((spec_handle*)PyLong_AsVoidPtr(a[0]), integer(a[1], "layer"), x.p, x.ld, o.p, o.ld,
+    return lib.prompt_append(a[0] == Py_None ? nullptr : (spec_handle*)PyLong_AsVoidPtr(a[0]), integer(a[1], "layer"), x.p, x.ld, o.p, o.ld,
                              (const int32_t*)shaped(row0, {batch + 1}, I32, "row0"), (const int32_t*)shaped(here(a[5], "seq_slot", a[10]), {batch}, I32, "seq_slot"),
                              (const int32_t*)optional_here(a[6], {batch}, I32, "pos0", a[10]), narrow(batch, "row0"), x.rows, stream_of(a[9]));
 }

@@ -130,8 +130,8 @@ class Rounds:
     """A bf16 target and the Draft8 that proposes to it: `feed` a context, then `round` after round.  Sequence b is slot b of both."""
 
     def __init__(self, target_shape, weights: dict, draft: Draft8, lookahead: int, prompt_rows: int = 0):
-        """weights: as workload.make_weights gives them, on the device.  prompt_rows > 0: `feed` takes contexts of up to so many tokens in all through
-        the target as whole prompts; else window by window."""
+        """weights: as workload.make_weights gives them, on the device.  `feed` takes contexts of up to prompt_rows tokens in all through the
+        target as whole prompts, longer ones window by window."""
         B, V, K, dev = draft.batch, target_shape.vocab, lookahead, draft.embed.device
         self.draft, self.K, self.B = draft, K, B
         cfg = sv.make_cfg(target_shape, B, draft.max_kv_len, K)
@@ -154,7 +154,7 @@ class Rounds:
             d.feed(window, at + t, logits=False)
         self.prev.copy_(context[:, n - 2])
         self.last.copy_(context[:, n - 1])
-        if self.prompt is not None:
+        if self.prompt is not None and self.B * (n - 1) <= self.prompt.max_rows:
             row0 = torch.arange(self.B + 1, dtype=torch.int32, device=context.device) * (n - 1)
             self.prompt.run(context[:, :n - 1].reshape(-1), row0, self.slots, n - 1, logits=False)
             self.kv_len.fill_(n - 1)

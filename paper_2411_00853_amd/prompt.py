@@ -38,6 +38,7 @@ class Prompt:
         self.qkv, self.attn, self.act = new(R, self.d_q + 2 * self.d_kv), new(R, self.d_q), new(R, c.d_ffn)
         self.ends, self.last_x, self.last_h = new(B, dtype=torch.int32), new(B, d, dtype=torch.float32), new(B, d)
         self.logits = new(B, c.vocab, dtype=torch.float32)
+        self.tokens, self.outside = new(R, dtype=torch.int32), new(R, dtype=torch.bool)
         shapes = ((R, self.d_q + 2 * self.d_kv, d, "none"), (R, d, self.d_q, "none"), (R, c.d_ffn, d, "swiglu"), (R, d, c.d_ffn, "none"),
                   (B, c.vocab, d, "none"))
         need = max([sv.spec_prompt_gemm_workspace_bytes(*s) for s in shapes] +
@@ -47,14 +48,19 @@ class Prompt:
     def run(self, tokens: torch.Tensor, row0: torch.Tensor, seq_slot: torch.Tensor, max_len: int = 0, logits: bool = True):
         """tokens int32 [rows]: prompt b is tokens[row0[b]:row0[b+1]], from position 0 of slot seq_slot[b] on (device int32 [batch + 1] and
         [batch]).  Returns fp32 logits [batch][vocab] of this object, behind each prompt's last token (an empty prompt's row means nothing);
-        None with logits=False.  The handle's kv_len is not changed.  max_len: the longest prompt, if known."""
+        None with logits=False.  The handle's kv_len is not changed.  max_len: the longest prompt, if known.  A token outside the vocabulary
+        makes everything behind it in its prompt NaN, the logits too."""
         c, rows, batch = self.handle.cfg, tokens.numel(), seq_slot.numel()
         if not 1 <= rows <= self.max_rows or not 1 <= batch <= self.max_batch:
             raise ValueError(f"{rows} rows of {batch} prompts, at most {self.max_rows} and {self.max_batch}")
         x, h, qkv, attn, act = (t[:rows] for t in (self.x, self.h, self.qkv, self.attn, self.act))
         q, k, v = qkv[:, :self.d_q], qkv[:, self.d_q:self.d_q + self.d_kv], qkv[:, self.d_q + self.d_kv:]
         rotated, scale = qkv[:, :self.d_q + self.d_kv], c.head_dim ** -0.5
-        x.copy_(torch.index_select(self.weights["tok_embed"], 0, tokens, out=self.embedded[:rows]))
+        if tokens.dtype != torch.int32 or tokens.dim() != 1:
+            raise ValueError(f"tokens: expected int32 [rows], got {tokens.dtype} {tuple(tokens.shape)}")
+        inside = torch.clamp(tokens, 0, c.vocab - 1, out=self.tokens[:rows])
+        embedded = torch.index_select(self.weights["tok_embed"], 0, inside, out=self.embedded[:rows])
+        x.copy_(embedded.masked_fill_(torch.ne(tokens, inside, out=self.outside[:rows])[:, None], float("nan")))
         for layer, w in enumerate(self.weights["layers"]):
             sv.spec_prompt_rmsnorm(x, w["attn_norm"], c.rms_eps, h)
             sv.spec_prompt_gemm(h, w["w_qkv"], qkv, workspace=self.work)

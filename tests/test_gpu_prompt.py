@@ -177,3 +177,49 @@ def test_the_binding_refuses(i):
     with pytest.raises(kind, match=match):
         call()
     assert len(calls) == 32
+
+
+def test_tokens_outside_the_vocabulary():
+    """They are told by NaN behind them in their prompt; the others do not notice."""
+    lens = [20, 9, 31]
+    _, h, _, prompt = setup(GROUPED, 3, 96, sum(lens))
+    tokens = wl.Rng(7, "cuda").randint(0, (sum(lens),), GROUPED.vocab)
+    row0, slots = ref.ints(ref.starts(lens)), ref.ints([0, 1, 2])
+    want = prompt.run(tokens, row0, slots).clone()
+    for bad in (-1, GROUPED.vocab, 2 ** 31 - 1, -2 ** 31):
+        tokens[22] = bad
+        got = prompt.run(tokens, row0, slots)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[2], want[2]) and torch.isnan(got[1]).all()
+    with pytest.raises(ValueError, match="tokens: expected int32"):
+        prompt.run(tokens.long(), row0, slots)
+    with pytest.raises(ValueError, match="tokens: expected int32"):
+        prompt.run(tokens[None], row0, slots)
+
+
+def test_contexts_longer_than_the_prompt_buffers_go_window_by_window():
+    from paper_2411_00853_amd.draft8 import Draft8, Rounds
+    batch, K, n = 2, 3, 20
+    w = wl.make_weights(GROUPED, 5, "cuda", std=0.05)
+    rounds = [Rounds(GROUPED, w, Draft8(GROUPED, w, batch, 64, 16), K, prompt_rows=rows) for rows in (0, batch * (n - 1) - 1, batch * (n - 1))]
+    context = wl.Rng(9, "cuda").randint(0, (batch, n), GROUPED.vocab)
+    for r in rounds:
+        r.feed(context)
+        assert r.kv_len.tolist() == [n - 1] * batch and torch.equal(r.last, context[:, n - 1]) and torch.equal(r.prev, context[:, n - 2])
+        r.propose(torch.full((K, batch), 0.5, device="cuda"))
+        r.verify(torch.full((batch, K + 1), 0.5, device="cuda"), 1.0)
+        sv.spec_verify_poll(r.handle)
+    assert torch.equal(rounds[0].out, rounds[1].out)
+
+
+def test_the_handle_of_another_device_is_refused():
+    h, _, _ = ref.handle(1, 4, 2, 64, 3, 96)
+    h.device = 1        # (as if its cache lay there)
+    with pytest.raises(ValueError, match="handle"):
+        sv.spec_prompt_append(h, 0, torch.zeros((10, 512), dtype=BF16, device="cuda"), torch.zeros((10, 384), dtype=BF16, device="cuda"), ref.ints([0, 10]), ref.ints([0]))
+
+
+def test_a_closed_handle_is_refused():
+    h, _, _ = ref.handle(1, 4, 2, 64, 3, 96)
+    h.close()
+    with pytest.raises(sv.SpecError, match="NULL handle"):
+        sv.spec_prompt_append(h, 0, torch.zeros((10, 512), dtype=BF16, device="cuda"), torch.zeros((10, 384), dtype=BF16, device="cuda"), ref.ints([0, 10]), ref.ints([0]))
