@@ -403,13 +403,14 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
 // ---- few rows: the stream of keys and values -----------------------------------------------------------------------------
 //
 // One wavefront takes 32 query rows (those of a kv head's query heads at one position, say).  What bounds it is how much a compute unit has asked
-// for at a time, so blocks are small, 32 positions, and go round in RING places of LDS of which all but one are under way.
-constexpr int FEW = 32, RING = 5;
+// for at a time.  Blocks are small, 32 positions, one in use and one under way, so that five workgroups (heads of 128) and more fit a compute unit:
+// 8 tokens behind 750 to 6000 positions 24.2 us with the join, with five places of LDS for blocks and two workgroups 26.5; one token behind 800 positions 10.4 either way.
+constexpr int FEW = 32;
 template <int HD>
 __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
 {
     constexpr int ROW = 2 * HD, PART = FEW * ROW, U = PART / 1024, PIECES = ROW / 16, ROWS = 1024 / ROW, TILE = 32;
-    __shared__ __attribute__((aligned(16))) char lds[RING * 2 * PART];     // [place][keys, values]
+    __shared__ __attribute__((aligned(16))) char lds[2 * 2 * PART];        // [place][keys, values]
     const int lane = threadIdx.x, r32 = lane & 31, half = lane >> 5;
     const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
     const Tile T = find_tile<TILE>(A, number, false);
@@ -438,7 +439,7 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
             q8_fetch_lds(vp, (uint32_t)from * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn<HD>(r)) * 16, lds0 + slot * (2 * PART) + PART + u * 1024);
         }
     };
-    for (int b = 0; b < min(n_blocks, RING - 1); ++b) fetch(b, b);
+    if (n_blocks) fetch(0, 0);
     const int2 to = place(A, T, r32);
     const int last = to_see + to.x;
     pr_bf16x8 qf[HD / 16];
@@ -451,12 +452,11 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = -INFINITY, l[2] = {0.f, 0.f};
     const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn<HD>(v_row);
-    int slot = 0;
     for (int block = 0; block < n_blocks; ++block) {
-        if (block + RING - 2 < n_blocks) q8_wait_fetches<(RING - 2) * 2 * U>();
-        else q8_wait_fetches<0>();
+        const int slot = block & 1;
+        q8_wait_fetches<0>();
         q8_wait_lds();
-        if (block + RING - 1 < n_blocks) fetch(block + RING - 1, slot == 0 ? RING - 1 : slot - 1);
+        if (block + 1 < n_blocks) fetch(block + 1, 1 - slot);
         char* const keys = lds + slot * (2 * PART);
         char* const values = keys + PART;
         pr_floatx16 s;
@@ -514,7 +514,6 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf, o[d], 0, 0, 0);
             }
         }
-        slot = slot == RING - 1 ? 0 : slot + 1;
     }
     leave<HD, TILE>(A, T, head, r32, half, o, m, both_sum(l[0] + l[1]), last >= 0);
 }
@@ -579,9 +578,10 @@ __global__ void __launch_bounds__(256) join_kernel(Args A)
 }
 
 // How many wavefronts a workgroup has -- as many rows as the sequences have -- and how many blocks of keys: such that all of them together fill the
-// places that the compute units have for workgroups once, at least four, and only if that saves more blocks (some microsecond each) than the
-// join costs.  Sequences differ in length: a tile may have several times as many parts as places allow on average.
-constexpr int MOST_PARTS = 64, LEAST_CHUNK = 4, JOIN_BLOCKS = 8;
+// places that the compute units have for workgroups at most once, and whatever of that takes least.  us: a block, with nothing to wait for but its
+// predecessor (0.8 with heads of 64 and 1.35 of 128, a quarter more by one wavefront), the join's launch (5), the parts' way to memory and back.  Sequences
+// differ in length: a tile may have several times as many parts as places allow on average.
+constexpr int MOST_PARTS = 64;
 struct Plan {
     int waves, parts, chunk;
     int64_t tiles;          // units of a launch, at most
@@ -602,12 +602,17 @@ Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head
     // One sequence: as many parts of each tile as there are places.  Several, of different lengths: the last part of a tile is rarely a whole one, and
     // a few workgroups more than there are places take as long as twice as many.
     const int64_t each = std::max((int64_t)1, places / wgs), spare = std::max(places - wgs, places / 2);
-    int64_t chunk = std::max((int64_t)LEAST_CHUNK, batch == 1 ? (longest + each - 1) / each : (wgs * mean + spare - 1) / spare);
-    p.parts = 1;
-    if (most > 1) {
-        chunk = std::max(chunk, (longest + most - 1) / most);
-        if (longest - chunk > JOIN_BLOCKS) p.parts = (int)((longest + chunk - 1) / chunk);
+    const int64_t least = std::max((int64_t)1, batch == 1 ? (longest + each - 1) / each : (wgs * mean + spare - 1) / spare);
+    const float block = (p.waves == 1 ? 1.25f : 1.f) * (head_dim == 128 ? 1.35f : 0.8f), part = 2.f * (float)wgs * rows * (head_dim + 2) * 4 / 3.5e6f;
+    int64_t chunk = longest;
+    float us = block * (float)longest;
+    for (int64_t n = 2; n <= most; n = n < most ? std::min(most, n + std::max((int64_t)1, n / 4)) : most + 1) {
+        const int64_t c = std::max(least, (longest + n - 1) / n), parts = (longest + c - 1) / c;
+        const float split = block * (float)c + 5.f + part * (float)parts;
+        if (parts > 1 && split < us) us = split, chunk = c;
     }
+    p.parts = (int)((longest + chunk - 1) / std::max((int64_t)1, chunk));
+    if (p.parts < 1) p.parts = 1;
     p.chunk = (int)std::min(chunk, (int64_t)1 << 26);
     p.by_place = p.waves > 1 && batch > 1 && wgs > places;
     return p;
