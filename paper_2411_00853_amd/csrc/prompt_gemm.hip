@@ -4,6 +4,8 @@
 // W is the instruction's first operand: a lane then holds four neighbouring columns of one row of Y, which the epilogue finishes and stores.
 #include "prompt.h"
 
+#include <cfloat>
+
 namespace specv {
 namespace {
 
@@ -462,7 +464,8 @@ void launch_tiled(const Call& c, int splits = 1, int per_split = 0)
 
 // Which tile, and among how many workgroups K is shared out.  us: a stage of 64 columns, with a workgroup on a compute unit and (where two fit) with two
 // on each; measured over K = 4096 and 8192, 48 to 8192 rows, 1024 to 32000 columns.  A launch takes some 3.5 us besides, one whose parts are
-// joined 2.5 us more and the parts' way to memory and back; none is faster than the weights come from memory.
+// joined 2.5 us more and the parts' way to memory and back; none is faster than the weights come from memory.  Gate and up in 32 rows have two
+// wavefronts instead of four (a stage 0.22).
 struct Shape {
     int rows, cols, slots;      // slots: SW, which a part's stages have to exceed
     float us1, us2;             // us2 = 0: one workgroup on a compute unit
@@ -474,13 +477,15 @@ struct Plan {
     size_t floats;                  // of the workspace
 };
 // floats: what the workspace holds
-Plan plan(int M, int n_tiles, int K, size_t floats)
+Plan plan(bool gated, int M, int n_tiles, int K, size_t floats)
 {
     const int stages = (K + 63) / 64;
     Plan best{-1, 1, stages, 0};
-    if (M <= 16) return best;
-    float least = 0.f;
+    // One workgroup for all rows of a column tile (or two) where that is at most one on each compute unit and two turns of its wavefronts: 17 to 32 rows of
+    // K = 2048 by 512 to 4096 columns 4.7 to 6.6 us, in tiles 6.4 to 7.6; 4096 or 6144 columns of K 1.0 to 1.6 times as long as in tiles
+    if (M <= 16 || (M <= 32 && K <= 2048 && n_tiles <= (gated ? 512 : 256))) return best;
     const float stream = (float)((double)n_tiles * 32. * K / 6.2e6);
+    float least = FLT_MAX;
     for (int i = 0; i < (int)(sizeof(SHAPES) / sizeof(SHAPES[0])); ++i) {
         const Shape& t = SHAPES[i];
         const int64_t tiles = (int64_t)((M + t.rows - 1) / t.rows) * ((16 * (int64_t)n_tiles + t.cols - 1) / t.cols);
@@ -492,9 +497,9 @@ Plan plan(int M, int n_tiles, int K, size_t floats)
             if (stages - (splits - 1) * per <= t.slots) continue;
             const int wgs = (int)tiles * splits, at_once = t.us2 ? 512 : 256, whole = wgs / at_once, rest = wgs % at_once;
             const float round = (float)whole * (t.us2 ? t.us2 : t.us1) + (rest == 0 ? 0.f : rest <= 256 ? t.us1 : t.us2);
-            const float work = round * per, join = splits > 1 ? 2.5f + (float)need * 8e-6f / 5.f : 0.f;
+            const float work = round * per * (gated && t.rows == 32 ? 1.16f : 1.f), join = splits > 1 ? 2.5f + (float)need * 8e-6f / 5.f : 0.f;
             const float us = std::max(work, stream) + 0.1f * work + join;
-            if (best.shape < 0 || us < least) {
+            if (us < least) {
                 least = us;
                 best = {i, splits, per, need};
             }
@@ -506,7 +511,7 @@ Plan plan(int M, int n_tiles, int K, size_t floats)
 template <bool GATED>
 void launch(const Call& c)
 {
-    const Plan p = plan(c.M, c.n_tiles, c.K, c.partial_floats);
+    const Plan p = plan(GATED, c.M, c.n_tiles, c.K, c.partial_floats);
     switch (p.shape) {
     case 0: return launch_tiled<GATED, 2, 4, 8, 4, 2, 3, 1>(c, p.splits, p.per_split);
     case 1: return launch_tiled<GATED, 4, 2, 4, 4, 3, 3, 3>(c, p.splits, p.per_split);
@@ -520,7 +525,8 @@ void launch(const Call& c)
             else return launch_tiled<GATED, 1, 2, 2, 2, 4, 5, 1>(c, p.splits, p.per_split);
     }
     // (one row of 4096 x 4096: 6.8 us, 8.2 with two column tiles and eight wavefronts; 8 rows of 32000 x 4096 42.6 with one tile and four, 39.3 with two)
-    if (c.M > 16) launch_skinny<GATED, GATED ? 2 : 4, GATED ? 2 : 1, 8>(c);
+    if (c.M > 32) launch_skinny<GATED, GATED ? 2 : 4, GATED ? 2 : 1, 8>(c);
+    else if (c.M > 16) launch_skinny<GATED, 2, GATED ? 2 : 1, 8>(c);
     else if (c.n_tiles >= 1024) launch_skinny<GATED, 1, 2, 4>(c);
     else launch_skinny<GATED, 1, GATED ? 2 : 1, 8>(c);
 }
@@ -533,7 +539,7 @@ using namespace specv;
 extern "C" size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t activation)
 {
     if (M <= 0 || N <= 0 || K <= 0 || M > MAX_ROWS || N > MAX_COLS || K > SPEC_PROMPT_MAX_LD) return 0;
-    return 4 * plan(M, ((activation == SPEC_ACT_SWIGLU ? 2 * N : N) + 15) / 16, K, MOST_PARTS).floats;
+    return 4 * plan(activation == SPEC_ACT_SWIGLU, M, ((activation == SPEC_ACT_SWIGLU ? 2 * N : N) + 15) / 16, K, MOST_PARTS).floats;
 }
 
 extern "C" int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packed, const spec_prompt_epilogue* epilogue, void* y, int32_t y_dtype,

@@ -125,3 +125,22 @@ def test_calls_at_once_on_two_streams():
     torch.cuda.synchronize()
     assert all(torch.equal(t.double(), want) for ys in y for t in ys)
     assert all(torch.equal(t, o[0][0]) for os in o for t in os) and close(o[0][0], q, k, v, hk, [2], [9000])
+
+
+@pytest.mark.parametrize("act", ("none", "swiglu"))
+@pytest.mark.parametrize("M", (17, 31, 32, 33))
+@pytest.mark.parametrize("N,K", [(4096, 2048), (4112, 2048), (4096, 2080), (48, 1056), (4080, 32)])
+def test_products_at_the_edge_between_the_kernels(act, M, N, K):
+    x, w = ref.small_ints(1, M, K), ref.small_ints(2, N if act == "none" else 2 * N, K)
+    y = torch.full((M, N), 7.0, device="cuda")
+    ws = torch.full((max(16, sv.spec_prompt_gemm_workspace_bytes(M, N, K, act)),), 255, dtype=torch.uint8, device="cuda")
+    sv.spec_prompt_gemm(x, ref.pack(w, act == "swiglu"), y, activation=act, workspace=ws)
+    want = ref.product(x, w, act=act)
+    if act == "none":
+        assert torch.equal(y.double(), want)
+    else:
+        # Both products are exact, gate g and up.  exp(-g) = 2^t with t = g * -1.44269504: that constant is off by less than 2^-25 of it, the product by
+        # 2^-24, so t by |g| 1.4427 * 1.5 * 2^-24 and 2^t by |g| 1.5 * 2^-24 of itself, which is less than |g| 2^-23; where g is negative the result is off
+        # by as much.  The exponential, the sum, the reciprocal and two products: some 2^-20.  Below 2^-126 the reciprocal is zero: 90 * 2^-126 * 2^17 < 1e-30.
+        gate = ref.product(x, w[:N])
+        assert torch.all((y.double() - want).abs() <= want.abs() * (2.0 ** -20 + gate.abs() * 2.0 ** -23) + 1e-30)
