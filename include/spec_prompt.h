@@ -41,7 +41,7 @@ int spec_prompt_rmsnorm(const void* x, int32_t x_dtype, int64_t ld, const float*
 #define SPEC_ACT_NONE 0
 #define SPEC_ACT_RELU 1     /* max(v, 0) */
 #define SPEC_ACT_GELU 2     /* v * (1 + erf(v / sqrt(2))) / 2, off by 5e-7 |v| at most */
-#define SPEC_ACT_SILU 3     /* v / (1 + exp(-v)) */
+#define SPEC_ACT_SILU 3     /* v / (1 + exp(-v)); off by (2^-20 + |v| 2^-23) of itself, or 1e-30, at most */
 #define SPEC_ACT_SWIGLU 4
 typedef struct {
     const float* bias;         /* device fp32[N] (SPEC_ACT_SWIGLU: [2 N], gate then up), or NULL */

@@ -36,7 +36,8 @@ __device__ __forceinline__ float wave_max(float v)
 }
 
 // W wavefronts take a row (W < 4: a workgroup takes 4 / W rows); a thread holds NV vectors of eight columns in registers between the sum of
-// squares and the product with the gain.
+// squares and the product with the gain, so the row is read once.  As many wavefronts as give a thread one vector, up to sixteen: all of a row is asked
+// for at once.  4096 rows of 4096 fp32 20.7 us, 4.9 TB/s (a copy's rate is 5.1); one row of 2048 2.5 us on the GPU.
 template <typename T, int W, int NV>
 __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) rmsnorm_kernel(const T* __restrict__ x, const float* __restrict__ gain, uint16_t* __restrict__ y, int64_t ld, int rows,
                                                        int cols, float eps)
@@ -199,7 +200,8 @@ __device__ __forceinline__ void rotate8(pr_uintx4& a, pr_uintx4& b, const float*
 }
 
 // The first kv_blocks * n_kv_heads workgroups take one head of 32 positions of a sequence, as the cache has them in one block; the others 16
-// rows' queries, 256 pairs of sixteen bytes at a time.
+// rows' queries, 256 pairs of sixteen bytes at a time.  Memory bounds it: 6020 rows of 32 query and 32 kv heads of 128 82 us, 4.2 TB/s (a copy 5.1); with four pairs
+// of a thread asked for at once 81, and a prompt of 37 rows 6.3 us instead of 5.2.
 template <int HD>
 __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
 {
