@@ -408,14 +408,15 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
 // ---- few rows: the stream of keys and values -----------------------------------------------------------------------------
 //
 // One wavefront takes 32 query rows (those of a kv head's query heads at one position, say).  What bounds it is how much a compute unit has asked
-// for at a time.  Blocks are small, 32 positions, one in use and one under way, so that five workgroups (heads of 128) and more fit a compute unit:
-// 8 tokens behind 750 to 6000 positions 24.2 us with the join, with five places of LDS for blocks and two workgroups 26.5; one token behind 800 positions 10.4 either way.
-constexpr int FEW = 32;
+// for at a time, so blocks are small, 32 positions, and go round in RING places of LDS of which all but one are under way.  More places leave room for
+// fewer workgroups: 8 tokens behind 750 to 6000 positions, keys and values from memory, with the join 37, 35.6, 34.6, 35 us with 2, 3, 4, 5 places; from the card's
+// last cache 24.2, 24.9, 25.8, 26.5; 64 behind 500 18.0, 16.4, 16.9, 17.4.
+constexpr int FEW = 32, RING = 3;
 template <int HD>
 __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
 {
     constexpr int ROW = 2 * HD, PART = FEW * ROW, U = PART / 1024, PIECES = ROW / 16, ROWS = 1024 / ROW, TILE = 32;
-    __shared__ __attribute__((aligned(16))) char lds[2 * 2 * PART];        // [place][keys, values]
+    __shared__ __attribute__((aligned(16))) char lds[RING * 2 * PART];     // [place][keys, values]
     const int lane = threadIdx.x, r32 = lane & 31, half = lane >> 5;
     const int job = A.heads.div(blockIdx.x), head = (int)blockIdx.x - job * (int)A.heads.d, number = A.parts.div(job), part = job - number * (int)A.parts.d;
     const Tile T = find_tile<TILE>(A, number, false);
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
             q8_fetch_lds(vp, (uint32_t)from * (uint32_t)(2 * A.ld_v) + (lane % PIECES ^ value_turn<HD>(r)) * 16, lds0 + slot * (2 * PART) + PART + u * 1024);
         }
     };
-    if (n_blocks) fetch(0, 0);
+    for (int b = 0; b < min(n_blocks, RING - 1); ++b) fetch(b, b);
     const int2 to = place(A, T, r32);
     const int last = to_see + to.x;
     pr_bf16x8 qf[HD / 16];
@@ -457,11 +458,12 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
     float m = -INFINITY, l[2] = {0.f, 0.f};
     const int v_row = 4 * half + ((lane & 15) >> 2), v_turn = value_turn<HD>(v_row);
+    int slot = 0;
     for (int block = 0; block < n_blocks; ++block) {
-        const int slot = block & 1;
-        q8_wait_fetches<0>();
+        if (block + RING - 2 < n_blocks) q8_wait_fetches<(RING - 2) * 2 * U>();
+        else q8_wait_fetches<0>();
         q8_wait_lds();
-        if (block + 1 < n_blocks) fetch(block + 1, 1 - slot);
+        if (block + RING - 1 < n_blocks) fetch(block + RING - 1, slot == 0 ? RING - 1 : slot - 1);
         char* const keys = lds + slot * (2 * PART);
         char* const values = keys + PART;
         pr_floatx16 s;
@@ -519,6 +521,7 @@ __global__ void __launch_bounds__(64, 1) few_kernel(Args A)
                 o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf.f, pf, o[d], 0, 0, 0);
             }
         }
+        slot = slot == RING - 1 ? 0 : slot + 1;
     }
     leave<HD, TILE>(A, T, head, r32, half, o, m, both_sum(l[0] + l[1]), last >= 0);
 }
@@ -602,7 +605,9 @@ Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head
     p.tiles = (int64_t)q_rows * group / rows + batch;
     p.part_bytes = (size_t)p.tiles * n_kv_heads * rows * (head_dim + 2) * 4;
     const int64_t wgs = std::min(p.tiles, std::max((int64_t)batch, ((int64_t)q_rows * group + rows - 1) / rows)) * n_kv_heads;
-    const int64_t places = 256 * (head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
+    // (one wavefront: three workgroups of heads of 128 fit a compute unit, but places for four do better than for three or two -- 16 tokens behind up to 4000
+    // 45.7, 52, 46.5 us, 8 behind 6000 35.5, 35.4, 37.4 -- as shorter parts follow the ones that end first)
+    const int64_t places = 256 * (p.waves == 1 ? 4 : head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
     const int64_t longest = (k_len + BLK - 1) / BLK, mean = std::min(longest, (int64_t)k_rows / batch / BLK + 1);
     const int64_t most = std::min((int64_t)MOST_PARTS, 4 / p.waves * places / wgs);
     // One sequence: as many parts of each tile as there are places.  Several, of different lengths: the last part of a tile is rarely a whole one, and
