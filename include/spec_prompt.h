@@ -24,6 +24,7 @@ extern "C" {
 #endif
 
 #define SPEC_PROMPT_MAX_COLS 65536       /* widest row of spec_prompt_rmsnorm */
+#define SPEC_PROMPT_MAX_ROWS (1 << 20)   /* of spec_prompt_rmsnorm and spec_prompt_gemm, at most */
 #define SPEC_PROMPT_MAX_LD (1 << 22)     /* elements from a row to the next, at most */
 #define SPEC_PROMPT_MAX_SEQS 65536
 

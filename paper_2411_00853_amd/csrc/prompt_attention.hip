@@ -689,6 +689,8 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     Plan p = plan(a.q_rows, a.k_rows, a.batch, a.n_kv_heads, group, a.head_dim, q_len, k_len);
     if (p.parts > 1) p.parts = workspace ? (int)std::min((size_t)p.parts, workspace_bytes / p.part_bytes) : 1;
     if (p.parts < 1) p.parts = 1;
+    const int64_t units = p.tiles * a.n_kv_heads, threads = std::max(units * p.parts * 64 * p.waves, p.parts > 1 ? units * p.waves * a.head_dim * 16 : 0);
+    if (threads > UINT32_MAX) return fail(SPEC_ERR_SHAPE, "spec_prompt_attention: %d query rows of %d sequences are too many for a launch", a.q_rows, a.batch);
     float* const ws = (float*)workspace;
     const size_t rows = p.part_bytes / (a.head_dim + 2) / 4 * p.parts;
     const Args g{(const uint16_t*)a.q, (const uint16_t*)a.k, (const uint16_t*)a.v, (uint16_t*)a.out, a.ld_q, a.ld_k, a.ld_v, a.ld_out, a.q_row0,

@@ -163,7 +163,7 @@ __device__ __forceinline__ pr_floatx4 mfma(pr_bf16x8 w, pr_bf16x8 x, pr_floatx4 
 
 constexpr int TILE = 1024;   // bytes of a 16 x 32 tile of W
 constexpr int PANEL = 8;     // row blocks of a panel
-constexpr int MAX_ROWS = 1 << 20, MAX_COLS = 1 << 23;
+constexpr int MAX_COLS = 1 << 23;
 constexpr size_t MOST_PARTS = (size_t)1 << 25;   // floats of a workspace that is asked for: where parts pay, they are few
 
 // ---- many rows: the matrix cores ----------------------------------------------------------------------------------------
@@ -538,7 +538,7 @@ using namespace specv;
 
 extern "C" size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t activation)
 {
-    if (M <= 0 || N <= 0 || K <= 0 || M > MAX_ROWS || N > MAX_COLS || K > SPEC_PROMPT_MAX_LD) return 0;
+    if (M <= 0 || N <= 0 || K <= 0 || M > SPEC_PROMPT_MAX_ROWS || N > MAX_COLS || K > SPEC_PROMPT_MAX_LD) return 0;
     return 4 * plan(activation == SPEC_ACT_SWIGLU, M, ((activation == SPEC_ACT_SWIGLU ? 2 * N : N) + 15) / 16, K, MOST_PARTS).floats;
 }
 
@@ -577,7 +577,7 @@ extern "C" int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packe
                        (!e.residual || (e.ld_residual % 4 == 0 && (uintptr_t)e.residual % (4 * rs) == 0));
     const Call c{(const uint16_t*)x, (const uint8_t*)w_packed, ld_x, M, K, n_tiles,
                  Out{y, e.bias, e.residual, ld_y, e.ld_residual, e.residual_dtype, y_dtype, e.activation, N, whole}, (hipStream_t)stream, (float*)workspace, workspace ? std::min(workspace_bytes / 4, MOST_PARTS) : 0};
-    if ((int64_t)((M + 15) / 16) * n_tiles > (int64_t)1 << 30 || M > MAX_ROWS)
+    if ((int64_t)((M + 15) / 16) * n_tiles > (int64_t)1 << 30 || M > SPEC_PROMPT_MAX_ROWS)
         return fail(SPEC_ERR_SHAPE, "spec_prompt_gemm: %d rows of %d columns are too many", M, N);
     if (swiglu) launch<true>(c);
     else launch<false>(c);

@@ -321,6 +321,7 @@ extern "C" int spec_prompt_rmsnorm(const void* x, int32_t x_dtype, int64_t ld, c
 {
     if (rows < 0 || cols <= 0) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_rmsnorm: %d rows of %d columns", rows, cols);
     if (cols > SPEC_PROMPT_MAX_COLS) return fail(SPEC_ERR_SHAPE, "spec_prompt_rmsnorm: %d columns, at most %d", cols, SPEC_PROMPT_MAX_COLS);
+    if (rows > SPEC_PROMPT_MAX_ROWS) return fail(SPEC_ERR_SHAPE, "spec_prompt_rmsnorm: %d rows, at most %d", rows, SPEC_PROMPT_MAX_ROWS);
     if (!q8_dtype(x_dtype)) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_rmsnorm: unknown type %d", x_dtype);
     if (ld < cols) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_rmsnorm: rows of %d columns are %lld elements apart", cols, (long long)ld);
     if (!(eps >= 0.f)) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_rmsnorm: eps %g", (double)eps);
@@ -353,7 +354,7 @@ extern "C" int spec_prompt_append(spec_handle* h, int32_t layer, const void* qkv
     if (qkv == rotated && ld_qkv != ld_rotated) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: in place with two different lds");
     const int64_t kv_blocks = std::min((int64_t)rows / 32 + 2 * (int64_t)batch, (int64_t)rows);   // a sequence of n rows reaches n / 32 + 2 blocks, and n at most
     const int64_t grid = kv_blocks * c.n_kv_heads + (rows + 15) / 16;
-    if (grid > 0x7fffffff) return fail(SPEC_ERR_SHAPE, "spec_prompt_append: %d rows are too many", rows);
+    if (grid * TPB > UINT32_MAX) return fail(SPEC_ERR_SHAPE, "spec_prompt_append: %d rows are too many", rows);
     hipStream_t s = (hipStream_t)stream;
     if (h->tables.pool.table) {
         hipLaunchKernelGGL(append_cover_kernel, dim3((batch + 63) / 64), dim3(64), 0, s, h->tables.pool, row0, seq_slot, pos0, batch, rows,

@@ -25,7 +25,7 @@ def pack_weights(weights: dict) -> dict:
 
 class Prompt:
     """The pass of prompts of up to max_rows tokens in all, max_batch of them at most.  weights: those the handle was made with
-    (pack_weights).  Device memory is allocated in __init__ alone, so `run` can be captured into a HIP graph."""
+    (pack_weights).  Device memory is allocated in __init__ alone, so `run` can be captured into a HIP graph; it is that of one run at a time."""
 
     def __init__(self, handle: sv.Handle, weights: dict, max_rows: int, max_batch: Optional[int] = None):
         c = handle.cfg
@@ -47,7 +47,7 @@ class Prompt:
 
     def run(self, tokens: torch.Tensor, row0: torch.Tensor, seq_slot: torch.Tensor, max_len: int = 0, logits: bool = True):
         """tokens int32 [rows]: prompt b is tokens[row0[b]:row0[b+1]], from position 0 of slot seq_slot[b] on (device int32 [batch + 1] and
-        [batch]).  Returns fp32 logits [batch][vocab] of this object, behind each prompt's last token (an empty prompt's row means nothing);
+        [batch]; no slot twice).  Returns fp32 logits [batch][vocab] of this object, behind each prompt's last token (an empty prompt's row means nothing);
         None with logits=False.  The handle's kv_len is not changed.  max_len: the longest prompt, if known.  A token outside the vocabulary
         makes everything behind it in its prompt NaN, the logits too."""
         c, rows, batch = self.handle.cfg, tokens.numel(), seq_slot.numel()

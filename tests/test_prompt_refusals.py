@@ -31,6 +31,7 @@ def test_norm(lib):
     refused(call(rows=-1), INVALID, lib, "rows")
     refused(call(cols=0), INVALID, lib, "columns")
     refused(call(cols=65537, ld=70000), SHAPE, lib, "65537")
+    refused(call(rows=(1 << 20) + 1), SHAPE, lib, "rows")
     for eps in (-1.0, NAN):
         refused(call(eps=eps), INVALID, lib, "eps")
     assert call(rows=0, x=None, gain=None, y=None) == 0
@@ -103,5 +104,6 @@ def test_attention(lib):
         refused(call(**{k: 516}), INVALID, lib, "apart")
         refused(call(**{k: (1 << 22) + 8}), INVALID, lib, "apart")
     refused(call(q_rows=1 << 30), SHAPE, lib, "too many")
+    refused(call(n_q_heads=1024, n_kv_heads=1024, batch=65536, ld_q=65536, ld_k=65536, ld_v=65536, ld_out=65536), SHAPE, lib, "too many")
     assert call(q_rows=0) == 0 and call(batch=0) == 0
     assert lib.spec_prompt_attention_workspace_bytes(0, 1, 8, 2, 64) == 0 and lib.spec_prompt_attention_workspace_bytes(4, 1, 8, 3, 64) == 0
