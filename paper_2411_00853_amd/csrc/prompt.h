@@ -20,6 +20,15 @@ __device__ __forceinline__ unsigned pr_pack2(float a, float b)
     return __builtin_bit_cast(unsigned, v);
 }
 
+// Sixteen bytes, at any even address, of an output as long as a prompt: past the L2s, which then keep what is read.  The norm of 4096 x 4096 fp32 (operands
+// from memory) 24.6 -> 19.6 us, of bf16 rows 20.8 -> 15.5, the rotary embedding of 6020 rows 84.4 -> 80; a pass of 3328 tokens, whose next kernel
+// reads them, takes the same 41 ms.
+__device__ __forceinline__ void pr_stream(void* to, const pr_uintx4& v)
+{
+    typedef pr_uintx4 __attribute__((aligned(2))) Any;
+    __builtin_nontemporal_store(v, (Any*)to);
+}
+
 // Rows [begin, end) of sequence b, cut to [0, rows)
 struct PromptSpan {
     int begin, end;

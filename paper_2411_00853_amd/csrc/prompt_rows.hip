@@ -37,7 +37,7 @@ __device__ __forceinline__ float wave_max(float v)
 
 // W wavefronts take a row (W < 4: a workgroup takes 4 / W rows); a thread holds NV vectors of eight columns in registers between the sum of
 // squares and the product with the gain, so the row is read once.  As many wavefronts as give a thread one vector, up to sixteen: all of a row is asked
-// for at once.  4096 rows of 4096 fp32 20.7 us, 4.9 TB/s (a copy's rate is 5.1); one row of 2048 2.5 us on the GPU.
+// for at once.  4096 rows of 4096 fp32 19.6 us, 5.1 TB/s (a copy's rate); one row of 2048 2.5 us on the GPU.
 template <typename T, int W, int NV>
 __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) rmsnorm_kernel(const T* __restrict__ x, const float* __restrict__ gain, uint16_t* __restrict__ y, int64_t ld, int rows,
                                                        int cols, float eps)
@@ -104,15 +104,15 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) rmsnorm_kernel(const T* 
         const int col = (k * 64 * W + sub) * 8;
         if (col >= cols) continue;
         if (!EARLY) load_cols(gain, col, cols, g[0]);
-        Q8Eight<uint16_t> o;
+        float o[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o.v[i] = q8_round_bf16(h[k][i] * r * g[EARLY ? k : 0][i]);
+        for (int i = 0; i < 8; ++i) o[i] = h[k][i] * r * g[EARLY ? k : 0][i];
         if (col + 8 <= cols) {
-            *reinterpret_cast<Q8Eight<uint16_t>*>(yr + col) = o;
+            pr_stream(yr + col, (pr_uintx4){pr_pack2(o[0], o[1]), pr_pack2(o[2], o[3]), pr_pack2(o[4], o[5]), pr_pack2(o[6], o[7])});
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (col + i < cols) yr[col + i] = o.v[i];
+                if (col + i < cols) yr[col + i] = q8_round_bf16(o[i]);
         }
     }
 }
@@ -200,8 +200,8 @@ __device__ __forceinline__ void rotate8(pr_uintx4& a, pr_uintx4& b, const float*
 }
 
 // The first kv_blocks * n_kv_heads workgroups take one head of 32 positions of a sequence, as the cache has them in one block; the others 16
-// rows' queries, 256 pairs of sixteen bytes at a time.  Memory bounds it: 6020 rows of 32 query and 32 kv heads of 128 82 us, 4.2 TB/s (a copy 5.1); with four pairs
-// of a thread asked for at once 81, and a prompt of 37 rows 6.3 us instead of 5.2.
+// rows' queries, 256 pairs of sixteen bytes at a time.  Memory bounds it: 6020 rows of 32 query and 32 kv heads of 128 80 us, 4.3 TB/s (a copy 5.1); four pairs
+// of a thread asked for at once take 1 us off that, and a prompt of 37 rows then takes 6.3 us instead of 5.2.
 template <int HD>
 __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
 {
@@ -237,11 +237,11 @@ __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
             if (s.ok) rotate8(a, b, A.cos_sin + (size_t)(base + t) * HD + 16 * p);
             else a = b = (pr_uintx4){0, 0, 0, 0};
             uint16_t* dst = A.rotated + row * A.ld_rot + (size_t)(A.n_q_heads + head) * HD + 8 * p;
-            *reinterpret_cast<pr_uintx4*>(dst) = a;
-            *reinterpret_cast<pr_uintx4*>(dst + HD / 2) = b;
+            pr_stream(dst, a);
+            pr_stream(dst + HD / 2, b);
             if (kc) {
-                *reinterpret_cast<pr_uintx4*>(kc + tiled_k_within(HD, t, 8 * p)) = a;
-                *reinterpret_cast<pr_uintx4*>(kc + tiled_k_within(HD, t, 8 * p + HD / 2)) = b;
+                pr_stream(kc + tiled_k_within(HD, t, 8 * p), a);
+                pr_stream(kc + tiled_k_within(HD, t, 8 * p + HD / 2), b);
             }
         }
         if (!kc) return;
@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
             if (lo == 0 && hi == 32) {
                 pr_uintx4 v;
                 __builtin_memcpy(&v, e8, 16);
-                *reinterpret_cast<pr_uintx4*>(dst) = v;
+                pr_stream(dst, v);
             } else {   // the block's other positions may hold entries: only these are written
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -306,8 +306,8 @@ __global__ void __launch_bounds__(TPB) append_kernel(AppendArgs A)
         if (at >= 0) rotate8(a, b, A.cos_sin + (size_t)at * HD + 2 * c);
         else a = b = (pr_uintx4){0, 0, 0, 0};
         uint16_t* dst = A.rotated + row * A.ld_rot + (size_t)head * HD + c;
-        *reinterpret_cast<pr_uintx4*>(dst) = a;
-        *reinterpret_cast<pr_uintx4*>(dst + HD / 2) = b;
+        pr_stream(dst, a);
+        pr_stream(dst + HD / 2, b);
     }
 }
 
