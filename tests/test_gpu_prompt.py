@@ -223,3 +223,20 @@ def test_a_closed_handle_is_refused():
     h.close()
     with pytest.raises(sv.SpecError, match="NULL handle"):
         sv.spec_prompt_append(h, 0, torch.zeros((10, 512), dtype=BF16, device="cuda"), torch.zeros((10, 384), dtype=BF16, device="cuda"), ref.ints([0, 10]), ref.ints([0]))
+
+
+def test_rows_behind_the_last_prompt():
+    """A padded batch: the rows behind the last prompt, and prompts without rows, change nothing but the tiles that the number of rows chooses."""
+    lens = [40, 0, 33]
+    rows = sum(lens)
+    _, h, _, prompt = setup(GROUPED, 3, 96, rows + 30)
+    for buffer in (prompt.x, prompt.h, prompt.qkv, prompt.attn, prompt.act):
+        buffer.fill_(float("nan"))
+    tokens = wl.Rng(7, "cuda").randint(0, (rows,), GROUPED.vocab)
+    padded = torch.cat((tokens, torch.zeros(30, dtype=torch.int32, device="cuda")))
+    row0, slots = ref.ints(ref.starts(lens)), ref.ints([0, 1, 2])
+    got = prompt.run(padded, row0, slots).clone()
+    want = prompt.run(tokens, row0, slots)
+    for b in (0, 2):
+        assert torch.isfinite(got[b]).all() and rms(got[b] - want[b]) < 0.01 * rms(want[b])
+    sv.spec_verify_poll(h)
