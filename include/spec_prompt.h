@@ -85,7 +85,7 @@ typedef struct {
     const void *q, *k, *v;
     int64_t ld_q, ld_k, ld_v, ld_out;
     const int32_t* q_row0;     /* device int32[batch+1] */
-    const int32_t* k_row0;     /* device int32[batch+1], or NULL: q_row0 */
+    const int32_t* k_row0;     /* device int32[batch+1], or NULL: q_row0 (k_rows is then q_rows) */
     int32_t n_q_heads, n_kv_heads, head_dim;
     int32_t batch, q_rows, k_rows;
     int32_t max_q_len, max_k_len;

@@ -684,6 +684,9 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     const int group = a.n_q_heads / a.n_kv_heads;
     if ((int64_t)a.q_rows * group > 0x3fffffff || ((int64_t)a.q_rows * group / 32 + a.batch) * a.n_kv_heads * 16 > 0x7fffffff)
         return fail(SPEC_ERR_SHAPE, "spec_prompt_attention: %d query rows are too many", a.q_rows);
+    // (q_row0 is cut to the query rows, whatever it is read for)
+    if (!a.k_row0 && a.k_rows != a.q_rows)
+        return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_attention: %d query rows, %d key rows and no k_row0", a.q_rows, a.k_rows);
     // lengths that are not known: all rows are of one sequence, or of as many as there are, whichever gives more workgroups
     const int64_t q_len = a.max_q_len ? a.max_q_len : a.q_rows, k_len = a.max_k_len ? a.max_k_len : a.k_rows;
     Plan p = plan(a.q_rows, a.k_rows, a.batch, a.n_kv_heads, group, a.head_dim, q_len, k_len);
