@@ -62,7 +62,7 @@ int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packed, const sp
  * qkv: bf16 [rows][(n_q_heads + 2 n_kv_heads) * head_dim] of the handle's model: query heads, key heads, value heads; rows ld_qkv elements apart.
  * Row row0[b] + j is at position pos0[b] + j (pos0 NULL: j) of slot seq_slot[b] (device int32[batch] both).
  * rotated: bf16 [rows][(n_q_heads + n_kv_heads) * head_dim], rows ld_rotated elements apart: the queries and keys, rotated in fp32 and rounded
- * once; the same keys, and the values, go to the cache.  rotated may be qkv with its ld: they are then rotated in place.
+ * once; the same keys, and the values, go to the cache.  rotated may be qkv with its ld (one row: any): they are then rotated in place.
  * kv_len is neither read nor changed: the caller sets it once all layers are in.  A sequence whose slot is outside [0, max_batch), or
  * whose positions leave [0, max_kv_len), is not written to the cache, its rotated rows are zero and spec_verify_poll reports
  * it (SPEC_ERR_INVALID_ARG, SPEC_ERR_KV_OVERFLOW).  A paged cache takes the pages that it lacks up to the last new position; where the

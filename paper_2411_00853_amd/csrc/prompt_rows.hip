@@ -351,7 +351,7 @@ extern "C" int spec_prompt_append(spec_handle* h, int32_t layer, const void* qkv
                     (long long)ld_qkv, (long long)ld_rotated, (long long)cols, (long long)rot, SPEC_PROMPT_MAX_LD);
     if (((uintptr_t)qkv | (uintptr_t)rotated | (uintptr_t)h->kv_cache) & 15)
         return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: qkv, rotated and the cache have to be 16-byte aligned");
-    if (qkv == rotated && ld_qkv != ld_rotated) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: in place with two different lds");
+    if (qkv == rotated && rows > 1 && ld_qkv != ld_rotated) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: in place with two different lds");
     const int64_t kv_blocks = std::min((int64_t)rows / 32 + 2 * (int64_t)batch, (int64_t)rows);   // a sequence of n rows reaches n / 32 + 2 blocks, and n at most
     const int64_t grid = kv_blocks * c.n_kv_heads + (rows + 15) / 16;
     if (grid * TPB > UINT32_MAX) return fail(SPEC_ERR_SHAPE, "spec_prompt_append: %d rows are too many", rows);
