@@ -71,12 +71,14 @@ __global__ void __launch_bounds__(W < 4 ? 256 : 64 * W) rmsnorm_kernel(const T* 
     };
     auto add = [](float a, float b) { return a + b; };
     ss = all(ss, wave_sum, add);
-    float r = 1.f / sqrtf(ss / (float)cols + eps);
-    // Squares that leave fp32's range: the row over a power of two near its largest number has others.  (The barriers are the workgroup's:
-    // where some row of it needs this, all do it, the others with the power 1.)
-    const bool odd = !(ss <= 0x1.fffffep127f) || (eps == 0.f && ss < 0x1p-80f);
+    const float mean = ss / (float)cols + eps;
+    float r = 1.f / sqrtf(mean);
+    // Squares that leave fp32's range, and an eps beside which such squares count: the row over a power of two near its largest number, or eps's root if that is
+    // larger, has others.  (Squares below 2^-126 lose bits; beside a sum of 2^-100 those do not count.  The barriers are the workgroup's: where some
+    // row of it needs this, all do it, the others with the power 1.)
+    const bool odd = !(ss <= 0x1.fffffep127f) || mean < 0x1p-100f;
     if (W == 1 ? (bool)__any(odd) : (bool)__syncthreads_or(odd)) {
-        float top = 0.f;
+        float top = sqrtf(eps);
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
