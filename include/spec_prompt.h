@@ -55,6 +55,8 @@ typedef struct {
  * than spec_prompt_gemm_workspace_bytes (0 where that would not pay) they do so less, or not (NULL: none).  Calls that overlap in time need
  * their own. */
 size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K, int32_t activation);
+/* The most of that over all numbers of rows up to M (many rows need none where few do): for a workspace that calls of different M use. */
+size_t spec_prompt_gemm_workspace_bytes_up_to(int32_t M, int32_t N, int32_t K, int32_t activation);
 int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packed, const spec_prompt_epilogue* epilogue, void* y, int32_t y_dtype,
                      int64_t ld_y, int32_t M, int32_t N, int32_t K, void* workspace, size_t workspace_bytes, void* stream);
 
@@ -93,6 +95,8 @@ typedef struct {
     void* out;
 } spec_prompt_attn_args;
 size_t spec_prompt_attention_workspace_bytes(int32_t q_rows, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
+/* At least that for any numbers of rows and sequences up to these; 2^20 (head_dim + 2) bytes at most. */
+size_t spec_prompt_attention_workspace_bytes_up_to(int32_t q_rows, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
 int spec_prompt_attention(const spec_prompt_attn_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus

@@ -218,12 +218,14 @@ def lib():
         L.spec_filter_workspace_bytes.argtypes = [i32, i32]
         L.spec_filter_sample.argtypes = [C.POINTER(spec_filter_args), C.POINTER(spec_filter_out), ptr, C.c_size_t, ptr]
         L.spec_prompt_rmsnorm.argtypes = [ptr, i32, i64, ptr, f32, i32, i32, ptr, ptr]
-        L.spec_prompt_gemm_workspace_bytes.restype = C.c_size_t
-        L.spec_prompt_gemm_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        for f in (L.spec_prompt_gemm_workspace_bytes, L.spec_prompt_gemm_workspace_bytes_up_to):
+            f.restype = C.c_size_t
+            f.argtypes = [i32, i32, i32, i32]
         L.spec_prompt_gemm.argtypes = [ptr, i64, ptr, C.POINTER(spec_prompt_epilogue), ptr, i32, i64, i32, i32, i32, ptr, C.c_size_t, ptr]
         L.spec_prompt_append.argtypes = [ptr, i32, ptr, i64, ptr, i64, ptr, ptr, ptr, i32, i32, ptr]
-        L.spec_prompt_attention_workspace_bytes.restype = C.c_size_t
-        L.spec_prompt_attention_workspace_bytes.argtypes = [i32, i32, i32, i32, i32]
+        for f in (L.spec_prompt_attention_workspace_bytes, L.spec_prompt_attention_workspace_bytes_up_to):
+            f.restype = C.c_size_t
+            f.argtypes = [i32, i32, i32, i32, i32]
         L.spec_prompt_attention.argtypes = [C.POINTER(spec_prompt_attn_args), ptr, C.c_size_t, ptr]
         _lib = L
     return _lib
@@ -625,6 +627,11 @@ def spec_prompt_gemm_workspace_bytes(M: int, N: int, K: int, activation: str = "
     return int(lib().spec_prompt_gemm_workspace_bytes(M, N, K, PROMPT_ACTIVATIONS[activation]))
 
 
+def spec_prompt_gemm_workspace_bytes_up_to(M: int, N: int, K: int, activation: str = "none") -> int:
+    """The most that any number of rows up to M asks for."""
+    return int(lib().spec_prompt_gemm_workspace_bytes_up_to(M, N, K, PROMPT_ACTIVATIONS[activation]))
+
+
 def spec_prompt_gemm(x: torch.Tensor, w_packed: torch.Tensor, y: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: str = "none",
                      residual: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """y [M][N] (float32 or bfloat16) = residual + activation(x [M][K] bf16 times the packed matrix + bias); any row strides.  residual may be
@@ -651,6 +658,11 @@ def spec_prompt_append(h: Handle, layer: int, qkv: torch.Tensor, rotated: torch.
 
 def spec_prompt_attention_workspace_bytes(q_rows: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
     return int(lib().spec_prompt_attention_workspace_bytes(q_rows, batch, n_q_heads, n_kv_heads, head_dim))
+
+
+def spec_prompt_attention_workspace_bytes_up_to(q_rows: int, batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    """At least what any numbers of rows and sequences up to these ask for."""
+    return int(lib().spec_prompt_attention_workspace_bytes_up_to(q_rows, batch, n_q_heads, n_kv_heads, head_dim))
 
 
 def spec_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_q_heads: int, n_kv_heads: int, q_row0: torch.Tensor,

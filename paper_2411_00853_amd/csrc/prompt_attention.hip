@@ -597,6 +597,11 @@ struct Plan {
     size_t part_bytes;      // of the workspace, for one part of every tile
     bool by_place;          // more workgroups than places
 };
+// (one wavefront: three workgroups of heads of 128 fit a compute unit, but places for four do better than for three or two -- 16 tokens behind up to 4000
+// 45.7, 52, 46.5 us, 8 behind 6000 35.5, 35.4, 37.4 -- as shorter parts follow the ones that end first)
+int64_t places_for(int waves, int head_dim) { return 256 * (waves == 1 ? 4 : head_dim == 128 ? 2 : waves == 4 ? 3 : 4); }
+// of a tile, if one part of each of them makes wgs workgroups
+int64_t most_parts(int waves, int head_dim, int64_t wgs) { return std::min((int64_t)MOST_PARTS, 4 / waves * places_for(waves, head_dim) / wgs); }
 Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head_dim, int64_t q_len, int64_t k_len, int waves = 0)
 {
     Plan p;
@@ -605,11 +610,9 @@ Plan plan(int q_rows, int k_rows, int batch, int n_kv_heads, int group, int head
     p.tiles = (int64_t)q_rows * group / rows + batch;
     p.part_bytes = (size_t)p.tiles * n_kv_heads * rows * (head_dim + 2) * 4;
     const int64_t wgs = std::min(p.tiles, std::max((int64_t)batch, ((int64_t)q_rows * group + rows - 1) / rows)) * n_kv_heads;
-    // (one wavefront: three workgroups of heads of 128 fit a compute unit, but places for four do better than for three or two -- 16 tokens behind up to 4000
-    // 45.7, 52, 46.5 us, 8 behind 6000 35.5, 35.4, 37.4 -- as shorter parts follow the ones that end first)
-    const int64_t places = 256 * (p.waves == 1 ? 4 : head_dim == 128 ? 2 : p.waves == 4 ? 3 : 4);
+    const int64_t places = places_for(p.waves, head_dim);
     const int64_t longest = (k_len + BLK - 1) / BLK, mean = std::min(longest, (int64_t)k_rows / batch / BLK + 1);
-    const int64_t most = std::min((int64_t)MOST_PARTS, 4 / p.waves * places / wgs);
+    const int64_t most = most_parts(p.waves, head_dim, wgs);
     // One sequence: as many parts of each tile as there are places.  Several, of different lengths: the last part of a tile is rarely a whole one, and
     // a few workgroups more than there are places take as long as twice as many.
     const int64_t each = std::max((int64_t)1, places / wgs), spare = std::max(places - wgs, places / 2);
@@ -653,6 +656,23 @@ extern "C" size_t spec_prompt_attention_workspace_bytes(int32_t q_rows, int32_t 
     for (int waves = 1; waves <= 4; waves *= 2) {
         const Plan p = plan(q_rows, INT_MAX, batch, n_kv_heads, n_q_heads / n_kv_heads, head_dim, 0, INT_MAX, waves);
         most = std::max(most, p.parts > 1 ? p.parts * p.part_bytes : 0);
+    }
+    return most;
+}
+
+extern "C" size_t spec_prompt_attention_workspace_bytes_up_to(int32_t q_rows, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim)
+{
+    if (q_rows <= 0 || batch <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || n_q_heads % n_kv_heads || (head_dim != 64 && head_dim != 128)) return 0;
+    size_t most = 0;
+    for (int waves = 1; waves <= 4; waves *= 2) {
+        // x: tiles that plan() counts on, the larger one of the sequences and of the tiles that the rows fill; a launch has those that the rows fill whole
+        // and one for each sequence, x of both at most
+        const int64_t rows = 32 * waves, whole = (int64_t)q_rows * (n_q_heads / n_kv_heads) / rows, all = std::max((int64_t)batch, whole + 1);
+        for (int64_t x = 1; x <= all; ++x) {
+            const int64_t parts = most_parts(waves, head_dim, x * n_kv_heads);
+            if (parts < 2) break;
+            most = std::max(most, (size_t)(parts * (std::min(x, whole) + std::min(x, (int64_t)batch)) * n_kv_heads * rows * (head_dim + 2) * 4));
+        }
     }
     return most;
 }

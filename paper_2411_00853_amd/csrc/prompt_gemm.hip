@@ -472,6 +472,7 @@ struct Shape {
 };
 constexpr Shape SHAPES[] = {{256, 256, 3, 1.4f, 0.f}, {256, 128, 3, 0.8f, 0.f}, {192, 128, 3, 0.66f, 0.f}, {128, 256, 3, 0.8f, 0.f},
                             {128, 128, 3, 0.56f, 0.88f}, {96, 128, 3, 0.48f, 0.70f}, {64, 128, 3, 0.30f, 0.52f}, {64, 64, 4, 0.23f, 0.36f}, {32, 64, 5, 0.19f, 0.30f}};
+constexpr int MOST_ROWS = 256, MOST_SPLIT = 1024;   // rows of a tile; workgroups of a launch that shares K out
 struct Plan {
     int shape, splits, per_split;   // shape < 0: K is shared out within workgroups
     size_t floats;                  // of the workspace
@@ -493,7 +494,7 @@ Plan plan(bool gated, int M, int n_tiles, int K, size_t floats)
         for (int splits = 1; splits <= 8; ++splits) {
             const int per = (stages + splits - 1) / splits;
             const size_t need = splits > 1 ? (size_t)splits * M * n_tiles * 16 : 0;
-            if (need > floats || (splits > 1 && tiles * splits > 1024)) break;   // (nor would more of them do)
+            if (need > floats || (splits > 1 && tiles * splits > MOST_SPLIT)) break;   // (nor would more of them do)
             if (stages - (splits - 1) * per <= t.slots) continue;
             const int wgs = (int)tiles * splits, at_once = t.us2 ? 512 : 256, whole = wgs / at_once, rest = wgs % at_once;
             const float round = (float)whole * (t.us2 ? t.us2 : t.us1) + (rest == 0 ? 0.f : rest <= 256 ? t.us1 : t.us2);
@@ -540,6 +541,15 @@ extern "C" size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t
 {
     if (M <= 0 || N <= 0 || K <= 0 || M > SPEC_PROMPT_MAX_ROWS || N > MAX_COLS || K > SPEC_PROMPT_MAX_LD) return 0;
     return 4 * plan(activation == SPEC_ACT_SWIGLU, M, ((activation == SPEC_ACT_SWIGLU ? 2 * N : N) + 15) / 16, K, MOST_PARTS).floats;
+}
+
+extern "C" size_t spec_prompt_gemm_workspace_bytes_up_to(int32_t M, int32_t N, int32_t K, int32_t activation)
+{
+    if (M > SPEC_PROMPT_MAX_ROWS) return 0;
+    size_t most = 0;
+    for (int m = 1; m <= std::min(M, MOST_ROWS * MOST_SPLIT / 2); ++m)   // (more rows have too many tiles for a second part)
+        most = std::max(most, spec_prompt_gemm_workspace_bytes(m, N, K, activation));
+    return most;
 }
 
 extern "C" int spec_prompt_gemm(const void* x, int64_t ld_x, const void* w_packed, const spec_prompt_epilogue* epilogue, void* y, int32_t y_dtype,

@@ -41,8 +41,9 @@ class Prompt:
         self.tokens, self.outside = new(R, dtype=torch.int32), new(R, dtype=torch.bool)
         shapes = ((R, self.d_q + 2 * self.d_kv, d, "none"), (R, d, self.d_q, "none"), (R, c.d_ffn, d, "swiglu"), (R, d, c.d_ffn, "none"),
                   (B, c.vocab, d, "none"))
-        need = max([sv.spec_prompt_gemm_workspace_bytes(*s) for s in shapes] +
-                   [sv.spec_prompt_attention_workspace_bytes(R, B, c.n_q_heads, c.n_kv_heads, hd)])
+        # of any run that fits: short prompts share out what long ones do not
+        need = max([sv.spec_prompt_gemm_workspace_bytes_up_to(*s) for s in shapes] +
+                   [sv.spec_prompt_attention_workspace_bytes_up_to(R, B, c.n_q_heads, c.n_kv_heads, hd)])
         self.work = torch.empty(max(16, need), dtype=torch.uint8, device=dev)
 
     def run(self, tokens: torch.Tensor, row0: torch.Tensor, seq_slot: torch.Tensor, max_len: int = 0, logits: bool = True):
