@@ -312,8 +312,9 @@ __global__ void __launch_bounds__(64 * WAVES, HD == 64 && WAVES == 4 ? 3 : 2) at
 #pragma unroll
         for (int i = 2; i < 32; i += 2) top = fmaxf(fmaxf(s.v[i / 16][i % 16], s.v[i / 16][i % 16 + 1]), top);
         top = both_max(top);
-        if (__any((top - m) * A.factor > 8.f)) {
-            const float up = fmaxf(top, m);
+        const bool higher = (top - m) * A.factor > 8.f;
+        if (__any(higher)) {
+            const float up = higher ? top : m;      // (rows that need none keep theirs: their bits do not depend on the others' numbers)
             const float f = m == up ? 1.f : __builtin_amdgcn_exp2f((m - up) * A.factor);
             l[0] *= f;
             l[1] *= f;
