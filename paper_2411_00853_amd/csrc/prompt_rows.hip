@@ -355,7 +355,7 @@ extern "C" int spec_prompt_append(spec_handle* h, int32_t layer, const void* qkv
         return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: qkv, rotated and the cache have to be 16-byte aligned");
     if (qkv == rotated && rows > 1 && ld_qkv != ld_rotated) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_append: in place with two different lds");
     const int64_t kv_blocks = std::min((int64_t)rows / 32 + 2 * (int64_t)batch, (int64_t)rows);   // a sequence of n rows reaches n / 32 + 2 blocks, and n at most
-    const int64_t grid = kv_blocks * c.n_kv_heads + (rows + 15) / 16;
+    const int64_t grid = kv_blocks * c.n_kv_heads + ((int64_t)rows + 15) / 16;
     if (grid * TPB > UINT32_MAX) return fail(SPEC_ERR_SHAPE, "spec_prompt_append: %d rows are too many", rows);
     hipStream_t s = (hipStream_t)stream;
     if (h->tables.pool.table) {
