@@ -91,7 +91,7 @@ typedef struct {
     int32_t n_q_heads, n_kv_heads, head_dim;
     int32_t batch, q_rows, k_rows;
     int32_t max_q_len, max_k_len;
-    float scale;
+    float scale;               /* |scale| log2(e) a finite float */
     void* out;
 } spec_prompt_attn_args;
 size_t spec_prompt_attention_workspace_bytes(int32_t q_rows, int32_t batch, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);

@@ -12,6 +12,8 @@
 // for the next tile and look for it beside this one's first fetch: 171.)
 #include "prompt.h"
 
+#include <cfloat>
+
 namespace specv {
 namespace {
 
@@ -688,7 +690,8 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     if (a.batch < 0 || a.batch > SPEC_PROMPT_MAX_SEQS || a.q_rows < 0 || a.k_rows < 0 || a.max_q_len < 0 || a.max_k_len < 0)
         return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_attention: %d sequences (at most %d), %d query rows, %d key rows, lengths up to %d and %d", a.batch,
                     SPEC_PROMPT_MAX_SEQS, a.q_rows, a.k_rows, a.max_q_len, a.max_k_len);
-    if (!(fabsf(a.scale) <= 3.402823466e38f)) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_attention: scale %g", (double)a.scale);
+    const float factor = fabsf(a.scale) * 1.44269504088896341f;
+    if (!(factor <= FLT_MAX)) return fail(SPEC_ERR_INVALID_ARG, "spec_prompt_attention: scale %g", (double)a.scale);
     const int64_t dq = (int64_t)a.n_q_heads * a.head_dim, dk = (int64_t)a.n_kv_heads * a.head_dim;
     const struct {
         const char* name;
@@ -718,7 +721,7 @@ extern "C" int spec_prompt_attention(const spec_prompt_attn_args* args, void* wo
     float* const ws = (float*)workspace;
     const size_t rows = p.part_bytes / (a.head_dim + 2) / 4 * p.parts;
     const Args g{(const uint16_t*)a.q, (const uint16_t*)a.k, (const uint16_t*)a.v, (uint16_t*)a.out, a.ld_q, a.ld_k, a.ld_v, a.ld_out, a.q_row0,
-                 a.k_row0, FastDiv(a.n_kv_heads), FastDiv(group), a.batch, a.q_rows, a.k_rows, fmaxf(fabsf(a.scale) * 1.44269504088896341f, 0x1p-149f),
+                 a.k_row0, FastDiv(a.n_kv_heads), FastDiv(group), a.batch, a.q_rows, a.k_rows, fmaxf(factor, 0x1p-149f),
                  a.scale < 0.f ? 0x80008000u : 0u, FastDiv(p.parts), p.parts > 1 ? p.chunk : 1 << 26, p.parts > 1 ? ws : nullptr, p.parts > 1 ? ws + rows * a.head_dim : nullptr, p.by_place && p.parts == 1};
     hipStream_t s = (hipStream_t)stream;
     if (a.head_dim == 128) {
