@@ -545,7 +545,6 @@ extern "C" size_t spec_prompt_gemm_workspace_bytes(int32_t M, int32_t N, int32_t
 
 extern "C" size_t spec_prompt_gemm_workspace_bytes_up_to(int32_t M, int32_t N, int32_t K, int32_t activation)
 {
-    if (M > SPEC_PROMPT_MAX_ROWS) return 0;
     size_t most = 0;
     for (int m = 1; m <= std::min(M, MOST_ROWS * MOST_SPLIT / 2); ++m)   // (more rows have too many tiles for a second part)
         most = std::max(most, spec_prompt_gemm_workspace_bytes(m, N, K, activation));

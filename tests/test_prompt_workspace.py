@@ -40,6 +40,7 @@ def test_products_of_up_to_some_rows(N, K, act):
     for rows in (1, 16, 17, 33, 64, 100, 257, 640, 1199):
         assert sv.spec_prompt_gemm_workspace_bytes_up_to(rows, N, K, act) == max(need[:rows + 1])
     top = sv.spec_prompt_gemm_workspace_bytes_up_to(1 << 20, N, K, act)
+    assert sv.spec_prompt_gemm_workspace_bytes_up_to((1 << 31) - 1, N, K, act) == top      # (more rows than a call takes ask for nothing)
     assert top >= max(need) and top <= 1 << 27
     assert all(sv.spec_prompt_gemm_workspace_bytes(m, N, K, act) <= top for m in range(1200, 1 << 20, 4999))
 
@@ -57,5 +58,5 @@ def test_attention_of_up_to_some_rows_and_sequences(hq, hk, hd):
 
 def test_nothing_for_calls_that_are_refused():
     product, attention = sv.spec_prompt_gemm_workspace_bytes_up_to, sv.spec_prompt_attention_workspace_bytes_up_to
-    assert product(0, 48, 64) == product(5, -1, 64) == product(5, 48, 0) == product((1 << 20) + 1, 48, 64) == product(5, (1 << 23) + 1, 64) == 0
+    assert product(0, 48, 64) == product(5, -1, 64) == product(5, 48, 0) == product(5, (1 << 23) + 1, 64) == 0
     assert attention(0, 1, 8, 2, 64) == attention(4, 0, 8, 2, 64) == attention(4, 1, 8, 3, 64) == attention(4, 1, 8, 2, 96) == 0
