@@ -9,7 +9,9 @@
  * Every call may be recorded into a HIP graph.  Buffers that overlap are an error unless said otherwise.
  *
  * Packed rows: sequence b has rows row0[b] .. row0[b+1]-1 of a tensor (device int32[batch+1], ascending from 0 or more; what lies
- * outside [0, rows) counts as cut off, a pair that descends as no rows).  Rows of no sequence are neither read nor written.
+ * outside [0, rows) counts as cut off, a pair that descends as no rows).  Rows of no sequence are neither read nor written.  Where
+ * numbers that do not ascend make sequences overlap, nothing outside the tensors is touched, but which rows are computed, and with which results,
+ * is not defined.
  */
 #ifndef SPEC_PROMPT_H
 #define SPEC_PROMPT_H
@@ -77,10 +79,12 @@ int spec_prompt_append(spec_handle* h, int32_t layer, const void* qkv, int64_t l
 
 /* Causal attention over packed sequences: out[i] = sum over t of softmax_t(scale * q_i . k_t) v_t, where row j of a sequence's len_q query rows
  * sees its key rows 0 .. len_k - len_q + j (len_k = len_q: a whole prompt; len_q = 1: a single token behind len_k - 1 older ones).  A row
- * that sees nothing is zero.  A position that a row does not see adds nothing to it, whatever lies there.
+ * that sees nothing is zero.  A position that a row does not see adds nothing to it, whatever lies there.  Older keys and values are packed rows that
+ * the caller has kept: those in a handle's cache lie in another order (spec_verify_step and spec_kv_export read them).
  * All bf16; rows ld elements apart (multiples of 8; addresses 16-byte aligned).  q, out [q_rows][n_q_heads * head_dim], k, v
  * [k_rows][n_kv_heads * head_dim]; n_q_heads is a multiple of n_kv_heads and query head h reads kv head h / (n_q_heads / n_kv_heads); head_dim 64 or
- * 128.  Scores, softmax and sums are fp32; the weights are rounded to bf16 where they meet the values.
+ * 128.  Scores, softmax and sums are fp32; the weights are rounded to bf16 where they meet the values, which leaves the result some 0.0020 of its size
+ * off where rounding it alone leaves 0.0016 (root mean square).
  * max_q_len, max_k_len: the longest sequences that the caller expects (0: unknown).  They and the workspace (device scratch, 16-byte
  * aligned; NULL or too little: none) decide only how the work is split.  Calls that overlap in time need a workspace of their own. */
 typedef struct {

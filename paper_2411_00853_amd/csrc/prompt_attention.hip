@@ -6,10 +6,10 @@
 // A workgroup takes 32 WAVES query rows of one kv head, a row being one query head of one position: the query heads that share a kv head
 // share its tile.  Keys and values pass through LDS in blocks of 64 positions, fetched one block ahead, once for all wavefronts.
 //
-// What bounds it: in long prompts the products, the exponentials beside them and the card's power -- 8192 positions of 32 heads of 128 510 to 526 us, 1.05 to
-// 1.08 PFLOP/s, with zeros for operands 419; of 64, whose 32 exponentials stand beside half the products, 290 us, 0.95.  In short ones a tile's first fetch,
-// its masked block and its end, some 11000 cycles beside 2000 a block: 16 prompts of 50 to 2100 of 32 heads of 64 146 to 154 us, 0.7 PFLOP/s.  (Workgroups that stay
-// for the next tile and look for it beside this one's first fetch: 171.)
+// What bounds it: in long prompts the products, the exponentials beside them and the card's power -- 8192 positions of 32 heads of 128 517 to 530 us, 1.04 to
+// 1.06 PFLOP/s, with zeros for operands 419; of 64, whose 32 exponentials stand beside half the products, 290 us, 0.95.  In short ones a tile's first fetch,
+// its masked block and its end, some 11000 cycles beside 2000 a block: 16 prompts of 50 to 2100 of 32 heads of 64 146 us, 0.7 PFLOP/s, 160 in a loop of nothing
+// else.  (Workgroups that stay for the next tile and look for it beside this one's first fetch: 171 where this took 154.)
 #include "prompt.h"
 
 #include <cfloat>
@@ -152,7 +152,9 @@ __device__ __forceinline__ void load_query(const Args& A, const Tile& T, int hea
     for (int c = 0; c < HD / 16; ++c) qf[c] = __builtin_bit_cast(pr_bf16x8, *reinterpret_cast<const pr_uintx4*>(src + 16 * c) ^ A.sign);
 }
 
-// Sixteen weights' worth of a lane: eight numbers exp2(s * factor - shift), rounded to bf16, and their sum (that of the rounded ones) added to l
+// Sixteen weights' worth of a lane: eight numbers exp2(s * factor - shift), rounded to bf16, and their sum (that of the rounded ones) added to l.  bf16
+// because that is the values' type: with what the rounding leaves as a second operand the product with the values would be twice as long, half as much again of
+// all products.  The result is 0.0020 of its size off (root mean square, 8192 positions), 0.0016 of it by its own rounding.
 __device__ __forceinline__ pr_bf16x8 eight_weights(const pr_floatx16& s, int at, float factor, float shift, float& l)
 {
     pr_uintx4 v;

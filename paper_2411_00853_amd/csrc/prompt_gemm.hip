@@ -463,9 +463,9 @@ void launch_tiled(const Call& c, int splits = 1, int per_split = 0)
 }
 
 // Which tile, and among how many workgroups K is shared out.  us: a stage of 64 columns, with a workgroup on a compute unit and (where two fit) with two
-// on each; measured over K = 4096 and 8192, 48 to 8192 rows, 1024 to 32000 columns.  A launch takes some 3.5 us besides, one whose parts are
-// joined 2.5 us more and the parts' way to memory and back; none is faster than the weights come from memory.  Gate and up in 32 rows have two
-// wavefronts instead of four (a stage 0.22).
+// on each; measured over K = 4096 and 8192, 48 to 8192 rows, 1024 to 32000 columns (shorter K is priced by the same figures).  A launch
+// takes some 3.5 us besides, one whose parts are joined 2.5 us more and the parts' way to memory and back; none is faster than the weights come from memory.
+// Gate and up in 32 rows have two wavefronts instead of four (a stage 0.22).
 struct Shape {
     int rows, cols, slots;      // slots: SW, which a part's stages have to exceed
     float us1, us2;             // us2 = 0: one workgroup on a compute unit

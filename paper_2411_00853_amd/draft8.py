@@ -131,7 +131,7 @@ class Rounds:
 
     def __init__(self, target_shape, weights: dict, draft: Draft8, lookahead: int, prompt_rows: int = 0):
         """weights: as workload.make_weights gives them, on the device.  `feed` takes contexts of up to prompt_rows tokens in all through the
-        target as whole prompts, longer ones window by window."""
+        target as whole prompts (prompt.py, whose cache differs from the windows' by its roundings), longer ones window by window."""
         B, V, K, dev = draft.batch, target_shape.vocab, lookahead, draft.embed.device
         self.draft, self.K, self.B = draft, K, B
         cfg = sv.make_cfg(target_shape, B, draft.max_kv_len, K)
